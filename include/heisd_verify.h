@@ -337,6 +337,175 @@ int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int32_t d, con
                                float *top_score, int32_t *top_payload, void *stream);
 
 /*
+ * Many requests from one pool: block tables, rotary positions, a cache held in 4 bits and the attention over it, and
+ * attention of packed prompts with grouped heads.  These calls serve decoders (or batches of episodes) whose caches do not
+ * fit the contiguous bf16 layout of heisd_kv_desc: contexts of different lengths share a pool of blocks, several query heads
+ * share a key head, and a cached row takes 17/64 of its bf16 bytes.  Used together, per step and layer:
+ *   heisd_paged_plan (once per step) -> heisd_rope -> heisd_kv4_append -> heisd_kv4_attention (single tokens, drafts) or
+ *   heisd_prompt_attention (prompts; with heisd_kv4_gather, chunks behind cached rows).
+ * All are asynchronous on `stream`, allocate nothing, keep nothing between calls, and run on the current device, whose memory
+ * every DEVICE pointer must belong to.  Results do not depend on timing (no floating-point atomics).  Errors are found before
+ * anything is enqueued; heisd_last_error(NULL) has the text.  Calls with no rows return OK and enqueue nothing (heisd_paged_plan always runs).
+ */
+#define HEISD_DTYPE_BF16 0
+#define HEISD_DTYPE_F16 1
+#define HEISD_DTYPE_F32 2
+
+/* Rows of heads: element i of head h of row r is data[r * row_stride + h * head_stride + i] (strides in elements, at least
+ * 0).  Any order of rows and heads fits; the values of a head are adjacent. */
+typedef struct {
+  void *data;                       /* DEVICE */
+  int64_t row_stride, head_stride;
+  int32_t heads;                    /* 1 .. 512 */
+  int32_t dtype;                    /* HEISD_DTYPE_* */
+} heisd_head_rows;
+
+/*
+ * Block tables, slots and positions from the requests' lengths.  A pool has n_blocks blocks of block_size tokens; request b
+ * owns the blocks block_table[b][0 .. owned[b]-1], and token t of it lies in slot block_table[b][t / block_size] * block_size +
+ * t % block_size.  One call extends every request by its new rows:
+ *   - a request with a negative cached_len is finished: its owned blocks are put on top of the free ones (in request and
+ *     table order) and it owns none; its row of the table stays as it was;
+ *   - every other request gets the blocks that its cached_len + new_len tokens need beyond those it owns, from the top of the
+ *     free ones, in request order (blocks that were given back are used first).  Blocks owned beyond that stay owned, so a
+ *     cache that shrinks again (rejected drafts) costs nothing;
+ *   - first come, first served: a request that needs more blocks than are left gets none, and neither does any later one that
+ *     needs some.  Such a request, one with a negative new_len, one whose tokens do not fit max_blocks blocks and one whose
+ *     rows do not fit `rows` is left out: seq_len -1, slots and positions -1, blocks unchanged.
+ *   cached_len     DEVICE i32 [batch]       tokens in the cache (negative: finished)
+ *   new_len        DEVICE i32 [batch]       tokens that are added (0 is fine); a finished request's rows get slot -1
+ *   owned_in       DEVICE i32 [batch]       blocks owned before; owned_out [batch] out: after
+ *   block_table    DEVICE i32 [batch][max_blocks] in, out (only new entries are written)
+ *   free_ids       DEVICE i32 [n_blocks] in, out: the free blocks are entries 0 .. *free_count_in - 1, the last is taken first;
+ *                  entries above the new count keep the blocks that were taken.  *free_count_out out: free ones after
+ *   cu_rows        DEVICE i32 [batch+1] out the new rows of request b are packed rows cu_rows[b] .. cu_rows[b+1]-1
+ *   seq_len        DEVICE i32 [batch] out   cached_len + new_len; -1 for finished requests and those left out
+ *   cu_seq         DEVICE i32 [batch+1] out, optional (NULL ok): prefix sums of seq_len (negative ones count 0)
+ *   slot, position DEVICE i32 [rows] out    of every packed row; -1 for rows of nobody (a padded batch) or left out
+ * owned_out may be owned_in and free_count_out free_count_in; no other buffers may overlap.  A table entry outside
+ * [0, n_blocks) gives slot -1.  rows: at least the sum of new_len.
+ * Errors: EINVAL (NULL, batch outside 1..65535, sizes: at most 2^31-1 slots, 2^20 blocks per request, 2^30 rows), EHIP.
+ */
+typedef struct {
+  int32_t batch, block_size, max_blocks, n_blocks, rows;
+  const int32_t *cached_len, *new_len, *owned_in;
+  int32_t *owned_out, *block_table, *free_ids;
+  const int32_t *free_count_in;
+  int32_t *free_count_out, *cu_rows, *seq_len, *slot, *position, *cu_seq;
+} heisd_plan_desc;
+int heisd_paged_plan(const heisd_plan_desc *plan, void *stream);
+
+/*
+ * Rotary positions.  heisd_rope_table computes on the HOST, in 64 bits, the turns per position of every pair, base^(-2 i /
+ * rotary_dim) / (2 pi), and the factor on cos and sin; the caller copies turns to the device once.  Scaling for contexts longer than a
+ * model was trained on:
+ *   NONE    LINEAR  every frequency / factor        BASE  base * factor^(n / (n - 2)), n = rotary_dim (n = 2: unchanged)
+ *   PARTS   pairs that turn more than beta_fast times within original_len keep their frequency, those that turn less than
+ *           beta_slow times have it divided by factor, a ramp over the pair's index between; factor on cos and sin 0.1 ln(factor) + 1
+ *   BANDS   the same by turns within original_len: high_freq or more kept, low_freq or less divided, a ramp over the turns between
+ *   turns      HOST f64 [rotary_dim / 2] out      magnitude  HOST f32 out
+ * heisd_rope rotates pairs (a, b) of the first rotary_dim values of every head by angle = position * frequency: (a cos - b sin,
+ * b cos + a sin) * magnitude.  HALF: a = x[i], b = x[i + rotary_dim / 2]; INTERLEAVED: a = x[2 i], b = x[2 i + 1].  inverse != 0
+ * is the transposed rotation (by the negative angle, the same magnitude): the gradient with respect to the input, from that with respect
+ * to the output.  Values behind rotary_dim are copied.  A row with a negative position is left out: nothing of it is read or written.
+ *   turns      DEVICE f64 [rotary_dim / 2]        position DEVICE i32 [rows]
+ *   q -> q_out, k -> k_out (k and k_out may be NULL together): the same heads and dtype (any of the three); in place when the
+ *   data pointers and strides are equal, otherwise not overlapping.  16-byte aligned rows (pointers, strides) with parts of a multiple of 16
+ *   bytes are fastest; anything else works element by element.
+ * head_dim <= 256, rotary_dim even and <= head_dim.  Angles are reduced in 64 bits: exact to fp32 rounding at any position.
+ * Errors: EINVAL, EHIP.
+ */
+#define HEISD_ROPE_HALF 0
+#define HEISD_ROPE_INTERLEAVED 1
+#define HEISD_ROPE_NONE 0
+#define HEISD_ROPE_LINEAR 1
+#define HEISD_ROPE_BASE 2
+#define HEISD_ROPE_PARTS 3
+#define HEISD_ROPE_BANDS 4
+typedef struct {
+  int32_t rotary_dim, scaling, original_len;
+  double base, factor, beta_fast, beta_slow, low_freq, high_freq;
+} heisd_rope_desc;
+int heisd_rope_table(const heisd_rope_desc *desc, double *turns, float *magnitude);
+int heisd_rope(const double *turns, float magnitude, int32_t rotary_dim, int32_t layout, int32_t inverse, const int32_t *position,
+               int32_t rows, int32_t head_dim, const heisd_head_rows *q, const heisd_head_rows *q_out, const heisd_head_rows *k,
+               const heisd_head_rows *k_out, void *stream);
+
+/*
+ * A cache of one layer in 4 bits.  Every group of 32 values of a row of one head is held as 4-bit floats (sign, two bits of
+ * exponent, one of mantissa: magnitudes 0 .5 1 1.5 2 3 4 6; round to nearest, ties to the even code) times 2^(e - 127), one byte
+ * e: the smallest e >= 1 for which the largest magnitude is at most 6 * 2^(e - 127).  A group with a value that is not finite is
+ * held as e = 255 and reads as NaN.  The pool is [n_blocks][kv_heads] cells of block_size * (head_dim + head_dim / 16) bytes: key
+ * codes [token][head_dim / 2], value codes [token / 4][16][token % 4][head_dim / 32], key exponents [token][head_dim / 32],
+ * value exponents [token / 4][head_dim / 32][token % 4]; in a byte of codes the lower-numbered value has the low half.  Nothing has to be
+ * cleared: what was never written is never read.
+ *   pool  DEVICE, 16-byte aligned, heisd_kv4_pool_bytes(...) bytes (0: invalid sizes)
+ * head_dim 64 or 128; block_size a power of two, 16 .. 4096; kv_heads 1 .. 512; at most 2^31 - 1 slots.
+ */
+typedef struct {
+  void *pool;
+  int32_t n_blocks, block_size, kv_heads, head_dim;
+} heisd_kv4_desc;
+size_t heisd_kv4_pool_bytes(int32_t n_blocks, int32_t block_size, int32_t kv_heads, int32_t head_dim);
+
+/* The requests of a call, as heisd_paged_plan leaves them (all DEVICE).  rows: packed query rows.  A request with a negative
+ * seq_len has no tokens; entries of cu_rows that decrease or leave [0, rows] describe no rows.  A table entry outside [0, n_blocks) stands for
+ * a block that is not there: its tokens are seen by nobody. */
+typedef struct {
+  const int32_t *block_table;  /* i32 [batch][max_blocks] */
+  const int32_t *seq_len;      /* i32 [batch]             */
+  const int32_t *cu_rows;      /* i32 [batch+1]; not read by heisd_kv4_gather */
+  int32_t batch, max_blocks, rows;
+} heisd_paged_batch;
+
+/*
+ * heisd_kv4_append writes row r of k and v into slot[r] (a slot outside the pool: the row is left out).  Two rows with one slot:
+ * what the slot then holds is undefined (nothing else is touched).  Any dtype, the same for k and v; 16-byte aligned rows are fastest.
+ * heisd_kv4_gather reads tokens 0 .. seq_len[b]-1 of every request back into packed rows cu_seq[b] .. (keys and values of earlier chunks for
+ * heisd_prompt_attention): the values they stand for, rounded to the outputs' dtype.  Rows of a missing block are zero; rows that no
+ * token belongs to (a request whose span in cu_seq is longer than its seq_len, rows behind the last request) are left as they were.
+ *   slot    DEVICE i32 [rows]          cu_seq  DEVICE i32 [batch+1], at most out_rows
+ * Errors: EINVAL, EUNSUPPORTED (head_dim), EHIP.
+ */
+int heisd_kv4_append(const heisd_kv4_desc *cache, const heisd_head_rows *k, const heisd_head_rows *v, const int32_t *slot, int32_t rows,
+                     void *stream);
+int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const int32_t *cu_seq, int32_t out_rows,
+                     const heisd_head_rows *k_out, const heisd_head_rows *v_out, void *stream);
+
+/*
+ * Attention over that cache: out[r][h] = softmax(scale * q[r][h] . K) V over the tokens that row r sees, with K and V of key head
+ * h / (q heads / kv_heads).  Row i of the n rows of request b sees tokens 0 .. seq_len[b] - n + i (the new rows are in the cache
+ * already and are its last n tokens).  A row that sees no token gives zeros and lse -inf; packed rows behind the last request are left
+ * as they were.  One token per request, drafts of several, whole chunks: any number of rows, at its best with few per request.
+ *   q, out    bf16 or fp16 (the same); q 16-byte aligned in pointer and strides, out 8
+ *   lse       DEVICE f32 [rows][q heads] out, optional (NULL ok): log of the sum of exp(scale * q . K)
+ *   max_q     at least the largest number of rows of a request (larger ones are computed too, more slowly)
+ *   max_seq   at least the largest seq_len, at most 2^24; a request with more is treated as one without tokens
+ *   workspace DEVICE, 256-byte aligned, heisd_kv4_attention_workspace_bytes(...) bytes (0: invalid sizes) for the same batch, rows,
+ *             heads, max_q and max_seq; nothing in it has to be cleared, two calls that may overlap in time need one each
+ * Scores, sums and the softmax are fp32; bf16 queries enter the matrix products as they are and probabilities as one bf16, fp16 ones and
+ * their probabilities as two.  Errors: EINVAL, EUNSUPPORTED (head_dim, fp32), ENOMEM (workspace), EHIP.
+ */
+size_t heisd_kv4_attention_workspace_bytes(const heisd_kv4_desc *cache, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_q,
+                                           int32_t max_seq);
+int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_head_rows *q, const heisd_head_rows *out,
+                        float *lse, float scale, int32_t max_q, int32_t max_seq, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of packed sequences: sequence b has query rows cu_q[b] .. cu_q[b+1]-1 and key rows cu_k[b] .. cu_k[b+1]-1.  causal != 0: row i
+ * of n sees keys 0 .. (number of keys) - n + i, so that queries are the last rows of their keys (a chunk behind earlier rows); 0: all of
+ * them.  Query head h reads key head h / (q heads / k heads).  Rows that see nothing give zeros and lse -inf; rows of no sequence are
+ * left as they were.  What a masked row of k or v holds (infinities, NaN) has no influence.
+ *   q, k, v, out  bf16 or fp16 (all the same); q, k, v 16-byte aligned in pointer and strides, out 8
+ *   lse           DEVICE f32 [rows][q heads] out, optional     rows, k_rows  rows in q and out, in k and v
+ * head_dim 64 or 128.  Scores, sums and the softmax are fp32, probabilities enter the second product in the rows' dtype.
+ * Errors: EINVAL, EUNSUPPORTED (head_dim, fp32), EHIP.
+ */
+int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out, float *lse,
+                           const int32_t *cu_q, const int32_t *cu_k, int32_t batch, int32_t rows, int32_t k_rows, int32_t head_dim, float scale,
+                           int32_t causal, void *stream);
+
+/*
  * Per-kernel timing for measurement runs (not part of the method).  With profiling enabled,
  * heisd_verify_step brackets every kernel launch with HIP events on the caller's stream;
  * heisd_verify_profile_read waits for the recorded events, adds the elapsed milliseconds
@@ -495,7 +664,7 @@ int heisd_measure_empty_launch(int32_t workgroups, void *stream);
 void heisd_free(heisd_verify_ctx *ctx);
 
 /* HOST string describing the last error of this context ("" if none); for ctx == NULL, the
- * last error of a failed heisd_verify_init on this thread. */
+ * last error on this thread of heisd_verify_init or of a call without a context. */
 const char *heisd_last_error(const heisd_verify_ctx *ctx);
 
 #ifdef __cplusplus

@@ -39,6 +39,34 @@ class heisd_accept_desc(Structure):
                 ("mode", c_int32)]
 
 
+class heisd_head_rows(Structure):
+    _fields_ = [("data", c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("heads", c_int32),
+                ("dtype", c_int32)]
+
+
+class heisd_plan_desc(Structure):
+    _fields_ = [(n, c_int32) for n in ("batch", "block_size", "max_blocks", "n_blocks", "rows")] + \
+               [(n, c_void_p) for n in ("cached_len", "new_len", "owned_in", "owned_out", "block_table", "free_ids", "free_count_in",
+                                        "free_count_out", "cu_rows", "seq_len", "slot", "position", "cu_seq")]
+
+
+class heisd_rope_desc(Structure):
+    _fields_ = [("rotary_dim", c_int32), ("scaling", c_int32), ("original_len", c_int32)] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "beta_fast", "beta_slow", "low_freq", "high_freq")]
+
+
+class heisd_kv4_desc(Structure):
+    _fields_ = [("pool", c_void_p)] + [(n, c_int32) for n in ("n_blocks", "block_size", "kv_heads", "head_dim")]
+
+
+class heisd_paged_batch(Structure):
+    _fields_ = [(n, c_void_p) for n in ("block_table", "seq_len", "cu_rows")] + [(n, c_int32) for n in ("batch", "max_blocks", "rows")]
+
+
+HEISD_DTYPE_BF16, HEISD_DTYPE_F16, HEISD_DTYPE_F32 = 0, 1, 2
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
+
 _lib = None
 
 
@@ -88,6 +116,28 @@ def load():
         lib.heisd_retrieve_topk_static.argtypes = [c_void_p, ctypes.c_int64, c_int32, c_void_p, c_int32, c_int32,
                                                    c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
         lib.heisd_retrieve_topk_static.restype = ctypes.c_int
+        rows_p, kv4_p, paged_p = POINTER(heisd_head_rows), POINTER(heisd_kv4_desc), POINTER(heisd_paged_batch)
+        lib.heisd_paged_plan.argtypes = [POINTER(heisd_plan_desc), c_void_p]
+        lib.heisd_paged_plan.restype = ctypes.c_int
+        lib.heisd_rope_table.argtypes = [POINTER(heisd_rope_desc), c_void_p, POINTER(c_float)]
+        lib.heisd_rope_table.restype = ctypes.c_int
+        lib.heisd_rope.argtypes = [c_void_p, c_float, c_int32, c_int32, c_int32, c_void_p, c_int32, c_int32, rows_p, rows_p, rows_p,
+                                   rows_p, c_void_p]
+        lib.heisd_rope.restype = ctypes.c_int
+        lib.heisd_kv4_pool_bytes.argtypes = [c_int32, c_int32, c_int32, c_int32]
+        lib.heisd_kv4_pool_bytes.restype = c_size_t
+        lib.heisd_kv4_append.argtypes = [kv4_p, rows_p, rows_p, c_void_p, c_int32, c_void_p]
+        lib.heisd_kv4_append.restype = ctypes.c_int
+        lib.heisd_kv4_gather.argtypes = [kv4_p, paged_p, c_void_p, c_int32, rows_p, rows_p, c_void_p]
+        lib.heisd_kv4_gather.restype = ctypes.c_int
+        lib.heisd_kv4_attention_workspace_bytes.argtypes = [kv4_p, c_int32, c_int32, c_int32, c_int32, c_int32]
+        lib.heisd_kv4_attention_workspace_bytes.restype = c_size_t
+        lib.heisd_kv4_attention.argtypes = [kv4_p, paged_p, rows_p, rows_p, c_void_p, c_float, c_int32, c_int32, c_void_p, c_size_t,
+                                            c_void_p]
+        lib.heisd_kv4_attention.restype = ctypes.c_int
+        lib.heisd_prompt_attention.argtypes = [rows_p, rows_p, rows_p, rows_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                               c_int32, c_float, c_int32, c_void_p]
+        lib.heisd_prompt_attention.restype = ctypes.c_int
         lib.heisd_free.argtypes = [c_void_p]
         lib.heisd_free.restype = None
         lib.heisd_verify_profile_enable.argtypes = [c_void_p, ctypes.c_int]
@@ -200,6 +250,58 @@ def heisd_retrieve_topk_static(db, n_vectors, d, queries, batch, K, payload, pay
     """All array arguments are integer device addresses (0/None = NULL)."""
     return load().heisd_retrieve_topk_static(db, n_vectors, d, queries, batch, K, payload, payload_len, top_index,
                                              top_score, top_payload, stream)
+
+
+def _ref(desc):
+    return ctypes.byref(desc) if desc is not None else None
+
+
+def heisd_paged_plan(plan: heisd_plan_desc, stream) -> int:
+    return load().heisd_paged_plan(_ref(plan), stream)
+
+
+def heisd_rope_table(desc: heisd_rope_desc):
+    """Returns (rc, turns per position of every pair, magnitude)."""
+    n = max(int(desc.rotary_dim), 0) // 2 if desc is not None else 0
+    turns, magnitude = (ctypes.c_double * max(n, 1))(), c_float(0)
+    rc = load().heisd_rope_table(_ref(desc), turns, ctypes.byref(magnitude))
+    return rc, list(turns)[:n], float(magnitude.value)
+
+
+def heisd_rope(turns, magnitude, rotary_dim, layout, inverse, position, rows, head_dim, q: heisd_head_rows, q_out: heisd_head_rows, k,
+               k_out, stream) -> int:
+    """turns, position: integer device addresses; k and k_out may be None together."""
+    return load().heisd_rope(turns, magnitude, rotary_dim, layout, inverse, position, rows, head_dim, _ref(q), _ref(q_out), _ref(k),
+                             _ref(k_out), stream)
+
+
+def heisd_kv4_pool_bytes(n_blocks, block_size, kv_heads, head_dim) -> int:
+    return int(load().heisd_kv4_pool_bytes(n_blocks, block_size, kv_heads, head_dim))
+
+
+def heisd_kv4_append(cache: heisd_kv4_desc, k: heisd_head_rows, v: heisd_head_rows, slot, rows, stream) -> int:
+    return load().heisd_kv4_append(_ref(cache), _ref(k), _ref(v), slot, rows, stream)
+
+
+def heisd_kv4_gather(cache: heisd_kv4_desc, batch: heisd_paged_batch, cu_seq, out_rows, k_out: heisd_head_rows, v_out: heisd_head_rows,
+                     stream) -> int:
+    return load().heisd_kv4_gather(_ref(cache), _ref(batch), cu_seq, out_rows, _ref(k_out), _ref(v_out), stream)
+
+
+def heisd_kv4_attention_workspace_bytes(cache: heisd_kv4_desc, batch, rows, q_heads, max_q, max_seq) -> int:
+    return int(load().heisd_kv4_attention_workspace_bytes(_ref(cache), batch, rows, q_heads, max_q, max_seq))
+
+
+def heisd_kv4_attention(cache: heisd_kv4_desc, batch: heisd_paged_batch, q: heisd_head_rows, out: heisd_head_rows, lse, scale, max_q, max_seq,
+                        workspace, workspace_bytes, stream) -> int:
+    return load().heisd_kv4_attention(_ref(cache), _ref(batch), _ref(q), _ref(out), lse, scale, max_q, max_seq, workspace,
+                                      workspace_bytes, stream)
+
+
+def heisd_prompt_attention(q: heisd_head_rows, k: heisd_head_rows, v: heisd_head_rows, out: heisd_head_rows, lse, cu_q, cu_k, batch, rows, k_rows,
+                           head_dim, scale, causal, stream) -> int:
+    return load().heisd_prompt_attention(_ref(q), _ref(k), _ref(v), _ref(out), lse, cu_q, cu_k, batch, rows, k_rows, head_dim, scale, causal,
+                                         stream)
 
 
 def heisd_free(ctx) -> None:

@@ -23,6 +23,9 @@
 #include "heisd_skip.h"
 #include "heisd_retrieve.h"
 #include "heisd_measure.h"
+#include "heisd_paged.h"
+#include "heisd_kv4.h"
+#include "heisd_prompt.h"
 
 using namespace heisd;
 
@@ -2199,6 +2202,8 @@ extern "C" int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int
   return retrieve_enqueue(rd, lay, rd->scratch, db, n_vectors, d, queries, batch, K, payload, payload_len, top_index,
                           top_score, top_payload, static_cast<hipStream_t>(stream), who);
 }
+
+#include "heisd_paged_api.h"
 
 // ---- reference measurements (not part of the method) ---------------------------------------------
 

@@ -1,0 +1,233 @@
+// Attention of packed prompts: whole sequences or chunks of them behind earlier rows, grouped heads, causal or not.
+#pragma once
+#include "heisd_common.h"
+#include "heisd_paged.h"
+
+namespace heisd {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+template <typename T>
+struct MatrixOf;
+template <>
+struct MatrixOf<__bf16> {
+  typedef bf16x8 x8;
+  static __device__ __forceinline__ f32x16 mul(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static constexpr uint32_t kExp = 0x7F807F80u, kOne = 0x00800080u;
+};
+template <>
+struct MatrixOf<_Float16> {
+  typedef f16x8 x8;
+  static __device__ __forceinline__ f32x16 mul(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static constexpr uint32_t kExp = 0x7C007C00u, kOne = 0x04000400u;
+};
+// Nonzero if one of two 16-bit floats has an exponent of ones (infinite or NaN).
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t two) {
+  return ((two & MatrixOf<T>::kExp) + MatrixOf<T>::kOne) & 0x80008000u;
+}
+
+constexpr int kPromptRows = 128, kPromptKeys = 64, kPromptWaves = 4;
+constexpr float kPromptLazy = 8.f;                  // the maximum is moved only when it grew by more than this (powers of two)
+
+template <int HD>
+constexpr int prompt_lds_bytes() { return 2 * 2 * kPromptKeys * HD * 2; }
+
+struct PromptArgs {
+  const int32_t *cu_q, *cu_k;
+  int batch, rows, k_rows, q_heads, kv_heads, group;
+  int tiles;                                        // row tiles in the grid
+  float scale_log2;                                 // softmax scale times log2(e)
+  float *lse;
+};
+
+// The plain loop, for the rows of a wave that met a value that is not finite among masked ones: a matrix product would multiply it
+// by a probability of zero, which is NaN.  One token after the other, 64 lanes over the channels.
+template <typename T, int HD, bool CAUSAL>
+__device__ __forceinline__ void prompt_rows_plain(HeadRows<const T> q, HeadRows<const T> k, HeadRows<const T> v, HeadRows<T> out, PromptArgs a,
+                                               int row0, int n_rows, int head, int k_row0, int n_keys, int shift) {
+  constexpr int V = HD / 64;
+  const int lane = threadIdx.x & 63, kvh = head / a.group;
+  for (int i = 0; i < n_rows; ++i) {
+    float x[V], y[V], o[V] = {}, m = -INFINITY, l = 0.f;
+    load_vec<T, V>(q.at(row0 + i, head) + lane * V, x);
+    const int seen = CAUSAL ? min(n_keys, shift + i + 1) : n_keys;
+    for (int t = 0; t < seen; ++t) {
+      load_vec<T, V>(k.at(k_row0 + t, kvh) + lane * V, y);
+      float s = 0.f;
+      for (int n = 0; n < V; ++n) s += x[n] * y[n];
+      s = wave_sum(s) * a.scale_log2;
+      load_vec<T, V>(v.at(k_row0 + t, kvh) + lane * V, y);
+      const float next = fmaxf(m, s), use = next == -INFINITY ? 0.f : next;
+      const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - use), p = __builtin_amdgcn_exp2f(s - use);
+      m = next;
+      l = l * by + p;
+      for (int n = 0; n < V; ++n) o[n] = o[n] * by + p * y[n];
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    for (int n = 0; n < V; ++n) o[n] *= inv;
+    store_vec<T, V>(out.at(row0 + i, head) + lane * V, o);
+    if (a.lse && lane == 0) a.lse[(long long)(row0 + i) * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+// softmax(q K^T) V.  A workgroup has 128 rows of one sequence and head, a wave 32 of them as the columns of its products:
+// scores^T = K q^T (64 keys at a time), out^T = V^T p^T.  A lane then holds 32 scores of one row, so maximum and sum need one exchange
+// (with lane + 32), rescaling is a multiplication by the lane's own factor, and the probabilities are the second product's
+// operand as they stand: its eight summed indices per lane are two runs of four keys, and the transposed LDS read delivers V in just that
+// order.  K and V go to LDS by direct transfers, two buffers, one barrier per 64 keys; 16-byte pieces are permuted within a row by
+// the row's number so that neither read meets bank conflicts.
+template <typename T, int HD, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, HeadRows<const T> k, HeadRows<const T> v, HeadRows<T> out,
+                                                       PromptArgs a) {
+  typedef typename MatrixOf<T>::x8 x8;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr int RB = HD * 2, CH = RB / 16, TILE = kPromptKeys * RB;                // bytes of a row, 16-byte pieces of it, a tile
+  constexpr int NS = HD / 16, ND = HD / 32, NT = kPromptKeys / 32, NK = kPromptKeys / 16;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
+  const int head = kvh * a.group + rest % a.group, tile = a.tiles - 1 - rest / a.group;
+  // which sequence: sequence i is given tiles floor(cu[i] / 128) + i and on, enough for any length
+  const int seq = wave_search(a.batch, tile, [&](int i) { return (long long)max(a.cu_q[i], 0) / kPromptRows + i; });
+  const Span rows = packed_span(a.cu_q, seq, a.rows), keys = packed_span(a.cu_k, seq, a.k_rows);
+  const int first = (tile - (rows.begin / kPromptRows + seq)) * kPromptRows;
+  if (first < 0 || first >= rows.count) return;
+  const int shift = CAUSAL ? keys.count - rows.count : 0;                          // row i sees keys 0 .. shift + i
+  const int n_keys = CAUSAL ? max(min(keys.count, shift + min(first + kPromptRows, rows.count)), 0) : keys.count;
+  const int mine = first + wave * 32, my_rows = min(max(rows.count - mine, 0), 32);   // the wave's rows
+  const int my_row = min(mine + col, rows.count - 1);
+  const int seen = CAUSAL ? min(keys.count, shift + my_row + 1) : keys.count;
+  const int all_see = CAUSAL ? min(keys.count, shift + mine + 1) : keys.count;        // keys that every row of the wave sees
+  const int some_see = CAUSAL ? min(n_keys, shift + min(mine + 32, rows.count)) : keys.count;   // ... that some row sees
+
+  x8 qf[NS];
+  {
+    const T *p = q.at(rows.begin + my_row, head) + half * 8;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const x8 *>(p + s * 16);
+  }
+  f32x16 acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  uint32_t odd = 0;
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+  constexpr int RP = 1024 / RB, NP = kPromptKeys / RP / kPromptWaves;              // rows per transfer, transfers per wave and matrix
+  auto stage = [&](int block, int buf) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      const int piece = n * kPromptWaves + wave;
+      const int row = piece * RP + lane / CH, chunk = (lane % CH) ^ (row % CH);
+      const int key = keys.begin + min(block * kPromptKeys + row, n_keys - 1);     // past the end: the last one again, masked
+      lds_dma16(k.at(key, kvh) + chunk * 8, __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + piece * 1024));
+      lds_dma16(v.at(key, kvh) + chunk * 8, __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + TILE + piece * 1024));
+    }
+  };
+  // byte offsets of the lane's reads; rows further on are constants away
+  uint32_t k_at[NS], v_at[ND][2];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) k_at[s] = col * RB + (((2 * s + half) ^ (col % CH)) << 4);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = 8 * e + 4 * half + ((lane & 15) >> 2), chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      v_at[d][e] = row * RB + ((chunk ^ (row % CH)) << 4) + (lane & 1) * 8;
+    }
+
+  const int n_blocks = (n_keys + kPromptKeys - 1) / kPromptKeys;
+  wait_vmcnt_all();
+  if (n_blocks > 0) stage(0, 0);
+  for (int blk = 0; blk < n_blocks; ++blk) {
+    const int buf = blk & 1, base = blk * kPromptKeys;
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (blk + 1 < n_blocks) stage(blk + 1, buf ^ 1);
+    if (base >= some_see) continue;
+    const unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE;
+    f32x16 s[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+        s[t] = MatrixOf<T>::mul(*reinterpret_cast<const x8 *>(kt + k_at[n] + t * 32 * RB), qf[n], s[t]);
+    }
+    const bool masked = base + kPromptKeys > all_see;
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float x = s[t][e] * a.scale_log2;
+        if (masked && base + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) x = -INFINITY;
+        s[t][e] = x;
+        top = fmaxf(top, x);
+      }
+    if (masked) {
+#pragma unroll 4
+      for (int i = 0; i < TILE / 1024; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + i * 1024 + lane * 16);
+        odd |= not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
+      }
+    }
+    top = max_xor32(top);
+    if (__ballot(top > m + kPromptLazy)) {
+      const float next = fmaxf(m, top);
+      const float by = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= by;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d] *= by;
+    }
+    const float use = m == -INFINITY ? 0.f : m;
+    x8 pf[NK];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(s[t][e] - use);
+        l += p;
+        pf[2 * t + (e >> 3)][e & 7] = (T)p;
+      }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int n = 0; n < NK; ++n) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][0] + n * 16 * RB));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][1] + n * 16 * RB));
+        struct Both { s16x4 a, b; } both = {lo, hi};
+        const x8 vf = __builtin_bit_cast(x8, both);
+        acc[d] = MatrixOf<T>::mul(vf, pf[n], acc[d]);
+      }
+  }
+  if (my_rows == 0) return;
+  if (__ballot(odd != 0)) {
+    prompt_rows_plain<T, HD, CAUSAL>(q, k, v, out, a, rows.begin + mine, my_rows, head, keys.begin, keys.count, shift + mine);
+    return;
+  }
+  l = sum_xor32(l);
+  if (col >= my_rows) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const long long r = rows.begin + mine + col;
+  T *o = out.at(r, head);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float f[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = acc[d][4 * e + i] * inv;
+      store_vec<T, 4>(o + d * 32 + e * 8 + half * 4, f);
+    }
+  if (a.lse && half == 0) a.lse[r * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+}  // namespace heisd

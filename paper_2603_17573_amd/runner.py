@@ -159,3 +159,65 @@ def build_sequence_tree(candidates, accept, max_tokens):
     if rc != 0:
         raise RuntimeError("heisd_build_sequence_tree failed (%d): %s" % (rc, B.heisd_last_error(None)))
     return tokens[:n].copy(), parent[:n].copy()
+
+
+# ---- requests that share one pool ---------------------------------------------------------------------------------
+
+_DTYPE = {torch.bfloat16: B.HEISD_DTYPE_BF16, torch.float16: B.HEISD_DTYPE_F16, torch.float32: B.HEISD_DTYPE_F32}
+
+
+def head_rows(t: torch.Tensor) -> B.heisd_head_rows:
+    """[rows, heads, head_dim] in any order of rows and heads; the values of a head must be adjacent."""
+    if t.dim() != 3 or t.dtype not in _DTYPE or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("expected [rows, heads, head_dim] of bf16, fp16 or fp32 with adjacent values, got %s %s strides %s"
+                         % (tuple(t.shape), t.dtype, t.stride()))
+    return B.heisd_head_rows(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _DTYPE[t.dtype])
+
+
+def _ints(t, shape, what):
+    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: expected contiguous int32 %s, got %s %s" % (what, tuple(shape), t.dtype, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def make_plan_desc(block_size, n_blocks, cached_len, new_len, owned_in, owned_out, block_table, free_ids, free_count_in, free_count_out,
+                   seq_len, cu_rows, slot, position, cu_seq=None) -> B.heisd_plan_desc:
+    """The tensors of one heisd_paged_plan call, which must stay alive as long as the descriptor is used."""
+    b, rows = cached_len.shape[0], slot.shape[0]
+    d = B.heisd_plan_desc(b, block_size, block_table.shape[1], n_blocks, rows)
+    for name, t, shape in (("cached_len", cached_len, (b,)), ("new_len", new_len, (b,)), ("owned_in", owned_in, (b,)),
+                           ("owned_out", owned_out, (b,)), ("block_table", block_table, (b, block_table.shape[1])),
+                           ("free_ids", free_ids, (n_blocks,)), ("free_count_in", free_count_in, (1,)),
+                           ("free_count_out", free_count_out, (1,)), ("cu_rows", cu_rows, (b + 1,)), ("seq_len", seq_len, (b,)),
+                           ("slot", slot, (rows,)), ("position", position, (rows,))):
+        setattr(d, name, _ints(t, shape, name))
+    if cu_seq is not None:
+        d.cu_seq = _ints(cu_seq, (b + 1,), "cu_seq")
+    return d
+
+
+def make_rope_desc(rotary_dim, base=10000.0, scaling="none", factor=1.0, original_len=0, beta_fast=32.0, beta_slow=1.0, low_freq=1.0,
+                   high_freq=4.0) -> B.heisd_rope_desc:
+    return B.heisd_rope_desc(rotary_dim, B.ROPE_SCALING[scaling], original_len, base, factor, beta_fast, beta_slow, low_freq, high_freq)
+
+
+def rope_table(desc: B.heisd_rope_desc, device):
+    """(turns per position of every pair, fp64 on the device, and the magnitude): once per model."""
+    rc, turns, magnitude = B.heisd_rope_table(desc)
+    if rc != 0:
+        raise ValueError("heisd_rope_table failed (%d): %s" % (rc, B.heisd_last_error(None)))
+    return torch.tensor(turns, dtype=torch.float64, device=device), magnitude
+
+
+def make_kv4_desc(pool: torch.Tensor, block_size, kv_heads, head_dim) -> B.heisd_kv4_desc:
+    """pool: contiguous uint8 whose size is that of a whole number of blocks; it must stay alive as long as the descriptor is used."""
+    cell = block_size * (head_dim + head_dim // 16) * kv_heads
+    if pool.dtype != torch.uint8 or not pool.is_contiguous() or cell <= 0 or pool.numel() % cell:
+        raise ValueError("pool: expected contiguous uint8 of a multiple of %d bytes" % cell)
+    return B.heisd_kv4_desc(pool.data_ptr(), pool.numel() // cell, block_size, kv_heads, head_dim)
+
+
+def make_paged_batch(block_table, seq_len, cu_rows, rows) -> B.heisd_paged_batch:
+    b, most = block_table.shape
+    return B.heisd_paged_batch(_ints(block_table, (b, most), "block_table"), _ints(seq_len, (b,), "seq_len"),
+                               _ints(cu_rows, (b + 1,), "cu_rows") if cu_rows is not None else None, b, most, rows)
