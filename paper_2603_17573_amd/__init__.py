@@ -20,7 +20,7 @@ from .binding import (heisd_model_desc, heisd_kv_desc, heisd_accept_desc, heisd_
                       HEISD_PATH_PERSIST, HEISD_PATH_BATCH,
                       make_accept_desc, make_model_desc, HEISD_OK, HEISD_EINVAL, HEISD_EUNSUPPORTED,
                       HEISD_ENOMEM, HEISD_EHIP)
-from .runner import (DeviceModel, Verifier, build_sequence_tree, head_rows, make_plan_desc, make_rope_desc, rope_table,
+from .runner import (DeviceModel, Verifier, PagedCache, build_sequence_tree, head_rows, make_plan_desc, make_rope_desc, rope_table,
                      make_kv4_desc, make_paged_batch)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

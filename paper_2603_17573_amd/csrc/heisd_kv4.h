@@ -24,7 +24,8 @@
 
 namespace heisd {
 
-constexpr int kKv4Group = 32, kKv4Tile = 16;
+constexpr int kKv4Tile = 16;
+constexpr uint32_t kKv4NotFinite = 253;             // from this exponent on a value may be 2^128 or more, which bf16 does not hold
 
 struct Kv4Cache {
   uint8_t *pool;
@@ -335,12 +336,11 @@ __global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, Head
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
             if (gone || t >= seen[ct]) x[ct][e] = -INFINITY;
-          // an exponent of 255 would make the products of tokens that nobody may see NaN (0 * NaN)
+          // a probability of zero times a value that is not finite would be NaN: such values leave the product
           const uint32_t mask = 0xFFu << (8 * (e & 3));
-          if ((ve[e >> 2] & mask) == mask) {
-            ve[e >> 2] &= ~mask;
-            odd = odd || !gone;
-          }
+          const bool large = ((ve[e >> 2] >> (8 * (e & 3))) & 0xFFu) >= kKv4NotFinite;
+          odd = odd || (large && !gone);
+          if (large || gone) ve[e >> 2] &= ~mask;
         }
         if (__ballot(odd)) {                        // and what is NaN makes NaN of the columns that do see it
           for (int t = base; t < min(base + 32, seq); ++t) {
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, Head
             const int o = t & (bs - 1);
             const uint8_t e = c.at(id, head)[Kv4Offsets<HD>::v_exp(bs) + ((o / 4) * (HD / 32) + quad * (HD / 4) / 32) * 4 + o % 4];
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) nan_out[ct] = nan_out[ct] || (e == 255 && t < seen[ct]);
+            for (int ct = 0; ct < CT; ++ct) nan_out[ct] = nan_out[ct] || (e >= kKv4NotFinite && t < seen[ct]);
           }
         }
       }

@@ -221,3 +221,106 @@ def make_paged_batch(block_table, seq_len, cu_rows, rows) -> B.heisd_paged_batch
     b, most = block_table.shape
     return B.heisd_paged_batch(_ints(block_table, (b, most), "block_table"), _ints(seq_len, (b,), "seq_len"),
                                _ints(cu_rows, (b + 1,), "cu_rows") if cu_rows is not None else None, b, most, rows)
+
+
+class PagedCache:
+    """The caches of every layer of a batch of requests, held in 4 bits in one pool of blocks per layer, and the calls of a step in
+    the order a decoder makes them: begin() once, then for every layer rotate(), append() and one of attend() (single
+    tokens and drafts), prompt() (whole prompts into empty caches) or chunk() (chunks behind cached rows).
+
+    max_batch requests of at most max_len tokens; a step has at most max_rows packed rows.  Everything the calls need is allocated
+    here, so a step can be captured into a HIP graph (chunk() too, once its buffers have been made by a first call)."""
+
+    def __init__(self, n_layers, q_heads, kv_heads, head_dim, max_batch, max_len, max_rows, n_blocks, block_size=64, rope=None,
+                 layout="half", max_new=1, device="cuda:0"):
+        self.device = torch.device(device)
+        self.q_heads, self.kv_heads, self.head_dim, self.max_new, self.max_len = q_heads, kv_heads, head_dim, max_new, max_len
+        self.block_size, self.n_blocks = block_size, n_blocks
+        nbytes = B.heisd_kv4_pool_bytes(n_blocks, block_size, kv_heads, head_dim)
+        if nbytes == 0:
+            raise ValueError("invalid cache: %d blocks of %d tokens, %d heads of %d" % (n_blocks, block_size, kv_heads, head_dim))
+        i32 = dict(dtype=torch.int32, device=self.device)
+        with torch.cuda.device(self.device):
+            self.pools = torch.empty((n_layers, nbytes), dtype=torch.uint8, device=self.device)
+            self.table = torch.full((max_batch, -(-max_len // block_size)), -1, **i32)
+            self.owned = torch.zeros(max_batch, **i32)
+            self.free_ids = torch.arange(n_blocks, **i32)
+            self.free_count = torch.full((1,), n_blocks, **i32)
+            self.seq_len = torch.full((max_batch,), -1, **i32)
+            self.cu_rows, self.cu_seq = torch.zeros(max_batch + 1, **i32), torch.zeros(max_batch + 1, **i32)
+            self.slot, self.position = torch.full((max_rows,), -1, **i32), torch.full((max_rows,), -1, **i32)
+            self.descs = [make_kv4_desc(p, block_size, kv_heads, head_dim) for p in self.pools]
+            n = B.heisd_kv4_attention_workspace_bytes(self.descs[0], max_batch, max_rows, q_heads, max_new, max_len)
+            if n == 0:
+                raise ValueError("invalid attention: %d query heads, %d rows, max_new %d, max_len %d" % (q_heads, max_rows, max_new, max_len))
+            self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+            desc = rope if rope is not None else make_rope_desc(head_dim)
+            self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]
+            self.turns, self.magnitude = rope_table(desc, self.device)
+        self.rows = 0
+
+    def _call(self, fn, *args):
+        with torch.cuda.device(self.device):
+            rc = fn(*args, torch.cuda.current_stream(self.device).cuda_stream)
+        if rc != 0:
+            raise RuntimeError("%s failed (%d): %s" % (fn.__name__, rc, B.heisd_last_error(None)))
+
+    def _of_step(self, t, heads, what):
+        if tuple(t.shape) != (self.rows, heads, self.head_dim) or t.device != self.device:
+            raise ValueError("%s: expected [%d, %d, %d] on %s, got %s on %s" % (what, self.rows, heads, self.head_dim, self.device,
+                                                                              tuple(t.shape), t.device))
+        return head_rows(t)
+
+    def begin(self, cached_len, new_len, rows):
+        """cached_len, new_len i32[max_batch] on the device (a negative cached_len: the request is finished and gives its blocks back);
+        rows: packed rows of this step, at least the sum of new_len.  A request that does not fit has seq_len -1 afterwards."""
+        if not 0 <= rows <= self.slot.shape[0]:
+            raise ValueError("rows=%d, made for at most %d" % (rows, self.slot.shape[0]))
+        self.rows = rows
+        self._call(B.heisd_paged_plan, make_plan_desc(self.block_size, self.n_blocks, cached_len, new_len, self.owned, self.owned, self.table,
+                                                      self.free_ids, self.free_count, self.free_count, self.seq_len, self.cu_rows,
+                                                      self.slot[:rows], self.position[:rows], self.cu_seq))
+        self.batch = make_paged_batch(self.table, self.seq_len, self.cu_rows, rows)
+
+    def rotate(self, q, k):
+        """q and k of this step's rows, in place."""
+        hq, hk = self._of_step(q, self.q_heads, "q"), self._of_step(k, self.kv_heads, "k")
+        self._call(B.heisd_rope, self.turns.data_ptr(), self.magnitude, self.rotary_dim, self.layout, 0, self.position.data_ptr(), self.rows,
+                   self.head_dim, hq, hq, hk, hk)
+
+    def append(self, layer, k, v):
+        self._call(B.heisd_kv4_append, self.descs[layer], self._of_step(k, self.kv_heads, "k"), self._of_step(v, self.kv_heads, "v"),
+                   self.slot.data_ptr(), self.rows)
+
+    def attend(self, layer, q, scale=None, out=None, lse=None):
+        """Attention of this step's rows over everything their requests have cached, the rows themselves included."""
+        out = torch.empty_like(q) if out is None else out
+        hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
+        self._call(B.heisd_kv4_attention, self.descs[layer], self.batch, hq, ho, lse.data_ptr() if lse is not None else None,
+                   self.head_dim ** -0.5 if scale is None else scale, self.max_new, self.max_len, self.workspace.data_ptr(),
+                   self.workspace.numel())
+        return out
+
+    def prompt(self, q, k, v, scale=None, out=None, lse=None):
+        """Causal attention of whole prompts over their own rows (nothing cached before them), as they are and not as they are held."""
+        out = torch.empty_like(q) if out is None else out
+        hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
+        hk, hv = self._of_step(k, self.kv_heads, "k"), self._of_step(v, self.kv_heads, "v")
+        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, lse.data_ptr() if lse is not None else None, self.cu_rows.data_ptr(),
+                   self.cu_rows.data_ptr(), self.table.shape[0], self.rows, self.rows, self.head_dim,
+                   self.head_dim ** -0.5 if scale is None else scale, 1)
+        return out
+
+    def chunk(self, layer, q, total, scale=None, out=None, lse=None):
+        """Causal attention of many rows per request over everything cached (total: at least the sum of the requests' lengths): the
+        cached rows are read back once and multiplied as a prompt's."""
+        out = torch.empty_like(q) if out is None else out
+        hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
+        if getattr(self, "_kv", None) is None or self._kv.shape[1] < total or self._kv.dtype != q.dtype:
+            self._kv = torch.empty((2, total, self.kv_heads, self.head_dim), dtype=q.dtype, device=self.device)
+        hk, hv = head_rows(self._kv[0]), head_rows(self._kv[1])
+        self._call(B.heisd_kv4_gather, self.descs[layer], self.batch, self.cu_seq.data_ptr(), total, hk, hv)
+        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, lse.data_ptr() if lse is not None else None, self.cu_rows.data_ptr(),
+                   self.cu_seq.data_ptr(), self.table.shape[0], self.rows, total, self.head_dim,
+                   self.head_dim ** -0.5 if scale is None else scale, 1)
+        return out
