@@ -500,7 +500,7 @@ int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *ba
  *   q, k, v, out  bf16 or fp16 (all the same); q, k, v 16-byte aligned in pointer and strides, out 8
  *   lse           DEVICE f32 [rows][q heads] out, optional     rows, k_rows  rows in q and out, in k and v
  * head_dim 64 or 128.  Scores, sums and the softmax are fp32, probabilities enter the second product in the rows' dtype.
- * Errors: EINVAL, EUNSUPPORTED (head_dim, fp32), EHIP.
+ * Errors: EINVAL, EUNSUPPORTED (head_dim, fp32, rows of k or v more than 2^25 elements apart), EHIP.
  */
 int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out, float *lse,
                            const int32_t *cu_q, const int32_t *cu_k, int32_t batch, int32_t rows, int32_t k_rows, int32_t head_dim, float scale,

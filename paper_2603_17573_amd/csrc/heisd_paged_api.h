@@ -383,10 +383,14 @@ extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head
     return fail(nullptr, HEISD_EINVAL, "%s: q, k, v (16 bytes) or out (8 bytes) misaligned", who);
   if (!cu_q || !cu_k || batch < 1 || batch > 65535 || rows < 0 || k_rows < 0 || !std::isfinite(scale))
     return fail(nullptr, HEISD_EINVAL, "%s: NULL lengths, batch=%d (1..65535) rows=%d k_rows=%d scale=%g", who, batch, rows, k_rows, scale);
+  if (k->row_stride > (1 << 25) || v->row_stride > (1 << 25))                       // 16 rows apart stays below 2^32 bytes
+    return fail(nullptr, HEISD_EUNSUPPORTED, "%s: rows of k or v more than 2^25 elements apart", who);
   const int64_t tiles = (int64_t)rows / kPromptRows + batch;
   if (tiles * q->heads > 0x7FFFFFFF) return fail(nullptr, HEISD_EINVAL, "%s: rows=%d too many", who, rows);
   if (rows == 0) return HEISD_OK;
-  const PromptArgs a{cu_q, cu_k, batch, rows, k_rows, q->heads, k->heads, q->heads / k->heads, (int)tiles, scale * 1.4426950408889634f, lse};
+  const PromptArgs a{cu_q, cu_k, batch, rows, k_rows, q->heads, k->heads, q->heads / k->heads, (int)tiles,
+                     std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f),   // not 0: minus infinity stands for masked scores
+                     scale < 0 ? 0x80008000u : 0u, lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (q->dtype == HEISD_DTYPE_BF16) {

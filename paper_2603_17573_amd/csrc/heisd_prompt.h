@@ -39,7 +39,8 @@ struct PromptArgs {
   const int32_t *cu_q, *cu_k;
   int batch, rows, k_rows, q_heads, kv_heads, group;
   int tiles;                                        // row tiles in the grid
-  float scale_log2;                                 // softmax scale times log2(e)
+  float scale_log2;                                 // magnitude of the softmax scale times log2(e)
+  uint32_t flip;                                    // 0x80008000 where the scale is negative
   float *lse;
 };
 
@@ -58,7 +59,7 @@ __device__ __forceinline__ void prompt_rows_plain(HeadRows<const T> q, HeadRows<
       load_vec<T, V>(k.at(k_row0 + t, kvh) + lane * V, y);
       float s = 0.f;
       for (int n = 0; n < V; ++n) s += x[n] * y[n];
-      s = wave_sum(s) * a.scale_log2;
+      s = wave_sum(s) * (a.flip ? -a.scale_log2 : a.scale_log2);
       load_vec<T, V>(v.at(k_row0 + t, kvh) + lane * V, y);
       const float next = fmaxf(m, s), use = next == -INFINITY ? 0.f : next;
       const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - use), p = __builtin_amdgcn_exp2f(s - use);
@@ -106,26 +107,41 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
   {
     const T *p = q.at(rows.begin + my_row, head) + half * 8;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const x8 *>(p + s * 16);
+    for (int s = 0; s < NS; ++s) {
+      u32x4 w = *reinterpret_cast<const u32x4 *>(p + s * 16);
+      w ^= a.flip;                                  // a negative scale: the queries' signs, so that larger products are larger scores
+      qf[s] = __builtin_bit_cast(x8, w);
+    }
   }
   f32x16 acc[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l[4] = {};                   // the row's maximum so far (powers of two), parts of its sum
   uint32_t odd = 0;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
   constexpr int RP = 1024 / RB, NP = kPromptKeys / RP / kPromptWaves;              // rows per transfer, transfers per wave and matrix
+  constexpr int STEP = RP * kPromptWaves;                                          // rows from one transfer of a wave to its next
+  const int lane_row = wave * RP + lane / CH, lane_chunk = (lane % CH) ^ (lane_row % CH);   // STEP is a multiple of CH
+  const uint32_t k_off = (uint32_t)(lane_row * k.rs + lane_chunk * 8) * sizeof(T), v_off = (uint32_t)(lane_row * v.rs + lane_chunk * 8) * sizeof(T);
   auto stage = [&](int block, int buf) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + wave * 1024);
+    const long long row0 = keys.begin + block * kPromptKeys;
+    if ((block + 1) * kPromptKeys <= n_keys) {
 #pragma unroll
-    for (int n = 0; n < NP; ++n) {
-      const int piece = n * kPromptWaves + wave;
-      const int row = piece * RP + lane / CH, chunk = (lane % CH) ^ (row % CH);
-      const int key = keys.begin + min(block * kPromptKeys + row, n_keys - 1);     // past the end: the last one again, masked
-      lds_dma16(k.at(key, kvh) + chunk * 8, __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + piece * 1024));
-      lds_dma16(v.at(key, kvh) + chunk * 8, __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + TILE + piece * 1024));
+      for (int n = 0; n < NP; ++n) {
+        lds_dma16_s(k.at(row0 + n * STEP, kvh), k_off, to + n * kPromptWaves * 1024);
+        lds_dma16_s(v.at(row0 + n * STEP, kvh), v_off, to + TILE + n * kPromptWaves * 1024);
+      }
+    } else {                                        // past the end: the last row again, masked
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const long long row = keys.begin + min(block * kPromptKeys + n * STEP + lane_row, n_keys - 1);
+        lds_dma16(k.at(row, kvh) + lane_chunk * 8, to + n * kPromptWaves * 1024);
+        lds_dma16(v.at(row, kvh) + lane_chunk * 8, to + TILE + n * kPromptWaves * 1024);
+      }
     }
   };
   // byte offsets of the lane's reads; rows further on are constants away
@@ -159,30 +175,30 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
       for (int n = 0; n < NS; ++n)
         s[t] = MatrixOf<T>::mul(*reinterpret_cast<const x8 *>(kt + k_at[n] + t * 32 * RB), qf[n], s[t]);
     }
-    const bool masked = base + kPromptKeys > all_see;
-    float top = -INFINITY;
+    if (base + kPromptKeys > all_see) {             // some row must not see some of these keys
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float x = s[t][e] * a.scale_log2;
-        if (masked && base + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) x = -INFINITY;
-        s[t][e] = x;
-        top = fmaxf(top, x);
-      }
-    if (masked) {
+        for (int e = 0; e < 16; ++e)
+          if (base + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) s[t][e] = -INFINITY;
 #pragma unroll 4
       for (int i = 0; i < TILE / 1024; ++i) {
         const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + i * 1024 + lane * 16);
         odd |= not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
       }
     }
-    top = max_xor32(top);
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+    top = max_xor32(top) * a.scale_log2;
     if (__ballot(top > m + kPromptLazy)) {
       const float next = fmaxf(m, top);
       const float by = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
       m = next;
-      l *= by;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l[i] *= by;
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[d] *= by;
     }
@@ -192,8 +208,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float p = __builtin_amdgcn_exp2f(s[t][e] - use);
-        l += p;
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], a.scale_log2, -use));
+        l[e & 3] += p;
         pf[2 * t + (e >> 3)][e & 7] = (T)p;
       }
 #pragma unroll
@@ -213,9 +229,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
     prompt_rows_plain<T, HD, CAUSAL>(q, k, v, out, a, rows.begin + mine, my_rows, head, keys.begin, keys.count, shift + mine);
     return;
   }
-  l = sum_xor32(l);
+  const float sum = sum_xor32((l[0] + l[1]) + (l[2] + l[3]));
   if (col >= my_rows) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const long long r = rows.begin + mine + col;
   T *o = out.at(r, head);
 #pragma unroll
@@ -227,7 +243,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
       for (int i = 0; i < 4; ++i) f[i] = acc[d][4 * e + i] * inv;
       store_vec<T, 4>(o + d * 32 + e * 8 + half * 4, f);
     }
-  if (a.lse && half == 0) a.lse[r * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && half == 0) a.lse[r * a.q_heads + head] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace heisd

@@ -673,6 +673,19 @@ def test_prompt_attention_not_finite_where_masked(P, dtype, head_dim):
     assert np.isfinite(host(out)[:100]).all() and np.isfinite(host(out)[150:189]).all()
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-42])
+def test_attention_with_other_scales(P, scale):
+    """Zero (a mean over what is seen), negative and subnormal scales."""
+    rng = np.random.default_rng(8)
+    q, k, v = (randn(rng, (90, h, 64), "bf16") for h in (2, 1, 1))
+    out, lse = prompt(P, q, k, v, [0, 90], [0, 90], scale, True)
+    check_prompt(q, k, v, out, lse, [0, 90], [0, 90], scale, True, "bf16")
+    c = Cache(P, rng, [90], 1, 64, 16)
+    c.write(P, k, v)
+    out, lse = attend(P, c, q[:3], [0, 3], 3, 90, scale)
+    check_attend(c, q[:3], out, lse, [0, 3], ref.held(host(k)), ref.held(host(v)), scale, "bf16")
+
+
 def test_prompt_attention_layouts(P):
     rng = np.random.default_rng(5)
     q, k, v = randn(rng, (140, 4, 64), "f16"), randn(rng, (140, 2, 64), "f16"), randn(rng, (140, 2, 64), "f16")
