@@ -35,6 +35,14 @@ constexpr float kPromptLazy = 8.f;                  // the maximum is moved only
 template <int HD>
 constexpr int prompt_lds_bytes() { return 2 * 2 * kPromptKeys * HD * 2; }
 
+// Where the 16-byte pieces of an LDS row go: piece c of row r lies at c ^ prompt_swizzle(r).  A read of K takes the same piece of 16
+// rows at a time, a transposed read of V 64 bytes of four rows: both must meet all 64 banks once.  A row of 256 bytes is all banks, of
+// 128 bytes half of them; the two lowest bits of r that leave the banks as they are move the 64-byte piece.
+template <int CH>
+__device__ __forceinline__ int prompt_swizzle(int r) {
+  return CH == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
+}
+
 struct PromptArgs {
   const int32_t *cu_q, *cu_k;
   int batch, rows, k_rows, q_heads, kv_heads, group;
@@ -124,7 +132,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
   constexpr int RP = 1024 / RB, NP = kPromptKeys / RP / kPromptWaves;              // rows per transfer, transfers per wave and matrix
   constexpr int STEP = RP * kPromptWaves;                                          // rows from one transfer of a wave to its next
-  const int lane_row = wave * RP + lane / CH, lane_chunk = (lane % CH) ^ (lane_row % CH);   // STEP is a multiple of CH
+  const int lane_row = wave * RP + lane / CH, lane_chunk = (lane % CH) ^ prompt_swizzle<CH>(lane_row);   // STEP is a multiple of 16
   const uint32_t k_off = (uint32_t)(lane_row * k.rs + lane_chunk * 8) * sizeof(T), v_off = (uint32_t)(lane_row * v.rs + lane_chunk * 8) * sizeof(T);
   auto stage = [&](int block, int buf) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + wave * 1024);
@@ -147,13 +155,13 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
   // byte offsets of the lane's reads; rows further on are constants away
   uint32_t k_at[NS], v_at[ND][2];
 #pragma unroll
-  for (int s = 0; s < NS; ++s) k_at[s] = col * RB + (((2 * s + half) ^ (col % CH)) << 4);
+  for (int s = 0; s < NS; ++s) k_at[s] = col * RB + (((2 * s + half) ^ prompt_swizzle<CH>(col)) << 4);
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int row = 8 * e + 4 * half + ((lane & 15) >> 2), chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-      v_at[d][e] = row * RB + ((chunk ^ (row % CH)) << 4) + (lane & 1) * 8;
+      v_at[d][e] = row * RB + ((chunk ^ prompt_swizzle<CH>(row)) << 4) + (lane & 1) * 8;
     }
 
   const int n_blocks = (n_keys + kPromptKeys - 1) / kPromptKeys;
