@@ -200,61 +200,146 @@ struct Kv4Pair {
 
 struct Kv4Attend {
   float scale_log2;                                 // softmax scale times log2(e)
-  int group, q_heads, chunk, n_chunks, max_seq;
-  float *part, *lse;                                // part: [row][query head][chunk][HD + 2] sums of chunks
+  int group, q_heads, max_seq, cols;                // cols: columns a workgroup takes (16 or 32)
+  long long *starts;                                // [batch + 1] units of work before each request
+  float *part, *part_ml;                            // sums of unfinished segments [2 * workgroups][cols][HD], their maxima and sums [..][cols][2]
+  float *lse;
 };
+
+// Work is counted in units: 128 tokens (a pair of tiles for each wave) of one request, key head and group of columns - a segment is all
+// units of such a three.  Every workgroup takes an equal run of the units of the whole call, whatever the requests' lengths are.
+constexpr int kKv4Unit = 128;
+
+// Workgroups of 256 threads that the registers of a compute unit hold: queries of two terms or two column tiles need more of them.
+__host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles, int terms) { return col_tiles == 1 && (terms == 1 || head_dim == 64) ? 3 : 2; }
+
+// What a request asks for: its rows, its tokens, units per segment, segments.
+struct Kv4Request {
+  Span rows;
+  int seq, units, segments;
+  __device__ __forceinline__ long long work() const { return (long long)units * segments; }
+};
+__device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const PagedBatch &b, const Kv4Attend &a, int i) {
+  Kv4Request r;
+  r.rows = packed_span(b.cu_rows, i, b.rows);
+  r.seq = b.seq_len[i];
+  if (r.seq < 0 || r.seq > a.max_seq || (long long)r.seq > (long long)b.max_blocks * c.block_size) r.seq = 0;
+  r.units = max((r.seq + kKv4Unit - 1) / kKv4Unit, 1);          // one even without tokens: somebody writes the zeros
+  r.segments = (r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads;
+  return r;
+}
+
+// Sum over the workgroup and, for each thread, over those before it (exclusive).
+__device__ __forceinline__ long long kv4_scan(long long v, long long &total, long long *wave_sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long long x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long t = __shfl_up(x, o);
+    if (lane >= o) x += t;
+  }
+  if (lane == 63) wave_sums[wave] = x;
+  __syncthreads();
+  long long before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += wave_sums[w];
+    total += wave_sums[w];
+  }
+  __syncthreads();
+  return before + x - v;
+}
 
 // Online softmax state of a column (one query row of one head): maximum and sum in powers of two.
 constexpr float kKv4Lazy = 8.f;                     // the maximum is moved only when it grew by more than this (powers of two)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// softmax(q K^T) V over the tokens of one chunk of one request and one key head.  The query rows of the heads that share the key head
-// are the columns of the matrix products (CT tiles of 16): scores^T = K q^T (tokens are rows), out^T = V^T p^T.  A lane holds the
-// scores of one column and four tokens of each tile, which are its summed indices of the second product, so the probabilities
-// never leave their lane.  Four waves take pairs of tiles in turn, each with a running maximum and sum of its own, joined
-// through LDS at the end; chunks are joined by kv4_join.  TERMS 2: queries and probabilities enter as a bf16 and a bf16
-// remainder (fp16 rows, whose 11 bits a bf16 does not hold); 1: as one bf16, rounding the probabilities by 2^-9.
+// softmax(q K^T) V over the tokens of segments.  The query rows of the heads that share the key head are the columns of the matrix products (CT tiles of
+// 16): scores^T = K q^T (tokens are rows), out^T = V^T p^T.  A lane holds the scores of one column and four tokens of each tile, which are
+// its summed indices of the second product, so the probabilities never leave their lane.  Four waves take pairs of tiles in turn,
+// each with a running maximum and sum of its own, joined through LDS at the end of a segment; what a workgroup has of a segment that it
+// shares with others goes to kv4_join.  TERMS 2: queries and probabilities enter as a bf16 and a bf16 remainder (fp16 rows, whose
+// 11 bits a bf16 does not hold); 1: as one bf16, rounding the probabilities by 2^-9.
 template <typename T, int HD, int CT, int TERMS>
-__global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
+__global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
   constexpr int W = HD / 32, ND = HD / 16, KJ = HD / 32;        // code dwords, tiles of channels, products per score tile
   constexpr int LD = HD + 4;
   __shared__ __attribute__((aligned(16))) float s_out[4][16 * LD];
   __shared__ float s_m[4][16], s_l[4][16];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-  const int head = blockIdx.x % c.kv_heads, req = blockIdx.z, chunk = blockIdx.y;
-  const Span rows = packed_span(b.cu_rows, req, b.rows);
-  int seq = b.seq_len[req];
-  if (seq > a.max_seq || (long long)seq > (long long)b.max_blocks * c.block_size) seq = 0;
-  seq = max(seq, 0);
-  const int t0 = chunk * a.chunk, t1 = min(seq, t0 + a.chunk);
-  if (rows.count == 0 || (chunk > 0 && t0 >= seq)) return;
-  const int n_cols = rows.count * a.group;
+  __shared__ long long s_sum[4], s_start[256];                  // units before each of the 256 requests at hand
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int bs = c.block_size;
-  const bool whole = seq <= a.chunk;
 
-  for (int col0 = blockIdx.x / c.kv_heads * (16 * CT); col0 < n_cols; col0 += gridDim.x / c.kv_heads * (16 * CT)) {
+  // this workgroup's run of units
+  long long all = 0, chunk_work = 0, mine = 0;
+  int first = 0;                                                // the requests at hand: first .. first + 255
+  for (int i = 0; i < b.batch; i += 256) {
+    const int r = i + threadIdx.x;
+    const long long w = r < b.batch ? kv4_request(c, b, a, r).work() : 0;
+    const long long before = all + kv4_scan(w, chunk_work, s_sum);
+    if (i == 0) mine = before;
+    if (blockIdx.x == 0 && r < b.batch) a.starts[r] = before;   // for kv4_join
+    all += chunk_work;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.starts[b.batch] = all;
+  const long long groups = min((long long)gridDim.x, all);       // no run is empty
+  if (blockIdx.x >= groups) return;
+  long long at = all * blockIdx.x / groups;
+  const long long run0 = at, run1 = all * (blockIdx.x + 1) / groups;
+  long long end = 0;                                            // units before the end of the requests at hand
+  {
+    long long carry = 0;
+    for (;; first += 256) {
+      const int r = first + threadIdx.x;
+      if (first > 0) mine = carry + kv4_scan(r < b.batch ? kv4_request(c, b, a, r).work() : 0, chunk_work, s_sum);
+      else if (b.batch > 256) kv4_scan(r < b.batch ? kv4_request(c, b, a, r).work() : 0, chunk_work, s_sum);
+      end = carry + chunk_work;
+      if (at < end) break;
+      carry = end;
+    }
+  }
+  s_start[threadIdx.x] = mine;
+  __syncthreads();
+
+  while (at < run1) {
+    if (at >= end) {                                            // on to the next requests
+      long long work;
+      do {
+        first += 256;
+        const int r = first + threadIdx.x;
+        const long long x = end + kv4_scan(r < b.batch ? kv4_request(c, b, a, r).work() : 0, work, s_sum);
+        s_start[threadIdx.x] = x;
+        end += work;
+      } while (at >= end);
+      __syncthreads();
+    }
+    const int local = wave_search(min(256, b.batch - first), at, [&](int i) { return s_start[i]; });
+    const int req = first + local;
+    const long long at_req = s_start[local];
+    Kv4Request rq = kv4_request(c, b, a, req);
+    const Span rows{__builtin_amdgcn_readfirstlane(rq.rows.begin), __builtin_amdgcn_readfirstlane(rq.rows.count)};
+    const int seq = __builtin_amdgcn_readfirstlane(rq.seq), units = __builtin_amdgcn_readfirstlane(rq.units);
+    const int segment = __builtin_amdgcn_readfirstlane((int)((at - at_req) / units));
+    const int u0 = __builtin_amdgcn_readfirstlane((int)(at - at_req - (long long)segment * units));
+    const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
+    const int head = segment % c.kv_heads, col0 = segment / c.kv_heads * (16 * CT);
+    const bool whole = u0 == 0 && u1 == units;
+    const long long slot = 2 * (long long)blockIdx.x + (at != run0);
+    const int n_cols = rows.count * a.group;
+    const int t1 = min(seq, u1 * kKv4Unit);
+
     // the columns' queries and how many tokens each may see
-    bf16x8 qf[CT][KJ][TERMS];
+    typename VecOf<T, 8>::type qr[CT][KJ];
     int seen[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      const int n = col0 + ct * 16 + col, i = n / a.group;
-      const bool there = n < n_cols;
-      seen[ct] = there ? seq - rows.count + i + 1 : 0;
-      const T *p = there ? q.at(rows.begin + i, head * a.group + (n - i * a.group)) + quad * (HD / 4) : nullptr;
+      const int n = min(col0 + ct * 16 + col, n_cols - 1), i = n / a.group;       // columns past the end: the last again, not stored
+      seen[ct] = seq - rows.count + i + 1;
+      const T *p = q.at(rows.begin + i, head * a.group + (n - i * a.group)) + quad * (HD / 4);
 #pragma unroll
-      for (int j = 0; j < KJ; ++j) {
-        float f[8];
-        if (there) load_vec<T, 8>(p + j * 8, f);
-        else
-          for (int e = 0; e < 8; ++e) f[e] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          qf[ct][j][0][e] = (__bf16)f[e];
-          if constexpr (TERMS == 2) qf[ct][j][1][e] = (__bf16)(f[e] - (float)qf[ct][j][0][e]);
-        }
-      }
+      for (int j = 0; j < KJ; ++j) qr[ct][j] = *reinterpret_cast<const typename VecOf<T, 8>::type *>(p + j * 8);
     }
     f32x4 acc[CT][ND];
     float m[CT], l[CT];
@@ -267,14 +352,7 @@ __global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, Head
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[ct][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // the blocks of the wave's tiles: lane 2 i + n holds that of tile n of its i-th pair (32 pairs: a chunk has at most 4096 tokens)
-    const int n_pairs = max((t1 - t0 + 127 - 32 * wave) >> 7, 0);
-    int my_id = -1;
-    {
-      const int t = t0 + 32 * (wave + 4 * (lane >> 1)) + 16 * (lane & 1);
-      if (t < t1) my_id = b.table[(long long)req * b.max_blocks + (t >> c.block_shift)];
-      if (my_id >= c.n_blocks) my_id = -1;
-    }
+    int t0 = 0, my_id = -1;                                     // tokens t0 .. t0 + 4095 are at hand
     auto load_pair = [&](Kv4Pair<HD> &p, int i) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -297,6 +375,18 @@ __global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, Head
                                                       (quad * (HD / 32) + col * (HD / 16) / 32) * 4);
       }
     };
+    Kv4Pair<HD> now, next;
+    bf16x8 qf[CT][KJ][TERMS];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int j = 0; j < KJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float f = (float)qr[ct][j][e];
+          qf[ct][j][0][e] = (__bf16)f;
+          if constexpr (TERMS == 2) qf[ct][j][1][e] = (__bf16)(f - (float)qf[ct][j][0][e]);
+        }
     auto use_pair = [&](const Kv4Pair<HD> &p, int i) {
       const int base = t0 + 32 * (wave + 4 * i);
       f32x4 s[CT][2];
@@ -421,14 +511,20 @@ __global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, Head
         channels(std::integral_constant<int, 3>{});
       }
     };
-    Kv4Pair<HD> now, next;
-    if (n_pairs > 0) load_pair(now, 0);
-    for (int i = 0; i < n_pairs; i += 2) {
-      if (i + 1 < n_pairs) load_pair(next, i + 1);
-      use_pair(now, i);
-      if (i + 1 >= n_pairs) break;
-      if (i + 2 < n_pairs) load_pair(now, i + 2);
-      use_pair(next, i + 1);
+    for (t0 = u0 * kKv4Unit; t0 < t1; t0 += 32 * kKv4Unit) {
+      // the blocks of the wave's tiles: lane 2 i + n holds that of tile n of its i-th pair of these 32
+      const int t = t0 + 32 * (wave + 4 * (lane >> 1)) + 16 * (lane & 1);
+      my_id = t < t1 ? b.table[(long long)req * b.max_blocks + (t >> c.block_shift)] : -1;
+      if (my_id >= c.n_blocks) my_id = -1;
+      const int n_pairs = max((min(t1 - t0, 32 * kKv4Unit) + 127 - 32 * wave) >> 7, 0);
+      if (n_pairs > 0) load_pair(now, 0);
+      for (int i = 0; i < n_pairs; i += 2) {
+        if (i + 1 < n_pairs) load_pair(next, i + 1);
+        use_pair(now, i);
+        if (i + 1 >= n_pairs) break;
+        if (i + 2 < n_pairs) load_pair(now, i + 2);
+        use_pair(next, i + 1);
+      }
     }
     // join the waves, a tile of columns at a time
 #pragma unroll
@@ -465,54 +561,55 @@ __global__ __launch_bounds__(256) void kv4_attend(Kv4Cache c, PagedBatch b, Head
           store_vec<T, 4>(out.at(r, h) + d, f);
           if (a.lse && d == 0) a.lse[r * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
         } else {
-          float *p = a.part + ((r * a.q_heads + h) * a.n_chunks + chunk) * (HD + 2);
-          *reinterpret_cast<float2 *>(p + d) = make_float2(o[0], o[1]);
-          *reinterpret_cast<float2 *>(p + d + 2) = make_float2(o[2], o[3]);
-          if (d == 0) {
-            p[HD] = top;
-            p[HD + 1] = sum;
-          }
+          const long long at_col = slot * a.cols + ct * 16 + n;
+          *reinterpret_cast<f32x4 *>(a.part + at_col * HD + d) = o;
+          if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + at_col * 2) = make_float2(top, sum);
         }
       }
       __syncthreads();
     }
+    at += u1 - u0;
   }
 }
 
-// Joins the chunks of rows that have more than one: a wave per row and head.  Chunks are added in their order.
+// Joins the parts of segments that several workgroups worked on, in the order of their tokens.  A workgroup per segment; 16 bytes of
+// a column per thread.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4Attend a) {
-  constexpr int V = HD / 64;
-  const int lane = threadIdx.x & 63;
-  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const long long r = at / a.q_heads;
-  const int h = (int)(at - r * a.q_heads);
-  if (r >= b.rows) return;
-  const int req = wave_search(b.batch, r, [&](int n) { return (long long)b.cu_rows[n]; });
-  const Span rows = packed_span(b.cu_rows, req, b.rows);
-  if (r < rows.begin || r >= rows.begin + rows.count) return;
-  const int seq = b.seq_len[req];
-  if (seq > a.max_seq || (long long)seq > (long long)b.max_blocks * c.block_size || seq <= a.chunk) return;
-  const int n = (seq + a.chunk - 1) / a.chunk;
-  const float *p = a.part + at * a.n_chunks * (HD + 2);
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, p[(long long)i * (HD + 2) + HD]);
-  top = wave_max(top);
-  float sum = 0.f, o[V] = {};
-  for (int i = 0; i < n; ++i) {
-    const float *x = p + (long long)i * (HD + 2);
-    const float m = x[HD];
-    if (m == -INFINITY) continue;
-    const float by = exp2_fast(m - top);
-    sum += x[HD + 1] * by;
-#pragma unroll
-    for (int v = 0; v < V; ++v) o[v] += x[lane * V + v] * by;
+__global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4Attend a, int grid) {
+  const int req = blockIdx.y, segment = blockIdx.x;
+  const Kv4Request r = kv4_request(c, b, a, req);
+  const long long all = a.starts[b.batch], groups = min((long long)grid, all);
+  for (int seg = segment; seg < r.segments; seg += gridDim.x) {
+    const long long s0 = a.starts[req] + (long long)seg * r.units, s1 = s0 + r.units - 1;
+    const int w0 = (int)(((s0 + 1) * groups - 1) / all), w1 = (int)(((s1 + 1) * groups - 1) / all);   // who has the first, the last unit
+    if (w0 == w1) continue;
+    const int first_slot = 2 * w0 + (all * w0 / groups != s0);                     // the others begin their runs inside the segment
+    const int head = seg % c.kv_heads, col0 = seg / c.kv_heads * a.cols, n_cols = min(r.rows.count * a.group - col0, a.cols);
+    for (int u = threadIdx.x; u < n_cols * (HD / 4); u += 256) {
+      const int n = u / (HD / 4), d = u % (HD / 4) * 4;
+      auto slot = [&](int w) { return (long long)(w == w0 ? first_slot : 2 * w) * a.cols + n; };
+      float top = -INFINITY;
+#pragma unroll 4
+      for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.part_ml[slot(w) * 2]);
+      float sum = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int w = w0; w <= w1; ++w) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + slot(w) * 2);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part + slot(w) * HD + d);
+        if (ml.x != -INFINITY) {
+          const float by = exp2_fast(ml.x - top);
+          sum += ml.y * by;
+          o += x * by;
+        }
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const int i = (col0 + n) / a.group, h = head * a.group + (col0 + n - i * a.group);
+      float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+      store_vec<T, 4>(out.at(r.rows.begin + i, h) + d, f);
+      if (a.lse && d == 0) a.lse[(long long)(r.rows.begin + i) * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int v = 0; v < V; ++v) o[v] *= inv;
-  store_vec<T, V>(out.at(r, h) + lane * V, o);
-  if (a.lse && lane == 0) a.lse[r * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace heisd

@@ -50,6 +50,12 @@ __device__ __forceinline__ Span packed_span(const int32_t *cu, int i, int rows) 
   return (a < 0 || b < a || b > rows) ? Span{0, 0} : Span{a, b - a};
 }
 
+// The same for a sequence that is the whole wave's, in scalar registers.
+__device__ __forceinline__ Span wave_span(const int32_t *cu, int i, int rows) {
+  const Span s = packed_span(cu, i, rows);
+  return Span{__builtin_amdgcn_readfirstlane(s.begin), __builtin_amdgcn_readfirstlane(s.count)};
+}
+
 // ---- block tables, slots and positions ---------------------------------------------------------------------------
 
 struct PlanArgs {

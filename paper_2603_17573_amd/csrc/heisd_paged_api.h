@@ -277,17 +277,26 @@ extern "C" int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_b
   return launched(who);
 }
 
-// How a call is cut: column tiles per workgroup, groups of them, tokens per chunk.  A chunk is a workgroup's; chunks of 128 tokens (one
-// pair of tiles per wave) up to 4096, the largest that still give four workgroups per compute unit.
+// How a call is cut: column tiles per workgroup, and workgroups: as many as are resident at once (kv4_per_unit), fewer where there is
+// little to do - four units of 128 tokens for each, counted with the largest lengths.
+constexpr int kKv4Units = 256;                       // compute units that the grid is made for (a fixed number: results do not depend on the device)
 struct Kv4Plan {
-  int col_tiles, col_groups, chunk, n_chunks;
-  Kv4Plan(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq) {
+  int col_tiles, segments;
+  int64_t units;
+  size_t starts, part, part_ml, total;
+  int groups(int terms, int head_dim) const {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, kv4_per_unit(head_dim, col_tiles, terms) * kKv4Units));
+  }
+  Kv4Plan(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, int64_t head_dim) {
     const int64_t cols = max_q * group;
     col_tiles = cols > 16 ? 2 : 1;
-    col_groups = (int)std::min<int64_t>((cols + 16 * col_tiles - 1) / (16 * col_tiles), 65535);
-    chunk = 4096;
-    while (chunk > 128 && batch * kv_heads * col_groups * ((max_seq + chunk - 1) / chunk) < 1024) chunk /= 2;
-    n_chunks = (int)std::max<int64_t>(1, (max_seq + chunk - 1) / chunk);
+    segments = (int)std::min<int64_t>(kv_heads * ((cols + 16 * col_tiles - 1) / (16 * col_tiles)), 65535);
+    units = batch * segments * ((max_seq + kKv4Unit - 1) / kKv4Unit);
+    const size_t rows = (size_t)2 * groups(1, (int)head_dim) * 16 * col_tiles;       // (one term: the larger grid)
+    starts = 0;
+    part = align256((size_t)(batch + 1) * sizeof(int64_t));
+    part_ml = part + align256(rows * (size_t)head_dim * sizeof(float));
+    total = part_ml + align256(rows * 2 * sizeof(float));
   }
 };
 
@@ -304,8 +313,7 @@ extern "C" size_t heisd_kv4_attention_workspace_bytes(const heisd_kv4_desc *cach
   if (!cache || !kv4_shape_ok(cache->n_blocks, cache->block_size, cache->kv_heads, cache->head_dim) || batch < 1 || batch > 65535 ||
       kv4_attention_sizes_ok("kv4_attention_workspace_bytes", cache->kv_heads, q_heads, rows, max_q, max_seq) != HEISD_OK)
     return 0;
-  const Kv4Plan plan(batch, cache->kv_heads, q_heads / cache->kv_heads, max_q, max_seq);
-  return plan.n_chunks == 1 ? 256 : align256((size_t)rows * q_heads * plan.n_chunks * (cache->head_dim + 2) * sizeof(float)) + 256;
+  return Kv4Plan(batch, cache->kv_heads, q_heads / cache->kv_heads, max_q, max_seq, cache->head_dim).total;
 }
 
 template <typename T, int HD, int TERMS>
@@ -313,11 +321,11 @@ static void kv4_attention_launch(const Kv4Cache &c, const PagedBatch &b, const h
                                  const Kv4Attend &a, const Kv4Plan &plan, hipStream_t st) {
   const HeadRows<T> qi = head_rows<T>(*q), o = head_rows<T>(*out);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
-  const dim3 grid(c.kv_heads * plan.col_groups, plan.n_chunks, b.batch), block(256);
-  if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS><<<grid, block, 0, st>>>(c, b, qc, o, a);
-  else kv4_attend<T, HD, 1, TERMS><<<grid, block, 0, st>>>(c, b, qc, o, a);
-  if (plan.n_chunks > 1)
-    kv4_join<T, HD><<<dim3((unsigned)(((int64_t)b.rows * a.q_heads + 3) / 4)), block, 0, st>>>(c, b, o, a);
+  const dim3 block(256);
+  const int groups = plan.groups(TERMS, HD);
+  if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
+  else kv4_attend<T, HD, 1, TERMS><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
+  if (groups > 1) kv4_join<T, HD><<<dim3(plan.segments, b.batch), block, 0, st>>>(c, b, o, a, groups);
 }
 
 extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_head_rows *q,
@@ -337,12 +345,14 @@ extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_page
   if (!rows_aligned(*q, 16) || !rows_aligned(*out, 8)) return fail(nullptr, HEISD_EINVAL, "%s: q (16 bytes) or out (8 bytes) misaligned", who);
   if (!std::isfinite(scale)) return fail(nullptr, HEISD_EINVAL, "%s: scale %g", who, scale);
   if (b.rows == 0) return HEISD_OK;
-  const Kv4Plan plan(b.batch, c.kv_heads, q->heads / c.kv_heads, max_q, max_seq);
-  const size_t need = heisd_kv4_attention_workspace_bytes(cache, b.batch, b.rows, q->heads, max_q, max_seq);
+  const Kv4Plan plan(b.batch, c.kv_heads, q->heads / c.kv_heads, max_q, max_seq, cache->head_dim);
+  const size_t need = plan.total;
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned workspace", who);
   if (workspace_bytes < need) return fail(nullptr, HEISD_ENOMEM, "%s: workspace %zu bytes < %zu needed", who, workspace_bytes, need);
-  const Kv4Attend a{scale * 1.4426950408889634f, q->heads / c.kv_heads, q->heads, plan.chunk, plan.n_chunks, max_seq,
-                    static_cast<float *>(workspace), lse};
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  const Kv4Attend a{scale * 1.4426950408889634f, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
+                    reinterpret_cast<long long *>(ws + plan.starts), reinterpret_cast<float *>(ws + plan.part),
+                    reinterpret_cast<float *>(ws + plan.part_ml), lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (q->dtype == HEISD_DTYPE_BF16) {

@@ -95,12 +95,12 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int RB = HD * 2, CH = RB / 16, TILE = kPromptKeys * RB;                // bytes of a row, 16-byte pieces of it, a tile
   constexpr int NS = HD / 16, ND = HD / 32, NT = kPromptKeys / 32, NK = kPromptKeys / 16;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const int head = kvh * a.group + rest % a.group, tile = a.tiles - 1 - rest / a.group;
   // which sequence: sequence i is given tiles floor(cu[i] / 128) + i and on, enough for any length
   const int seq = wave_search(a.batch, tile, [&](int i) { return (long long)max(a.cu_q[i], 0) / kPromptRows + i; });
-  const Span rows = packed_span(a.cu_q, seq, a.rows), keys = packed_span(a.cu_k, seq, a.k_rows);
+  const Span rows = wave_span(a.cu_q, seq, a.rows), keys = wave_span(a.cu_k, seq, a.k_rows);
   const int first = (tile - (rows.begin / kPromptRows + seq)) * kPromptRows;
   if (first < 0 || first >= rows.count) return;
   const int shift = CAUSAL ? keys.count - rows.count : 0;                          // row i sees keys 0 .. shift + i
