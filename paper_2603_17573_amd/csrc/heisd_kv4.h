@@ -201,7 +201,6 @@ struct Kv4Pair {
 struct Kv4Attend {
   float scale_log2;                                 // softmax scale times log2(e)
   int group, q_heads, max_seq, cols;                // cols: columns a workgroup takes (16 or 32)
-  long long *starts;                                // [batch + 1] units of work before each request
   float *part, *part_ml;                            // sums of unfinished segments [2 * workgroups][cols][HD], their maxima and sums [..][cols][2]
   float *lse;
 };
@@ -213,11 +212,11 @@ constexpr int kKv4Unit = 128;
 // Workgroups of 256 threads that the registers of a compute unit hold: queries of two terms or two column tiles need more of them.
 __host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles, int terms) { return col_tiles == 1 && (terms == 1 || head_dim == 64) ? 3 : 2; }
 
-// What a request asks for: its rows, its tokens, units per segment, segments.
+// What a request asks for: its rows, its tokens, units per segment, units in all.
 struct Kv4Request {
   Span rows;
-  int seq, units, segments;
-  __device__ __forceinline__ long long work() const { return (long long)units * segments; }
+  int seq, units;
+  long long work;
 };
 __device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const PagedBatch &b, const Kv4Attend &a, int i) {
   Kv4Request r;
@@ -225,31 +224,25 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const Paged
   r.seq = b.seq_len[i];
   if (r.seq < 0 || r.seq > a.max_seq || (long long)r.seq > (long long)b.max_blocks * c.block_size) r.seq = 0;
   r.units = max((r.seq + kKv4Unit - 1) / kKv4Unit, 1);          // one even without tokens: somebody writes the zeros
-  r.segments = (r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads;
+  r.work = (long long)r.units * ((r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads);
   return r;
 }
 
-// Sum over the workgroup and, for each thread, over those before it (exclusive).
-__device__ __forceinline__ long long kv4_scan(long long v, long long &total, long long *wave_sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long long x = v;
+__device__ __forceinline__ long long wave_sum64(long long v) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long t = __shfl_up(x, o);
-    if (lane >= o) x += t;
-  }
-  if (lane == 63) wave_sums[wave] = x;
-  __syncthreads();
-  long long before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += wave_sums[w];
-    total += wave_sums[w];
-  }
-  __syncthreads();
-  return before + x - v;
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
 }
+__device__ __forceinline__ long long lane_value64(long long v, int lane) {
+  return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)v, lane) |
+                     (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32);
+}
+// Quotient of numbers that are not negative; nearly always they fit 32 bits.
+__device__ __forceinline__ long long wave_div(long long a, long long b) {
+  return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+// Units per workgroup of a call of `all` units.
+__device__ __forceinline__ long long kv4_run(long long all, int groups) { return max(wave_div(all + groups - 1, groups), 1ll); }
 
 // Online softmax state of a column (one query row of one head): maximum and sum in powers of two.
 constexpr float kKv4Lazy = 8.f;                     // the maximum is moved only when it grew by more than this (powers of two)
@@ -268,61 +261,46 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
   constexpr int LD = HD + 4;
   __shared__ __attribute__((aligned(16))) float s_out[4][16 * LD];
   __shared__ float s_m[4][16], s_l[4][16];
-  __shared__ long long s_sum[4], s_start[256];                  // units before each of the 256 requests at hand
+  __shared__ long long s_start[4][64];
+  __shared__ int4 s_req[4][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int bs = c.block_size;
 
-  // this workgroup's run of units
-  long long all = 0, chunk_work = 0, mine = 0;
-  int first = 0;                                                // the requests at hand: first .. first + 255
-  for (int i = 0; i < b.batch; i += 256) {
-    const int r = i + threadIdx.x;
-    const long long w = r < b.batch ? kv4_request(c, b, a, r).work() : 0;
-    const long long before = all + kv4_scan(w, chunk_work, s_sum);
-    if (i == 0) mine = before;
-    if (blockIdx.x == 0 && r < b.batch) a.starts[r] = before;   // for kv4_join
-    all += chunk_work;
-  }
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.starts[b.batch] = all;
-  const long long groups = min((long long)gridDim.x, all);       // no run is empty
-  if (blockIdx.x >= groups) return;
-  long long at = all * blockIdx.x / groups;
-  const long long run0 = at, run1 = all * (blockIdx.x + 1) / groups;
-  long long end = 0;                                            // units before the end of the requests at hand
-  {
-    long long carry = 0;
-    for (;; first += 256) {
-      const int r = first + threadIdx.x;
-      if (first > 0) mine = carry + kv4_scan(r < b.batch ? kv4_request(c, b, a, r).work() : 0, chunk_work, s_sum);
-      else if (b.batch > 256) kv4_scan(r < b.batch ? kv4_request(c, b, a, r).work() : 0, chunk_work, s_sum);
-      end = carry + chunk_work;
-      if (at < end) break;
-      carry = end;
+  // This workgroup's run of units.  Every wave finds it for itself: 64 requests are at hand (in LDS, a request per lane), 64 more while the
+  // run lies behind them.
+  int first = 0;
+  long long end;                                                // units before the end of these 64
+  auto requests = [&](long long before) {
+    Kv4Request r = kv4_request(c, b, a, min(first + lane, b.batch - 1));
+    if (first + lane >= b.batch) r.work = 0;
+    long long start = r.work;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long t = __shfl_up(start, o);
+      if (lane >= o) start += t;
     }
-  }
-  s_start[threadIdx.x] = mine;
-  __syncthreads();
+    end = before + lane_value64(start, 63);
+    s_start[wave][lane] = start + before - r.work;
+    s_req[wave][lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
+  };
+  requests(0);
+  long long all = end;
+  for (int i = 64; i < b.batch; i += 64) all += wave_sum64(i + lane < b.batch ? kv4_request(c, b, a, i + lane).work : 0);
+  const long long per = kv4_run(all, gridDim.x), run0 = blockIdx.x * per, run1 = min(run0 + per, all);
 
-  while (at < run1) {
-    if (at >= end) {                                            // on to the next requests
-      long long work;
-      do {
-        first += 256;
-        const int r = first + threadIdx.x;
-        const long long x = end + kv4_scan(r < b.batch ? kv4_request(c, b, a, r).work() : 0, work, s_sum);
-        s_start[threadIdx.x] = x;
-        end += work;
-      } while (at >= end);
-      __syncthreads();
+  for (long long at = run0; at < run1;) {
+    while (at >= end) {
+      first += 64;
+      requests(end);
     }
-    const int local = wave_search(min(256, b.batch - first), at, [&](int i) { return s_start[i]; });
+    const int local = 63 - __clzll(__ballot(s_start[wave][lane] <= at));      // the last of those that begin here has the work
     const int req = first + local;
-    const long long at_req = s_start[local];
-    Kv4Request rq = kv4_request(c, b, a, req);
-    const Span rows{__builtin_amdgcn_readfirstlane(rq.rows.begin), __builtin_amdgcn_readfirstlane(rq.rows.count)};
-    const int seq = __builtin_amdgcn_readfirstlane(rq.seq), units = __builtin_amdgcn_readfirstlane(rq.units);
-    const int segment = __builtin_amdgcn_readfirstlane((int)((at - at_req) / units));
-    const int u0 = __builtin_amdgcn_readfirstlane((int)(at - at_req - (long long)segment * units));
+    const int4 rq = s_req[wave][local];
+    const Span rows{__builtin_amdgcn_readfirstlane(rq.x), __builtin_amdgcn_readfirstlane(rq.y)};
+    const int seq = __builtin_amdgcn_readfirstlane(rq.z), units = __builtin_amdgcn_readfirstlane(rq.w);
+    const long long in_req = at - lane_value64(s_start[wave][lane], local);
+    const int segment = __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
+    const int u0 = __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
     const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
     const int head = segment % c.kv_heads, col0 = segment / c.kv_heads * (16 * CT);
     const bool whole = u0 == 0 && u1 == units;
@@ -343,12 +321,11 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
     }
     f32x4 acc[CT][ND];
     float m[CT], l[CT];
-    bool nan_out[CT];
+    uint32_t odd = 0;                                           // met a value that is not finite among tokens that not everybody may see
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       m[ct] = -INFINITY;
       l[ct] = 0.f;
-      nan_out[ct] = false;
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[ct][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -418,7 +395,6 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[ct][e] = s[ct][e >> 2][e & 3] * a.scale_log2;
       if (gone0 || gone1 || base + 32 > seq - rows.count + 1) {
-        bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int t = base + 16 * (e >> 2) + 4 * quad + (e & 3);
@@ -429,18 +405,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
           // a probability of zero times a value that is not finite would be NaN: such values leave the product
           const uint32_t mask = 0xFFu << (8 * (e & 3));
           const bool large = ((ve[e >> 2] >> (8 * (e & 3))) & 0xFFu) >= kKv4NotFinite;
-          odd = odd || (large && !gone);
+          odd |= (uint32_t)(large && !gone);
           if (large || gone) ve[e >> 2] &= ~mask;
-        }
-        if (__ballot(odd)) {                        // and what is NaN makes NaN of the columns that do see it
-          for (int t = base; t < min(base + 32, seq); ++t) {
-            const int id = __builtin_amdgcn_readlane(my_id, 2 * i + ((t - base) >> 4));
-            if (id < 0) continue;
-            const int o = t & (bs - 1);
-            const uint8_t e = c.at(id, head)[Kv4Offsets<HD>::v_exp(bs) + ((o / 4) * (HD / 32) + quad * (HD / 4) / 32) * 4 + o % 4];
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) nan_out[ct] = nan_out[ct] || (e >= kKv4NotFinite && t < seen[ct]);
-          }
         }
       }
       bf16x8 pf[CT][TERMS];
@@ -504,12 +470,17 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
             acc[ct][2 * dd + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[ct][e], acc[ct][2 * dd + 1], 0, 0, 0);
           }
       };
+      // one after the other: the compiler would convert them all first and run out of registers
       channels(std::integral_constant<int, 0>{});
+      __builtin_amdgcn_sched_barrier(0);
       channels(std::integral_constant<int, 1>{});
       if constexpr (HD == 128) {
+        __builtin_amdgcn_sched_barrier(0);
         channels(std::integral_constant<int, 2>{});
+        __builtin_amdgcn_sched_barrier(0);
         channels(std::integral_constant<int, 3>{});
       }
+      __builtin_amdgcn_sched_barrier(0);
     };
     for (t0 = u0 * kKv4Unit; t0 < t1; t0 += 32 * kKv4Unit) {
       // the blocks of the wave's tiles: lane 2 i + n holds that of tile n of its i-th pair of these 32
@@ -526,6 +497,18 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
         use_pair(next, i + 1);
       }
     }
+    // what is not finite makes NaN of the columns that do see it (rare: the exponents of all of the wave's tokens are read again)
+    uint32_t nan_out = 0;                                       // bit ct: the lane's column of tile ct, in the lane's channels
+    if (__ballot(odd)) {
+      for (int t = u0 * kKv4Unit; t < t1; ++t) {
+        if ((t / 32 - wave) % 4) continue;
+        const int id = b.table[(long long)req * b.max_blocks + (t >> c.block_shift)], o = t & (bs - 1);
+        if (id < 0 || id >= c.n_blocks) continue;
+        const uint8_t e = c.at(id, head)[Kv4Offsets<HD>::v_exp(bs) + ((o / 4) * (HD / 32) + quad * (HD / 4) / 32) * 4 + o % 4];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) nan_out |= (uint32_t)(e >= kKv4NotFinite && t < seen[ct]) << ct;
+      }
+    }
     // join the waves, a tile of columns at a time
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -538,7 +521,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) to[(4 * quad + e) * ND + d] = nan_out[ct] ? __uint_as_float(0x7FC00000u) : acc[ct][d][e];
+        for (int d = 0; d < ND; ++d) to[(4 * quad + e) * ND + d] = nan_out >> ct & 1 ? __uint_as_float(0x7FC00000u) : acc[ct][d][e];
       __syncthreads();
       for (int u = threadIdx.x; u < 16 * (HD / 4); u += 256) {
         const int n = u / (HD / 4), d = u % (HD / 4) * 4, cn = col0 + ct * 16 + n;
@@ -576,32 +559,54 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
 // a column per thread.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4Attend a, int grid) {
-  const int req = blockIdx.y, segment = blockIdx.x;
+  const int req = blockIdx.y, lane = threadIdx.x & 63;
+  long long before = 0, all = 0;
+  for (int i = lane; i < b.batch; i += 64) {
+    const long long work = kv4_request(c, b, a, i).work;
+    all += work;
+    if (i < req) before += work;
+  }
   const Kv4Request r = kv4_request(c, b, a, req);
-  const long long all = a.starts[b.batch], groups = min((long long)grid, all);
-  for (int seg = segment; seg < r.segments; seg += gridDim.x) {
-    const long long s0 = a.starts[req] + (long long)seg * r.units, s1 = s0 + r.units - 1;
-    const int w0 = (int)(((s0 + 1) * groups - 1) / all), w1 = (int)(((s1 + 1) * groups - 1) / all);   // who has the first, the last unit
+  before = wave_sum64(before);
+  const long long per = kv4_run(wave_sum64(all), grid);
+  const int segments = (int)wave_div(r.work, r.units);
+  for (int seg = blockIdx.x; seg < segments; seg += gridDim.x) {
+    const long long s0 = before + (long long)seg * r.units;
+    const int w0 = (int)wave_div(s0, per), w1 = (int)wave_div(s0 + r.units - 1, per);   // who has the first, the last unit
     if (w0 == w1) continue;
-    const int first_slot = 2 * w0 + (all * w0 / groups != s0);                     // the others begin their runs inside the segment
+    const int first_slot = 2 * w0 + (w0 * per != s0);                              // the others begin their runs inside the segment
     const int head = seg % c.kv_heads, col0 = seg / c.kv_heads * a.cols, n_cols = min(r.rows.count * a.group - col0, a.cols);
     for (int u = threadIdx.x; u < n_cols * (HD / 4); u += 256) {
       const int n = u / (HD / 4), d = u % (HD / 4) * 4;
-      auto slot = [&](int w) { return (long long)(w == w0 ? first_slot : 2 * w) * a.cols + n; };
-      float top = -INFINITY;
-#pragma unroll 4
-      for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.part_ml[slot(w) * 2]);
-      float sum = 0.f;
+      float top = -INFINITY, sum = 0.f;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int w = w0; w <= w1; ++w) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + slot(w) * 2);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part + slot(w) * HD + d);
-        if (ml.x != -INFINITY) {
-          const float by = exp2_fast(ml.x - top);
-          sum += ml.y * by;
-          o += x * by;
+      constexpr int K = 8;                                                         // parts requested at once
+      for (int w = w0; w <= w1; w += K) {
+        float2 ml[K];
+        f32x4 x[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+          const int wi = min(w + i, w1);
+          const long long at = (long long)(wi == w0 ? first_slot : 2 * wi) * a.cols + n;
+          ml[i] = *reinterpret_cast<const float2 *>(a.part_ml + at * 2);
+          x[i] = *reinterpret_cast<const f32x4 *>(a.part + at * HD + d);
+          if (w + i > w1) ml[i].x = -INFINITY;
         }
+        float next = top;
+#pragma unroll
+        for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
+        if (next == -INFINITY) continue;
+        const float keep = exp2_fast(top - next);
+        sum *= keep;
+        o *= keep;
+        top = next;
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+          if (ml[i].x != -INFINITY) {
+            const float by = exp2_fast(ml[i].x - top);
+            sum += ml[i].y * by;
+            o += x[i] * by;
+          }
       }
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       const int i = (col0 + n) / a.group, h = head * a.group + (col0 + n - i * a.group);

@@ -283,7 +283,7 @@ constexpr int kKv4Units = 256;                       // compute units that the g
 struct Kv4Plan {
   int col_tiles, segments;
   int64_t units;
-  size_t starts, part, part_ml, total;
+  size_t part_ml, total;
   int groups(int terms, int head_dim) const {
     return (int)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, kv4_per_unit(head_dim, col_tiles, terms) * kKv4Units));
   }
@@ -293,9 +293,7 @@ struct Kv4Plan {
     segments = (int)std::min<int64_t>(kv_heads * ((cols + 16 * col_tiles - 1) / (16 * col_tiles)), 65535);
     units = batch * segments * ((max_seq + kKv4Unit - 1) / kKv4Unit);
     const size_t rows = (size_t)2 * groups(1, (int)head_dim) * 16 * col_tiles;       // (one term: the larger grid)
-    starts = 0;
-    part = align256((size_t)(batch + 1) * sizeof(int64_t));
-    part_ml = part + align256(rows * (size_t)head_dim * sizeof(float));
+    part_ml = align256(rows * (size_t)head_dim * sizeof(float));
     total = part_ml + align256(rows * 2 * sizeof(float));
   }
 };
@@ -351,8 +349,7 @@ extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_page
   if (workspace_bytes < need) return fail(nullptr, HEISD_ENOMEM, "%s: workspace %zu bytes < %zu needed", who, workspace_bytes, need);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   const Kv4Attend a{scale * 1.4426950408889634f, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
-                    reinterpret_cast<long long *>(ws + plan.starts), reinterpret_cast<float *>(ws + plan.part),
-                    reinterpret_cast<float *>(ws + plan.part_ml), lse};
+                    reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + plan.part_ml), lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (q->dtype == HEISD_DTYPE_BF16) {
