@@ -46,6 +46,10 @@ __device__ __forceinline__ void lds_dma16_s(const void *sbase, uint32_t lane_off
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(lane_off), "s"(sbase)
                : "memory");
 }
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void lds_dma4(const void *gptr, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr), "v"(gptr) : "memory");
+}
 // s_waitcnt vmcnt(N) and nothing else, as a compiler-level memory barrier too: no load or store of
 // the surrounding code may be moved across it (the count is only right for the written order).
 template <int N>

@@ -190,12 +190,20 @@ __global__ __launch_bounds__(256) void kv4_gather(Kv4Cache c, PagedBatch b, cons
 
 // ---- attention ------------------------------------------------------------------------------------------------------
 
-// What a wave holds of two tiles of 16 tokens.
+// What a lane holds of two tiles of 16 tokens.
 template <int HD>
 struct Kv4Pair {
   static constexpr int W = HD / 32;                 // dwords of codes per lane and tile
   uint32_t kc[2][W], vc[2][W];
   uint32_t ke[2], ve[2];                            // the lane's key exponent; the exponents of its four value tokens
+};
+// Where two tiles lie in LDS: key codes of both, value codes of both, then 64 bytes each of key exponents and of value exponents.  With heads of 128 the
+// pieces of a tile's key codes are in the order of the lanes that read them.
+constexpr int kKv4Ring = 2;                         // pairs of tiles on their way per wave
+template <int HD>
+struct Kv4Slot {
+  static constexpr int TILE = 16 * HD / 2, V = 2 * TILE, EXP = 4 * TILE, BYTES = EXP + 256;
+  static constexpr int TRANSFERS = (HD == 128 ? 4 : 2) + 1;
 };
 
 struct Kv4Attend {
@@ -259,7 +267,10 @@ template <typename T, int HD, int CT, int TERMS>
 __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
   constexpr int W = HD / 32, ND = HD / 16, KJ = HD / 32;        // code dwords, tiles of channels, products per score tile
   constexpr int LD = HD + 4;
-  __shared__ __attribute__((aligned(16))) float s_out[4][16 * LD];
+  typedef Kv4Slot<HD> Slot;
+  constexpr int MINE = kKv4Ring * Slot::BYTES;                  // a wave's part of LDS: its ring, at the end of a segment its sums
+  static_assert(MINE >= 16 * LD * 4 && MINE % 16 == 0, "the sums take the ring's place");
+  __shared__ __attribute__((aligned(16))) unsigned char s_mine[4][MINE];
   __shared__ float s_m[4][16], s_l[4][16];
   __shared__ long long s_start[4][64];
   __shared__ int4 s_req[4][64];
@@ -330,29 +341,49 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       for (int d = 0; d < ND; ++d) acc[ct][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     int t0 = 0, my_id = -1;                                     // tokens t0 .. t0 + 4095 are at hand
-    auto load_pair = [&](Kv4Pair<HD> &p, int i) {
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)s_mine[wave];
+    // Requests pair i: codes 16 bytes a lane, all exponents in one transfer of 4 bytes a lane.
+    auto fetch = [&](int i) {
+      const uint32_t to = __builtin_amdgcn_readfirstlane(ring + i % kKv4Ring * Slot::BYTES);
+      const uint8_t *cell[2];
+      int t[2];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        const int id = max(__builtin_amdgcn_readlane(my_id, 2 * i + n), 0);          // a missing block: any block, masked below
-        const int t = (t0 + 32 * (wave + 4 * i) + 16 * n) & (bs - 1);
-        const uint8_t *cell = c.at(id, head);
-        const uint8_t *kp = cell + t * (HD / 2) + col * (HD / 2) + quad * (HD / 8);
-        const uint8_t *vp = cell + Kv4Offsets<HD>::v_codes(bs) + t * (HD / 2) + quad * (2 * HD) + col * (HD / 8);
+        cell[n] = c.at(max(__builtin_amdgcn_readlane(my_id, 2 * i + n), 0), head);   // a missing block: any block, masked below
+        t[n] = (t0 + 32 * (wave + 4 * i) + 16 * n) & (bs - 1);
+        if constexpr (HD == 128) {
+          lds_dma16_s(cell[n] + t[n] * (HD / 2), col * (HD / 2) + quad * (HD / 8), to + n * Slot::TILE);
+          lds_dma16_s(cell[n] + Kv4Offsets<HD>::v_codes(bs) + t[n] * (HD / 2), lane * 16, to + Slot::V + n * Slot::TILE);
+        }
+      }
+      const int n = lane >> 4 & 1;                              // the exponents: both tiles' keys, then both tiles' values
+      const uint8_t *e = (n ? cell[1] : cell[0]) + (n ? t[1] : t[0]) * (HD / 32) + lane % (HD / 8) * 4;
+      if constexpr (HD == 64) {                                 // a transfer brings both tiles
+        const uint8_t *x = (lane >> 5 ? cell[1] : cell[0]) + (lane >> 5 ? t[1] : t[0]) * (HD / 2) + lane % 32 * 16;
+        lds_dma16(x, to);
+        lds_dma16(x + Kv4Offsets<HD>::v_codes(bs), to + Slot::V);
+      }
+      lds_dma4(e + (lane >> 5 ? Kv4Offsets<HD>::v_exp(bs) : Kv4Offsets<HD>::k_exp(bs)), to + Slot::EXP);
+    };
+    auto take = [&](Kv4Pair<HD> &p, int i) {
+      const unsigned char *from = s_mine[wave] + i % kKv4Ring * Slot::BYTES;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
         if constexpr (W == 4) {
-          const u32x4 x = *reinterpret_cast<const u32x4 *>(kp), y = *reinterpret_cast<const u32x4 *>(vp);
+          const u32x4 x = *reinterpret_cast<const u32x4 *>(from + n * Slot::TILE + lane * 16);
+          const u32x4 y = *reinterpret_cast<const u32x4 *>(from + Slot::V + n * Slot::TILE + lane * 16);
 #pragma unroll
           for (int w = 0; w < W; ++w) p.kc[n][w] = x[w], p.vc[n][w] = y[w];
         } else {
-          const u32x2 x = *reinterpret_cast<const u32x2 *>(kp), y = *reinterpret_cast<const u32x2 *>(vp);
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(from + n * Slot::TILE + col * (HD / 2) + quad * (HD / 8));
+          const u32x2 y = *reinterpret_cast<const u32x2 *>(from + Slot::V + n * Slot::TILE + lane * 8);
 #pragma unroll
           for (int w = 0; w < W; ++w) p.kc[n][w] = x[w], p.vc[n][w] = y[w];
         }
-        p.ke[n] = cell[Kv4Offsets<HD>::k_exp(bs) + (t + col) * (HD / 32) + quad * (HD / 4) / 32];
-        p.ve[n] = *reinterpret_cast<const uint32_t *>(cell + Kv4Offsets<HD>::v_exp(bs) + t * (HD / 32) +
-                                                      (quad * (HD / 32) + col * (HD / 16) / 32) * 4);
+        p.ke[n] = from[Slot::EXP + n * 64 + col * (HD / 32) + quad * (HD / 4) / 32];
+        p.ve[n] = *reinterpret_cast<const uint32_t *>(from + Slot::EXP + 128 + n * 64 + (quad * (HD / 32) + col * (HD / 16) / 32) * 4);
       }
     };
-    Kv4Pair<HD> now, next;
     bf16x8 qf[CT][KJ][TERMS];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -488,13 +519,16 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       my_id = t < t1 ? b.table[(long long)req * b.max_blocks + (t >> c.block_shift)] : -1;
       if (my_id >= c.n_blocks) my_id = -1;
       const int n_pairs = max((min(t1 - t0, 32 * kKv4Unit) + 127 - 32 * wave) >> 7, 0);
-      if (n_pairs > 0) load_pair(now, 0);
-      for (int i = 0; i < n_pairs; i += 2) {
-        if (i + 1 < n_pairs) load_pair(next, i + 1);
-        use_pair(now, i);
-        if (i + 1 >= n_pairs) break;
-        if (i + 2 < n_pairs) load_pair(now, i + 2);
-        use_pair(next, i + 1);
+      wait_vmcnt_all();                                         // the compiler's own loads: none may be waited for among the transfers
+      for (int i = 0; i < min(n_pairs, kKv4Ring); ++i) fetch(i);
+      for (int i = 0; i < n_pairs; ++i) {
+        if (i + kKv4Ring - 1 < n_pairs) wait_vmcnt<(kKv4Ring - 1) * Slot::TRANSFERS>();
+        else wait_vmcnt<0>();
+        Kv4Pair<HD> p;
+        take(p, i);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the pair is in registers: its place may be written again
+        if (i + kKv4Ring < n_pairs) fetch(i + kKv4Ring);
+        use_pair(p, i);
       }
     }
     // what is not finite makes NaN of the columns that do see it (rare: the exponents of all of the wave's tokens are read again)
@@ -517,7 +551,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
         s_m[wave][col] = m[ct];
         s_l[wave][col] = l[ct];
       }
-      float *to = s_out[wave] + col * LD;
+      float *to = reinterpret_cast<float *>(s_mine[wave]) + col * LD;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -534,7 +568,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
           if (s_m[w][n] != -INFINITY) {             // a wave that saw nothing holds nothing
             const float by = exp2_fast(s_m[w][n] - top);
             sum += s_l[w][n] * by;
-            o += *reinterpret_cast<const f32x4 *>(s_out[w] + n * LD + d) * by;
+            o += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_mine[w]) + n * LD + d) * by;
           }
         const int i = cn / a.group, h = head * a.group + (cn - i * a.group);
         const long long r = rows.begin + i;
