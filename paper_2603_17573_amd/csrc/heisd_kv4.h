@@ -207,7 +207,8 @@ struct Kv4Slot {
 };
 
 struct Kv4Attend {
-  float scale_log2;                                 // softmax scale times log2(e)
+  float scale_log2;                                 // magnitude of the softmax scale times log2(e)
+  bool flip;                                        // the scale is negative
   int group, q_heads, max_seq, cols;                // cols: columns a workgroup takes (16 or 32)
   float *part, *part_ml;                            // sums of unfinished segments [2 * workgroups][cols][HD], their maxima and sums [..][cols][2]
   float *lse;
@@ -218,7 +219,7 @@ struct Kv4Attend {
 constexpr int kKv4Unit = 128;
 
 // Workgroups of 256 threads that the registers of a compute unit hold: queries of two terms or two column tiles need more of them.
-__host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles, int terms) { return col_tiles == 1 && (terms == 1 || head_dim == 64) ? 3 : 2; }
+__host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles, int terms) { return col_tiles == 2 ? 2 : head_dim == 64 ? 4 : 3; }
 
 // What a request asks for: its rows, its tokens, units per segment, units in all.
 struct Kv4Request {
@@ -272,8 +273,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
   static_assert(MINE >= 16 * LD * 4 && MINE % 16 == 0, "the sums take the ring's place");
   __shared__ __attribute__((aligned(16))) unsigned char s_mine[4][MINE];
   __shared__ float s_m[4][16], s_l[4][16];
-  __shared__ long long s_start[4][64];
-  __shared__ int4 s_req[4][64];
+  __shared__ long long s_start[64];                             // every wave writes the same values before it reads them
+  __shared__ int4 s_req[64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int bs = c.block_size;
 
@@ -291,8 +292,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       if (lane >= o) start += t;
     }
     end = before + lane_value64(start, 63);
-    s_start[wave][lane] = start + before - r.work;
-    s_req[wave][lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
+    s_start[lane] = start + before - r.work;
+    s_req[lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
   };
   requests(0);
   long long all = end;
@@ -304,12 +305,12 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       first += 64;
       requests(end);
     }
-    const int local = 63 - __clzll(__ballot(s_start[wave][lane] <= at));      // the last of those that begin here has the work
+    const int local = 63 - __clzll(__ballot(s_start[lane] <= at));      // the last of those that begin here has the work
     const int req = first + local;
-    const int4 rq = s_req[wave][local];
+    const int4 rq = s_req[local];
     const Span rows{__builtin_amdgcn_readfirstlane(rq.x), __builtin_amdgcn_readfirstlane(rq.y)};
     const int seq = __builtin_amdgcn_readfirstlane(rq.z), units = __builtin_amdgcn_readfirstlane(rq.w);
-    const long long in_req = at - lane_value64(s_start[wave][lane], local);
+    const long long in_req = at - lane_value64(s_start[lane], local);
     const int segment = __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
     const int u0 = __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
     const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       for (int j = 0; j < KJ; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float f = (float)qr[ct][j][e];
+          const float f = a.flip ? -(float)qr[ct][j][e] : (float)qr[ct][j][e];   // a negative scale: larger products are larger scores
           qf[ct][j][0][e] = (__bf16)f;
           if constexpr (TERMS == 2) qf[ct][j][1][e] = (__bf16)(f - (float)qf[ct][j][0][e]);
         }
@@ -424,7 +425,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[ct][e] = s[ct][e >> 2][e & 3] * a.scale_log2;
+        for (int e = 0; e < 8; ++e) x[ct][e] = s[ct][e >> 2][e & 3];
       if (gone0 || gone1 || base + 32 > seq - rows.count + 1) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
         float top = x[ct][0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, x[ct][e]);
-        top = max_xor32(max_xor16(top));
+        top = max_xor32(max_xor16(top)) * a.scale_log2;
         if (__ballot(top > m[ct] + kKv4Lazy)) {
           const float next = fmaxf(m[ct], top);
           const float by = next == -INFINITY ? 1.f : exp2_fast(m[ct] - next);
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
         const float use = m[ct] == -INFINITY ? 0.f : m[ct];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float pr = exp2_fast(x[ct][e] - use);
+          const float pr = exp2_fast(__builtin_fmaf(x[ct][e], a.scale_log2, -use));
           l[ct] += pr;
           pf[ct][0][e] = (__bf16)pr;
           if constexpr (TERMS == 2) pf[ct][1][e] = (__bf16)(pr - (float)pf[ct][0][e]);
@@ -467,10 +468,10 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       float vs[2][4];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        vs[n][0] = __uint_as_float((ve[n] << 23) & 0x7F800000u);
-        vs[n][1] = __uint_as_float((ve[n] << 15) & 0x7F800000u);
-        vs[n][2] = __uint_as_float((ve[n] << 7) & 0x7F800000u);
-        vs[n][3] = __uint_as_float((ve[n] >> 1) & 0x7F800000u);
+        vs[n][0] = __uint_as_float(ve[n] << 23);    // of a scale the conversion reads the exponent only: the bits beside it may stay
+        vs[n][1] = __uint_as_float(ve[n] << 15);
+        vs[n][2] = __uint_as_float(ve[n] << 7);
+        vs[n][3] = __uint_as_float(ve[n] >> 1);
       }
       // two channels at a time: a conversion gives channels 2 d, 2 d + 1 of one token, a product takes one channel of eight tokens
       auto channels = [&](auto which) {

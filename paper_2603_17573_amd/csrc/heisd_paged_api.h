@@ -348,7 +348,8 @@ extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_page
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned workspace", who);
   if (workspace_bytes < need) return fail(nullptr, HEISD_ENOMEM, "%s: workspace %zu bytes < %zu needed", who, workspace_bytes, need);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  const Kv4Attend a{scale * 1.4426950408889634f, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
+  const Kv4Attend a{std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f),      // not 0: minus infinity stands for masked scores
+                    scale < 0, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
                     reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + plan.part_ml), lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
