@@ -119,18 +119,22 @@ __device__ __forceinline__ float kv4_scale(uint32_t e) {
   return e == 255 ? __uint_as_float(0x7FC00000u) : e == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(e << 23);
 }
 
-constexpr int kGatherRows = 16;
+// Rows and heads that a workgroup reads back; a lane writes 16 bytes, so that a wave's store is whole lines in either width.
+template <typename T>
+constexpr int kGatherRows = 32 / sizeof(T);
+constexpr int kGatherHeads = 4;
 
-// Sixteen packed rows per workgroup, head by head: the rows of a block that follow each other lie together in the cache.  Rows
-// of a block that the pool does not have are zero.  Bound by memory.
+// Some packed rows and heads per workgroup, head by head: the rows of a block that follow each other lie together in the cache.
+// A thread requests its values of all heads before it converts the first.  Rows of a block that the pool does not have are
+// zero.  Bound by memory, most of it the rows that are written.
 template <typename T, int HD, bool VEC>
 __global__ __launch_bounds__(256) void kv4_gather(Kv4Cache c, PagedBatch b, const int32_t *cu_seq, int out_rows,
                                                   HeadRows<T> k, HeadRows<T> v) {
-  constexpr int LH = HD / 8;
-  __shared__ int where[kGatherRows];                // slot, -1: no such token (a zero row), -2: nobody's row
-  const int r0 = blockIdx.x * kGatherRows, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const bool is_v = blockIdx.y;
-  for (int i = wave; i < kGatherRows; i += 4) {
+  constexpr int E = 16 / sizeof(T), LH = HD / E, ROWS = kGatherRows<T>, PER = 256 / (ROWS * LH);   // values per lane, lanes per row and head, heads at a time
+  __shared__ int where[ROWS];                       // slot, -1: no such token (a zero row), -2: nobody's row
+  const int r0 = blockIdx.x * ROWS, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool is_v = blockIdx.z;
+  for (int i = wave; i < ROWS; i += 4) {
     int w = -2;
     if (r0 + i < out_rows) {
       const int q = wave_search(b.batch, r0 + i, [&](int n) { return (long long)cu_seq[n]; });
@@ -145,45 +149,47 @@ __global__ __launch_bounds__(256) void kv4_gather(Kv4Cache c, PagedBatch b, cons
     if (lane == 0) where[i] = w;
   }
   __syncthreads();
-  for (int u = threadIdx.x; u < c.kv_heads * kGatherRows * LH; u += 256) {
-    const int j = u % LH, i = u / LH % kGatherRows, h = u / (LH * kGatherRows);
-    const int s = where[i];
-    if (s == -2) continue;
-    float f[8];
-    if (s < 0) {
+  const int j = threadIdx.x % LH, i = threadIdx.x / LH % ROWS, h0 = blockIdx.y * kGatherHeads + threadIdx.x / (LH * ROWS);
+  const int s = where[i];
+  if (s == -2) return;
+  const int id = max(s, 0) >> c.block_shift, t = s & (c.block_size - 1);
+  uint32_t code[kGatherHeads / PER], e[kGatherHeads / PER];
 #pragma unroll
-      for (int n = 0; n < 8; ++n) f[n] = 0.f;
+  for (int n = 0; n < kGatherHeads / PER; ++n) {
+    code[n] = e[n] = 0;
+    const int h = h0 + n * PER;
+    if (s < 0 || h >= c.kv_heads) continue;
+    const uint8_t *cell = c.at(id, h);
+    const int d = j * E;                            // the lane's first channel
+    if (!is_v) {
+      const uint8_t *from = cell + t * (HD / 2) + d / 2;
+      code[n] = E == 8 ? *reinterpret_cast<const uint32_t *>(from) : *reinterpret_cast<const uint16_t *>(from);
+      e[n] = cell[Kv4Offsets<HD>::k_exp(c.block_size) + t * (HD / 32) + d / 32];
     } else {
-      const int id = s >> c.block_shift, t = s & (c.block_size - 1);
-      const uint8_t *cell = c.at(id, h);
-      uint32_t code, e;
-      if (!is_v) {
-        code = *reinterpret_cast<const uint32_t *>(cell + t * (HD / 2) + j * 4);
-        e = cell[Kv4Offsets<HD>::k_exp(c.block_size) + t * (HD / 32) + j / 4];
-      } else {
-        const uint8_t *from = cell + Kv4Offsets<HD>::v_codes(c.block_size) + (t / 4) * (2 * HD);
-        if constexpr (HD == 128) code = *reinterpret_cast<const uint32_t *>(from + j * 16 + (t % 4) * 4);
-        else
-          code = *reinterpret_cast<const uint16_t *>(from + 2 * j * 8 + (t % 4) * 2) |
-                 (uint32_t)*reinterpret_cast<const uint16_t *>(from + (2 * j + 1) * 8 + (t % 4) * 2) << 16;
-        e = cell[Kv4Offsets<HD>::v_exp(c.block_size) + ((t / 4) * (HD / 32) + j / 4) * 4 + t % 4];
-      }
-      const float scale = kv4_scale(e);
-      const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 1),
-                 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 3);
-      f[0] = p0[0] * scale, f[1] = p0[1] * scale, f[2] = p1[0] * scale, f[3] = p1[1] * scale;
+      constexpr int PIECE = HD / 16;                // channels that lie together
+      const uint8_t *from = cell + Kv4Offsets<HD>::v_codes(c.block_size) + (t / 4) * (2 * HD) + d / PIECE * (2 * PIECE) + (t % 4) * (PIECE / 2) + d % PIECE / 2;
+      if constexpr (E <= PIECE) code[n] = E == 8 ? *reinterpret_cast<const uint32_t *>(from) : *reinterpret_cast<const uint16_t *>(from);
+      else code[n] = *reinterpret_cast<const uint16_t *>(from) | (uint32_t)*reinterpret_cast<const uint16_t *>(from + 2 * PIECE) << 16;
+      e[n] = cell[Kv4Offsets<HD>::v_exp(c.block_size) + ((t / 4) * (HD / 32) + d / 32) * 4 + t % 4];
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kGatherHeads / PER; ++n) {
+    const int h = h0 + n * PER;
+    if (h >= c.kv_heads) return;
+    const float scale = kv4_scale(e[n]);
+    float f[8];
+    const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[n], 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[n], 1.f, 1);
+    f[0] = p0[0] * scale, f[1] = p0[1] * scale, f[2] = p1[0] * scale, f[3] = p1[1] * scale;
+    if constexpr (E == 8) {
+      const auto p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[n], 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[n], 1.f, 3);
       f[4] = p2[0] * scale, f[5] = p2[1] * scale, f[6] = p3[0] * scale, f[7] = p3[1] * scale;
     }
-    T *y = (is_v ? v : k).at(r0 + i, h) + j * 8;
-    if constexpr (VEC) {
-      if constexpr (sizeof(T) == 2) store_vec<T, 8>(y, f);
-      else {
-        store_vec<T, 4>(y, f);
-        store_vec<T, 4>(y + 4, f + 4);
-      }
-    } else {
+    T *y = (is_v ? v : k).at(r0 + i, h) + j * E;
+    if constexpr (VEC) store_vec_once<T, E>(y, f);
+    else {
 #pragma unroll
-      for (int n = 0; n < 8; ++n) y[n] = (T)f[n];
+      for (int x = 0; x < E; ++x) y[x] = (T)f[x];
     }
   }
 }

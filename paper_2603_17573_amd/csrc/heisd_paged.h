@@ -259,6 +259,15 @@ __device__ __forceinline__ void store_vec(T *p, const float *x) {
   }
 }
 
+// The same past the caches' keeping: rows that are written once and are too many to stay.
+template <typename T, int V>
+__device__ __forceinline__ void store_vec_once(T *p, const float *x) {
+  typename VecOf<T, V>::type v;
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = (T)x[i];
+  __builtin_nontemporal_store(v, reinterpret_cast<typename VecOf<T, V>::type *>(p));
+}
+
 // (a, b) -> (a cos - b sin, b cos + a sin) for every pair of a row's heads.  The angle is position * frequency, reduced in 64
 // bits to a fraction of a turn (at position 100000 a 32-bit product is off by 1e-3 of a radian), then sine and cosine in 32.
 // They are the same for all heads of a row: a workgroup computes them once into LDS, then every thread turns V pairs at a

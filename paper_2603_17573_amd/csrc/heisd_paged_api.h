@@ -242,7 +242,7 @@ extern "C" int heisd_kv4_append(const heisd_kv4_desc *cache, const heisd_head_ro
 template <typename T, int HD>
 static void kv4_gather_launch(const Kv4Cache &c, const PagedBatch &b, const int32_t *cu_seq, int out_rows, const heisd_head_rows *k,
                               const heisd_head_rows *v, bool wide, hipStream_t st) {
-  const dim3 grid((out_rows + kGatherRows - 1) / kGatherRows, 2), block(256);
+  const dim3 grid((out_rows + kGatherRows<T> - 1) / kGatherRows<T>, (c.kv_heads + kGatherHeads - 1) / kGatherHeads, 2), block(256);
   if (wide) kv4_gather<T, HD, true><<<grid, block, 0, st>>>(c, b, cu_seq, out_rows, head_rows<T>(*k), head_rows<T>(*v));
   else kv4_gather<T, HD, false><<<grid, block, 0, st>>>(c, b, cu_seq, out_rows, head_rows<T>(*k), head_rows<T>(*v));
 }
