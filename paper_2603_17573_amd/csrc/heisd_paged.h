@@ -66,10 +66,8 @@ struct PlanArgs {
   int32_t *free_out, *cu_rows, *seq_len, *slot, *position, *cu_seq;
 };
 
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-
-// Inclusive sum over the workgroup, plus `carry`; carry becomes the total.  part: kPlanWaves values of LDS.
-template <typename N>
+// Inclusive sum over a workgroup of W waves, plus `carry`; carry becomes the total.  part: W values of LDS.
+template <int W, typename N>
 __device__ __forceinline__ N plan_scan(N v, N &carry, N *part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -77,17 +75,35 @@ __device__ __forceinline__ N plan_scan(N v, N &carry, N *part) {
     const N t = __shfl_up(v, o);
     if (lane >= o) v += t;
   }
+  if (W == 1) {
+    v += carry;
+    carry = __shfl(v, 63);
+    return v;
+  }
   if (lane == 63) part[wave] = v;
   __syncthreads();
   N before = carry, total = carry;
-#pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
-    if (w < wave) before += part[w];
-    total += part[w];
+#pragma unroll 4
+  for (int w = 0; w < W; ++w) {
+    const N x = part[w];
+    if (w < wave) before += x;
+    total += x;
   }
   __syncthreads();
   carry = total;
   return v + before;
+}
+
+// The first i of n values in LDS that do not decrease with end[i] > want (n: none).
+template <typename N>
+__device__ __forceinline__ int plan_owner(const N *end, int n, N want) {
+  int lo = 0;
+  while (lo < n) {
+    const int mid = (lo + n) >> 1;
+    if (end[mid] > want) n = mid;
+    else lo = mid + 1;
+  }
+  return lo;
 }
 
 // The slot and the position of row r, which is row `i` of request b's new rows.
@@ -105,54 +121,54 @@ __device__ __forceinline__ void plan_row(const PlanArgs &a, int r, int cached, i
 
 // One workgroup keeps the books: prefix sums over the requests decide who gets which free block.  Blocks that finished requests
 // give back go on top of the free ones first; a request that needs blocks then takes them from the top, first come, first
-// served.  Everything is a function of the inputs alone, so the outputs may be the inputs' own buffers.  SLOTS: the rows' slots
-// too (few rows); otherwise plan_slots fills them.  Sums of rows are held in 64 bits; those of blocks stay below 2^32 because a
-// request has at most 2^20 and the carries are clamped.
-template <bool SLOTS>
-__global__ __launch_bounds__(kPlanThreads) void plan_books(PlanArgs a) {
-  __shared__ uint32_t part[kPlanWaves];
-  __shared__ unsigned long long wide[kPlanWaves];
-  __shared__ int4 req[kPlanThreads];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// served.  Everything is a function of the inputs alone, so the outputs may be the inputs' own buffers.  A request per thread for the
+// sums; then a block (or a row) per thread, which finds its request by bisection in LDS: with a wave per request, each waited for its own
+// few blocks (512 requests: 17.7 us).  SLOTS: the rows' slots too; otherwise plan_slots fills them.  Sums of rows are held in 64 bits; those
+// of blocks stay below 2^32 because a request has at most 2^20 and the carries are clamped.  Bound by latency: three sums and four
+// round trips to memory.
+template <int W, bool SLOTS>
+__global__ __launch_bounds__(W * 64) void plan_books(PlanArgs a) {
+  constexpr int N = W * 64;
+  __shared__ uint32_t part[W], ends[N];
+  __shared__ unsigned long long wide[W], row_ends[N];
+  __shared__ int firsts[N], lengths[N];
+  const int tid = threadIdx.x;
   const uint32_t free0 = (uint32_t)min(max(a.free_in[0], 0), a.n_blocks);
   // finished requests' blocks
   uint32_t back_sum = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < a.batch; b0 += N) {
     const int b = b0 + tid;
     const int back = b < a.batch && a.cached[b] < 0 ? min(max(a.owned_in[b], 0), a.max_blocks) : 0;
     if (!__syncthreads_or(back)) continue;
-    const uint32_t end = plan_scan((uint32_t)back, back_sum, part);
-    back_sum = min(back_sum, (uint32_t)a.n_blocks);
-    req[tid] = make_int4((int)(end - back), back, 0, 0);
+    const uint32_t before = back_sum;
+    ends[tid] = plan_scan<W>((uint32_t)back, back_sum, part);
+    lengths[tid] = back;
     __syncthreads();
-    for (int i = wave; i < kPlanThreads && b0 + i < a.batch; i += kPlanWaves) {
-      const int4 q = req[i];
-      for (int j = lane; j < q.y; j += 64) {
-        const uint32_t to = free0 + (uint32_t)q.x + j;
-        if (to < (uint32_t)a.n_blocks) a.free_ids[to] = a.table[(long long)(b0 + i) * a.max_blocks + j];
-      }
+    for (uint32_t j = before + tid; j < back_sum && free0 + j < (uint32_t)a.n_blocks; j += N) {
+      const int i = plan_owner(ends, N, j);
+      a.free_ids[free0 + j] = a.table[(long long)(b0 + i) * a.max_blocks + (j - (ends[i] - lengths[i]))];
     }
+    back_sum = min(back_sum, (uint32_t)a.n_blocks);
     __syncthreads();
   }
   const uint32_t n_free = min(free0 + back_sum, (uint32_t)a.n_blocks);
   unsigned long long row_sum = 0, seq_sum = 0;
-  uint32_t need_sum = 0, granted = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
+  uint32_t need_sum = 0, granted = 0;               // blocks asked for, blocks given
+  const unsigned long long rows = (unsigned long long)a.rows;
+  for (int b0 = 0; b0 < a.batch; b0 += N) {
     const int b = b0 + tid;
     const bool in = b < a.batch;
     const int cached = in ? a.cached[b] : -1, fresh = in ? a.fresh[b] : 0;
     const int owned = in ? min(max(a.owned_in[b], 0), a.max_blocks) : 0;
-    const unsigned long long n = (unsigned long long)max(fresh, 0), rows = (unsigned long long)a.rows;
-    const unsigned long long row_end = plan_scan(n, row_sum, wide);
+    const unsigned long long n = (unsigned long long)max(fresh, 0);
+    const unsigned long long rows_before = row_sum, row_end = plan_scan<W>(n, row_sum, wide);
     const long long total = (long long)cached + fresh;
     bool live = in && cached >= 0 && fresh >= 0 && total <= (long long)a.max_blocks * a.block_size && row_end <= rows;
     int need = live ? max((int)((total + a.block_size - 1) / a.block_size) - owned, 0) : 0;
-    const uint32_t need_end = plan_scan((uint32_t)need, need_sum, part);
+    const uint32_t need_end = plan_scan<W>((uint32_t)need, need_sum, part);
     need_sum = min(need_sum, (uint32_t)a.n_blocks + 1);
     live = live && (need == 0 || need_end <= n_free);
-    if (!live) need = 0;
-    const unsigned long long seq_end = plan_scan(live ? (unsigned long long)total : 0ull, seq_sum, wide);
-    granted = max(granted, need ? need_end : 0u);
+    const unsigned long long seq_end = plan_scan<W>(live ? (unsigned long long)total : 0ull, seq_sum, wide);
     if (in) {
       if (b == 0) {
         a.cu_rows[0] = 0;
@@ -161,40 +177,39 @@ __global__ __launch_bounds__(kPlanThreads) void plan_books(PlanArgs a) {
       a.cu_rows[b + 1] = (int)min(row_end, rows);
       a.seq_len[b] = live ? (int)total : -1;
       if (a.cu_seq) a.cu_seq[b + 1] = (int)min(seq_end, 0x7FFFFFFFull);
+      a.owned_out[b] = cached < 0 ? 0 : owned + (live ? need : 0);
     }
-    req[tid] = make_int4((int)(n_free - (need_end - need)) - 1, need, owned, 0);   // the first block it takes, how many, from which entry
+    // requests are granted in order until one is refused: what they get is a run of the free blocks
+    ends[tid] = need_end;
+    firsts[tid] = need;
+    lengths[tid] = owned;
     __syncthreads();
-    for (int i = wave; i < kPlanThreads && b0 + i < a.batch; i += kPlanWaves) {
-      const int4 q = req[i];
-      for (int j = lane; j < q.y; j += 64) a.table[(long long)(b0 + i) * a.max_blocks + q.z + j] = a.free_ids[q.x - j];
+    const int last = plan_owner(ends, N, n_free);     // the first that gets nothing more
+    const uint32_t upto = last > 0 ? ends[last - 1] : granted;
+    for (uint32_t j = granted + tid; j < upto; j += N) {
+      const int i = plan_owner(ends, N, j);
+      a.table[(long long)(b0 + i) * a.max_blocks + lengths[i] + (j - (ends[i] - firsts[i]))] = a.free_ids[n_free - 1 - j];
     }
+    granted = max(granted, upto);
     __syncthreads();
-    if (in) a.owned_out[b] = cached < 0 ? 0 : owned + need;
     if (SLOTS) {
-      req[tid] = make_int4((int)min(row_end - n, rows), (int)min(row_end, rows), cached, live);
+      row_ends[tid] = row_end;
+      firsts[tid] = live ? cached : -1;
+      ends[tid] = (uint32_t)min(n, rows);
       __syncthreads();
-      for (int i = wave; i < kPlanThreads && b0 + i < a.batch; i += kPlanWaves) {
-        const int4 q = req[i];
-        for (int r = q.x + lane; r < q.y; r += 64) plan_row(a, r, q.z, r - q.x, b0 + i, q.w != 0);
+      for (unsigned long long r = rows_before + tid; r < min(row_sum, rows); r += N) {
+        const int i = plan_owner(row_ends, N, r);
+        plan_row(a, (int)r, firsts[i], (int)(r - (row_ends[i] - ends[i])), b0 + i, firsts[i] >= 0);
       }
       __syncthreads();
     }
   }
   if (SLOTS)
-    for (int r = (int)min(row_sum, (unsigned long long)a.rows) + tid; r < a.rows; r += kPlanThreads) {
+    for (int r = (int)min(row_sum, rows) + tid; r < a.rows; r += N) {
       a.slot[r] = -1;
       a.position[r] = -1;
     }
-  // the largest end of a granted run
-  __shared__ uint32_t most[kPlanWaves];
-#pragma unroll
-  for (int o = 32; o; o >>= 1) granted = max(granted, (uint32_t)__shfl_xor((int)granted, o));
-  if (lane == 0) most[wave] = granted;
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kPlanWaves; ++w) granted = max(granted, most[w]);
-    a.free_out[0] = (int)(n_free - granted);
-  }
+  if (tid == 0) a.free_out[0] = (int)(n_free - granted);
 }
 
 // Slots and positions of many rows: a wave finds the requests of its first and its last row, a lane those between.

@@ -51,11 +51,14 @@ extern "C" int heisd_paged_plan(const heisd_plan_desc *p, void *stream) {
                    p->block_table, p->free_ids, p->free_count_in, p->free_count_out, p->cu_rows, p->seq_len, p->slot, p->position, p->cu_seq};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (p->rows <= kPlanOneGroupRows) plan_books<true><<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
-  else {
-    plan_books<false><<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
+  const int most = std::max(p->batch, p->rows / 4);            // threads that have something to do
+  if (p->rows > kPlanOneGroupRows) {
+    if (p->batch <= 256) plan_books<4, false><<<dim3(1), dim3(256), 0, st>>>(a);
+    else plan_books<16, false><<<dim3(1), dim3(1024), 0, st>>>(a);
     plan_slots<<<dim3((p->rows + 255) / 256), dim3(256), 0, st>>>(a);
-  }
+  } else if (most <= 64) plan_books<1, true><<<dim3(1), dim3(64), 0, st>>>(a);
+  else if (most <= 256) plan_books<4, true><<<dim3(1), dim3(256), 0, st>>>(a);
+  else plan_books<16, true><<<dim3(1), dim3(1024), 0, st>>>(a);
   return launched(who);
 }
 
