@@ -368,12 +368,37 @@ extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_page
 
 // ---- attention of packed prompts -------------------------------------------------------------------------------------
 
-template <typename T, int HD, bool CAUSAL>
-static void prompt_launch(const PromptArgs &a, const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v,
-                          const heisd_head_rows *out, hipStream_t st) {
+// Two sets of waves share a workgroup's keys where the workgroups are few and the keys of a sequence (on average) many.  us, one set / two, one
+// causal sequence: 1024 keys, heads of 128, 36 workgroups 22.8 / 20.6, 288 25.2 / 23.3, 576 29.9 / 34.6, 1152 50.7 / 66.9; heads of 64, 288
+// 17.7 / 14.9, 576 19.0 / 20.5; 4096 keys, 264 77.6 / 63.0, 528 90.3 / 79.5; 276 keys, heads of 128, 12 9.9 / 10.8, 192 11.2 / 12.0.
+constexpr int64_t kPromptSplitGroups = 320, kPromptSplitKeys = 512;
+
+template <typename T, int HD, bool CAUSAL, int SPLIT>
+static hipError_t prompt_launch_one(const PromptArgs &a, const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v,
+                                    const heisd_head_rows *out, hipStream_t st) {
   const HeadRows<T> qi = head_rows<T>(*q), ki = head_rows<T>(*k), vi = head_rows<T>(*v);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs}, kc{ki.p, ki.rs, ki.hs}, vc{vi.p, vi.rs, vi.hs};
-  prompt_attend<T, HD, CAUSAL><<<dim3((unsigned)((int64_t)a.tiles * a.q_heads)), dim3(256), prompt_lds_bytes<HD>(), st>>>(qc, kc, vc, head_rows<T>(*out), a);
+  constexpr int lds = prompt_lds_bytes<HD>(SPLIT);
+  if constexpr (lds > 65536) {                       // above the usual limit of a workgroup, which is raised once per device
+    static std::atomic<bool> raised[kRetrieveMaxDevices];
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && (dev < 0 || dev >= kRetrieveMaxDevices)) e = hipErrorInvalidDevice;
+    if (e == hipSuccess && !raised[dev].load()) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attend<T, HD, CAUSAL, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e == hipSuccess) raised[dev].store(true);
+    }
+    if (e != hipSuccess) return e;
+  }
+  prompt_attend<T, HD, CAUSAL, SPLIT><<<dim3((unsigned)((int64_t)a.tiles * a.q_heads)), dim3(256 * SPLIT), lds, st>>>(qc, kc, vc, head_rows<T>(*out), a);
+  return hipSuccess;
+}
+
+template <typename T, int HD, bool CAUSAL>
+static hipError_t prompt_launch(const PromptArgs &a, const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v,
+                                const heisd_head_rows *out, hipStream_t st) {
+  const bool split = (int64_t)a.tiles * a.q_heads <= kPromptSplitGroups && a.k_rows >= kPromptSplitKeys * a.batch;
+  return split ? prompt_launch_one<T, HD, CAUSAL, 2>(a, q, k, v, out, st) : prompt_launch_one<T, HD, CAUSAL, 1>(a, q, k, v, out, st);
 }
 
 extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out,
@@ -404,12 +429,14 @@ extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head
                      scale < 0 ? 0x80008000u : 0u, lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  hipError_t e;
   if (q->dtype == HEISD_DTYPE_BF16) {
-    if (head_dim == 128) causal ? prompt_launch<__bf16, 128, true>(a, q, k, v, out, st) : prompt_launch<__bf16, 128, false>(a, q, k, v, out, st);
-    else causal ? prompt_launch<__bf16, 64, true>(a, q, k, v, out, st) : prompt_launch<__bf16, 64, false>(a, q, k, v, out, st);
+    if (head_dim == 128) e = causal ? prompt_launch<__bf16, 128, true>(a, q, k, v, out, st) : prompt_launch<__bf16, 128, false>(a, q, k, v, out, st);
+    else e = causal ? prompt_launch<__bf16, 64, true>(a, q, k, v, out, st) : prompt_launch<__bf16, 64, false>(a, q, k, v, out, st);
   } else {
-    if (head_dim == 128) causal ? prompt_launch<_Float16, 128, true>(a, q, k, v, out, st) : prompt_launch<_Float16, 128, false>(a, q, k, v, out, st);
-    else causal ? prompt_launch<_Float16, 64, true>(a, q, k, v, out, st) : prompt_launch<_Float16, 64, false>(a, q, k, v, out, st);
+    if (head_dim == 128) e = causal ? prompt_launch<_Float16, 128, true>(a, q, k, v, out, st) : prompt_launch<_Float16, 128, false>(a, q, k, v, out, st);
+    else e = causal ? prompt_launch<_Float16, 64, true>(a, q, k, v, out, st) : prompt_launch<_Float16, 64, false>(a, q, k, v, out, st);
   }
+  if (e != hipSuccess) return fail(nullptr, HEISD_EHIP, "%s: %s", who, hipGetErrorString(e));
   return launched(who);
 }

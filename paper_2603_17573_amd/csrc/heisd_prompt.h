@@ -32,8 +32,9 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t two) {
 constexpr int kPromptRows = 128, kPromptKeys = 64, kPromptWaves = 4;
 constexpr float kPromptLazy = 8.f;                  // the maximum is moved only when it grew by more than this (powers of two)
 
+// The join of two sets takes less than their buffers.
 template <int HD>
-constexpr int prompt_lds_bytes() { return 2 * 2 * kPromptKeys * HD * 2; }
+constexpr int prompt_lds_bytes(int split) { return split * 2 * 2 * kPromptKeys * HD * 2; }
 
 // Where the 16-byte pieces of an LDS row go: piece c of row r lies at c ^ prompt_swizzle(r).  A read of K takes the same piece of 16
 // rows at a time, a transposed read of V 64 bytes of four rows: both must meet all 64 banks once.  A row of 256 bytes is all banks, of
@@ -87,15 +88,17 @@ __device__ __forceinline__ void prompt_rows_plain(HeadRows<const T> q, HeadRows<
 // (with lane + 32), rescaling is a multiplication by the lane's own factor, and the probabilities are the second product's
 // operand as they stand: its eight summed indices per lane are two runs of four keys, and the transposed LDS read delivers V in just that
 // order.  K and V go to LDS by direct transfers, two buffers, one barrier per 64 keys; 16-byte pieces are permuted within a row by
-// the row's number so that neither read meets bank conflicts.
-template <typename T, int HD, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, HeadRows<const T> k, HeadRows<const T> v, HeadRows<T> out,
-                                                       PromptArgs a) {
+// the row's number so that neither read meets bank conflicts.  SPLIT 2: two such sets of four waves, each with buffers of its own, take every
+// other block of keys and are joined through LDS: half as many steps one after the other, for calls too small to fill the chip.
+template <typename T, int HD, bool CAUSAL, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, HD == 64 && SPLIT == 1 ? 3 : 2) void prompt_attend(HeadRows<const T> q, HeadRows<const T> k, HeadRows<const T> v,
+                                                                                             HeadRows<T> out, PromptArgs a) {
   typedef typename MatrixOf<T>::x8 x8;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int RB = HD * 2, CH = RB / 16, TILE = kPromptKeys * RB;                // bytes of a row, 16-byte pieces of it, a tile
   constexpr int NS = HD / 16, ND = HD / 32, NT = kPromptKeys / 32, NK = kPromptKeys / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), set = wave8 / kPromptWaves, wave = wave8 % kPromptWaves;
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const int head = kvh * a.group + rest % a.group, tile = a.tiles - 1 - rest / a.group;
   // which sequence: sequence i is given tiles floor(cu[i] / 128) + i and on, enough for any length
@@ -129,20 +132,25 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
   float m = -INFINITY, l[4] = {};                   // the row's maximum so far (powers of two), parts of its sum
   uint32_t odd = 0;
 
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+  const unsigned char *mine_lds = smem + set * 4 * TILE;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + set * 4 * TILE;
   constexpr int RP = 1024 / RB, NP = kPromptKeys / RP / kPromptWaves;              // rows per transfer, transfers per wave and matrix
   constexpr int STEP = RP * kPromptWaves;                                          // rows from one transfer of a wave to its next
   const int lane_row = wave * RP + lane / CH, lane_chunk = (lane % CH) ^ prompt_swizzle<CH>(lane_row);   // STEP is a multiple of 16
   const uint32_t k_off = (uint32_t)(lane_row * k.rs + lane_chunk * 8) * sizeof(T), v_off = (uint32_t)(lane_row * v.rs + lane_chunk * 8) * sizeof(T);
-  auto stage = [&](int block, int buf) {
+  const T *k_next = k.at(keys.begin + set * kPromptKeys, kvh), *v_next = v.at(keys.begin + set * kPromptKeys, kvh);   // the next transfer's first row
+  auto stage = [&](int block, int buf) __attribute__((always_inline)) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + buf * 2 * TILE + wave * 1024);
-    const long long row0 = keys.begin + block * kPromptKeys;
     if ((block + 1) * kPromptKeys <= n_keys) {
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
-        lds_dma16_s(k.at(row0 + n * STEP, kvh), k_off, to + n * kPromptWaves * 1024);
-        lds_dma16_s(v.at(row0 + n * STEP, kvh), v_off, to + TILE + n * kPromptWaves * 1024);
+        lds_dma16_s(k_next, k_off, to + n * kPromptWaves * 1024);
+        lds_dma16_s(v_next, v_off, to + TILE + n * kPromptWaves * 1024);
+        k_next += STEP * k.rs;
+        v_next += STEP * v.rs;
       }
+      k_next += (SPLIT - 1) * kPromptKeys * k.rs;
+      v_next += (SPLIT - 1) * kPromptKeys * v.rs;
     } else {                                        // past the end: the last row again, masked
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
@@ -166,23 +174,24 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
 
   const int n_blocks = (n_keys + kPromptKeys - 1) / kPromptKeys;
   wait_vmcnt_all();
-  if (n_blocks > 0) stage(0, 0);
-  for (int blk = 0; blk < n_blocks; ++blk) {
-    const int buf = blk & 1, base = blk * kPromptKeys;
+  if (set < n_blocks) stage(set, 0);
+  for (int step = 0; step * SPLIT < n_blocks; ++step) {
+    const int blk = step * SPLIT + set, buf = step & 1, base = blk * kPromptKeys;
     wait_vmcnt<0>();
     __syncthreads();
-    if (blk + 1 < n_blocks) stage(blk + 1, buf ^ 1);
-    if (base >= some_see) continue;
-    const unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE;
+    if (blk + SPLIT < n_blocks) stage(blk + SPLIT, buf ^ 1);
+    if (base >= some_see) continue;                 // some_see is at most n_keys: a set's last block may not be there
+    const unsigned char *kt = mine_lds + buf * 2 * TILE, *vt = kt + TILE;
     f32x16 s[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-      for (int n = 0; n < NS; ++n)
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
         s[t] = MatrixOf<T>::mul(*reinterpret_cast<const x8 *>(kt + k_at[n] + t * 32 * RB), qf[n], s[t]);
-    }
     if (base + kPromptKeys > all_see) {             // some row must not see some of these keys
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -221,9 +230,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
         pf[2 * t + (e >> 3)][e & 7] = (T)p;
       }
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int n = 0; n < NK; ++n)
 #pragma unroll
-      for (int n = 0; n < NK; ++n) {
+      for (int d = 0; d < ND; ++d) {
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][0] + n * 16 * RB));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][1] + n * 16 * RB));
@@ -231,6 +240,31 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(HeadRows<const T> q, Hea
         const x8 vf = __builtin_bit_cast(x8, both);
         acc[d] = MatrixOf<T>::mul(vf, pf[n], acc[d]);
       }
+  }
+  if constexpr (SPLIT == 2) {                       // the second set's sums through LDS, a register after the other
+    __syncthreads();
+    float *to = reinterpret_cast<float *>(smem) + wave * 64 + lane;
+    if (set) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) to[(d * 16 + e) * 256] = acc[d][e];
+      to[ND * 16 * 256] = m;
+      to[(ND * 16 + 1) * 256] = (l[0] + l[1]) + (l[2] + l[3]);
+      to[(ND * 16 + 2) * 256] = __uint_as_float(odd);
+    }
+    __syncthreads();
+    if (set) return;
+    const float m2 = to[ND * 16 * 256], next = fmaxf(m, m2);
+    const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next), by2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - next);
+    m = next;
+    l[0] = ((l[0] + l[1]) + (l[2] + l[3])) * by + to[(ND * 16 + 1) * 256] * by2;
+    l[1] = l[2] = l[3] = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] = acc[d][e] * by + to[(d * 16 + e) * 256] * by2;
+    odd |= __float_as_uint(to[(ND * 16 + 2) * 256]);
   }
   if (my_rows == 0) return;
   if (__ballot(odd != 0)) {

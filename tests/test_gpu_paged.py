@@ -472,6 +472,45 @@ def test_attention_of_long_contexts(P):
         check_attend(c, q, out, lse, [0, 1, 2, 3, 4], ref.held(host(k)), ref.held(host(v)), 0.088, "bf16")
 
 
+@pytest.mark.parametrize("batch,heads,head_dim", [(64, (2, 1), 64), (65, (4, 2), 128), (130, (2, 2), 64), (333, (1, 1), 64)])
+def test_attention_of_many_requests(P, batch, heads, head_dim):
+    """More requests than a wave looks at together; some without rows, some without tokens."""
+    rng = np.random.default_rng(batch)
+    total = [int(x) for x in rng.integers(0, 300, batch)]
+    new = [int(min(x, max(t, 1))) for x, t in zip(rng.integers(0, 3, batch), total)]
+    c = Cache(P, rng, total, heads[1], head_dim, 16)
+    k, v = (randn(rng, (sum(total), heads[1], head_dim), "bf16") for _ in range(2))
+    c.write(P, k, v)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    q = randn(rng, (int(cu[-1]), heads[0], head_dim), "bf16")
+    out, lse = attend(P, c, q, cu, 2, 300, 0.1)
+    check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.1, "bf16")
+
+
+def test_attention_of_long_runs(P):
+    """So much work that a workgroup has more than 4096 tokens of one request and head."""
+    rng = np.random.default_rng(0)
+    total, heads, hd = [8192, 8000, 8191, 4097, 8192, 8100, 8192, 8192], 64, 64
+    c = Cache(P, rng, total, heads, hd, 64)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn((sum(total), heads, hd), generator=g, device=DEV).bfloat16() for _ in range(2))
+    c.write(P, k, v)
+    kk, vv = c.read(P)
+    q = torch.randn((8, heads, hd), generator=g, device=DEV).bfloat16()
+    out, lse = attend(P, c, q, list(range(9)), 1, 8192, 0.125)
+    for i in range(8):
+        rows = slice(int(c.cu_seq[i]), int(c.cu_seq[i + 1]))
+        for h in (0, 17, 63):
+            x, y = kk[rows, h].double(), vv[rows, h].double()
+            s = x @ q[i, h].double() * 0.125
+            w = torch.softmax(s, 0)
+            want, mean = w @ y, w @ y.abs()
+            size = (x.abs() @ q[i, h].double().abs()).max() * 0.125
+            tol = tolerance("bf16", 2.0 ** -8, 0.0, hd, total[i], host(want), host(mean), 0.0, np.asarray(size.item())[None])
+            assert np.all(np.abs(host(out[i, h]) - host(want)) <= tol.reshape(-1))
+            assert abs(lse[i, h].item() - torch.logsumexp(s, 0).item()) <= lse_tolerance(hd, total[i], lse[i, h].item(), size.item())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_attention_with_holes(P, dtype):
     """Blocks that are not there, requests left out (-1), more rows than tokens (rows that see nothing), longer than max_seq."""
@@ -623,6 +662,22 @@ def test_prompt_attention(P, causal, dtype, new, past, heads, head_dim):
     assert np.all(host(out)[cu_q[-1]:] == 7) and np.all(host(lse)[cu_q[-1]:] == 7)
     again, _ = prompt(P, q, k, v, cu_q, cu_k, scale, causal, want_lse=False)
     assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("head_dim,causal", [(64, True), (64, False), (128, True), (128, False)])
+def test_prompt_attention_of_large_batches(P, dtype, head_dim, causal):
+    """A batch with so many (empty) sequences that a workgroup is one set of waves, and the same rows in a small one."""
+    rng = np.random.default_rng(head_dim)
+    new, past = [129, 1, 300, 0, 70], [0, 333, 64, 5, 500]
+    cu_q, cu_k = np.concatenate([[0], np.cumsum(new)]), np.concatenate([[0], np.cumsum(np.add(new, past))])
+    q = randn(rng, (500, 4, head_dim), dtype)
+    k, v = (randn(rng, (int(cu_k[-1]), 2, head_dim), dtype) for _ in range(2))
+    v[129 + 334 + 64 + 290, 0, 1] = math.inf                           # masked for most rows of the third
+    for empty in (0, 400):
+        a, b = (np.concatenate([x, np.full(empty, x[-1])]) for x in (cu_q, cu_k))
+        out, lse = prompt(P, q, k, v, a, b, head_dim ** -0.5, causal)
+        check_prompt(q, k, v, out, lse, cu_q, cu_k, head_dim ** -0.5, causal, dtype)
 
 
 def test_prompt_attention_many_short_sequences(P):

@@ -165,3 +165,15 @@ def test_torch_side_checks(P):
         P.make_kv4_desc(torch.zeros(100, dtype=torch.uint8), 16, 1, 64)
     with pytest.raises(ValueError):
         P.rope_table(P.make_rope_desc(63), "cpu")
+
+
+def test_the_two_references_of_the_format_agree():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((40, 3, 64)) * np.exp(4 * rng.standard_normal((40, 3, 1)))
+    x[0, 0, :32] = 0
+    x[1, 0, :32] = [0.25, -0.75, 1.25, 1.75, -2.5, 3.5, 5, 6] * 4
+    x[2, 0, :32] = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -6.0001] * 4) * 2.0 ** -130
+    x[3, 1, 40], x[3, 2, 0] = np.inf, np.nan
+    x[4, 0, 5] = 3 * 2.0 ** 127
+    assert np.array_equal(ref.held(x), ref.held_plain(x), equal_nan=True)
+    assert np.array_equal(np.signbit(ref.held(x[:3])), np.signbit(ref.held_plain(x[:3])))
