@@ -393,6 +393,64 @@ def run_retrieve_mode(args):
     print(json.dumps(line))
 
 
+def run_paged_mode(args):
+    """--mode paged: what one decode step of 64 requests with ragged contexts does besides its projections, on PagedCache:
+    block tables once, then in each of 32 layers the rotation, the append and the attention over the 4-bit cache (32 query and
+    8 key heads of 128), captured into one HIP graph."""
+    import random
+    import torch
+    import paper_2603_17573_amd as P
+    assert torch.cuda.is_available(), "bench.py needs a GPU"
+    dev, layers, batch, q_heads, kv_heads, hd, block, most = "cuda:0", 32, 64, 32, 8, 128, 64, 4096
+    rng = random.Random(1)
+    lens = [rng.randrange(256, most - 64) for _ in range(batch)]
+    n_blocks = sum(-(-(n + 64) // block) for n in lens) + batch
+    i32 = dict(dtype=torch.int32, device=dev)
+    c = P.PagedCache(layers, q_heads, kv_heads, hd, batch, most, sum(lens), n_blocks, block, device=dev)
+    c.begin(torch.zeros(batch, **i32), torch.tensor(lens, **i32), sum(lens))
+    for layer in range(layers):
+        k, v = (torch.randn((sum(lens), kv_heads, hd), device=dev, dtype=torch.bfloat16) for _ in range(2))
+        c.append(layer, k, v)
+    del k, v
+    cached, one = torch.tensor(lens, **i32), torch.ones(batch, **i32)
+    q, k, v = (torch.randn((batch, n, hd), device=dev, dtype=torch.bfloat16) for n in (q_heads, kv_heads, kv_heads))
+    out = torch.empty_like(q)
+
+    def step():
+        c.begin(cached, one, batch)
+        for layer in range(layers):
+            c.rotate(q, k)
+            c.append(layer, k, v)
+            c.attend(layer, q, out=out)
+
+    step()
+    torch.cuda.synchronize()
+    assert bool((c.seq_len == cached + 1).all()) and bool(torch.isfinite(out).all())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(args.warmup):
+        graph.replay()
+    torch.cuda.synchronize()
+    ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    ev0.record()
+    for _ in range(args.steps):
+        graph.replay()
+    ev1.record()
+    torch.cuda.synchronize()
+    ms = ev0.elapsed_time(ev1) / args.steps
+    nbytes = layers * (sum(lens) + batch) * kv_heads * (hd + hd // 16)
+    print(json.dumps({
+        "metric": "decode steps/s without projections (%d layers, %d requests, 4-bit paged cache)" % (layers, batch),
+        "value": round(1000.0 / ms, 1), "unit": "steps/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "ms_per_step": round(ms, 4), "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
+        "dtype": "bf16 rows, 4-bit cache", "data": "synthetic",
+        "config": {"requests": batch, "cached_tokens": sum(lens), "q_heads": q_heads, "kv_heads": kv_heads, "head_dim": hd, "block": block,
+                   "launches_per_step": 1 + 4 * layers},
+        "roofline": {"kernel": "the whole step", "bound": "hbm", "achieved": round(nbytes / (ms * 1e-3) / 1e9, 1), "peak": HBM_PEAK / 1e9,
+                     "unit": "GB/s", "frac": round(nbytes / (ms * 1e-3) / HBM_PEAK, 4), "bytes_per_launch": nbytes}}))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -417,9 +475,10 @@ def main():
                          "sequence-wise draft tree (paper Sec. 4.2); 0 = the linear step")
     ap.add_argument("--prefill-chunks", type=int, default=1, choices=[1, 2],
                     help="--mode prefill: 1 = visual embeddings and prompt ids in one call (default), 2 = one call each")
-    ap.add_argument("--mode", default="verify", choices=["verify", "decode", "prefill", "skip", "retrieve", "readbw"],
+    ap.add_argument("--mode", default="verify", choices=["verify", "decode", "prefill", "skip", "retrieve", "readbw", "paged"],
                     help="verify (default): the verify step; decode: one autoregressive decode step; prefill: the "
-                         "workload's prefix from an empty cache, in chunks")
+                         "workload's prefix from an empty cache, in chunks; paged: rotation, append and attention of a "
+                         "decode step of many requests over the 4-bit cache")
     args = ap.parse_args()
     if args.gpus != 1:
         print("bench.py: this build runs the verify step on ONE GPU (episodes would shard by batch "
@@ -435,6 +494,8 @@ def main():
             return run_retrieve_mode(args)
         if args.mode == "readbw":
             return run_readbw_mode(args)
+        if args.mode == "paged":
+            return run_paged_mode(args)
         return run_skip_mode(args) if args.mode == "skip" else run_aux_mode(args)
 
     import numpy as np
