@@ -268,8 +268,9 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // 16): scores^T = K q^T (tokens are rows), out^T = V^T p^T.  A lane holds the scores of one column and four tokens of each tile, which are
 // its summed indices of the second product, so the probabilities never leave their lane.  Four waves take pairs of tiles in turn,
 // each with a running maximum and sum of its own, joined through LDS at the end of a segment; what a workgroup has of a segment that it
-// shares with others goes to kv4_join.  TERMS 2: queries and probabilities enter as a bf16 and a bf16 remainder (fp16 rows, whose
-// 11 bits a bf16 does not hold); 1: as one bf16, rounding the probabilities by 2^-9.
+// shares with others goes to kv4_join.  A probability enters as a bf16 and a bf16 remainder: one bf16 alone (off by 2^-9, and with few
+// large probabilities nothing averages that out) made the results of single tokens 1.4 times as inexact as their own rounding does, for 3 % of the
+// time (59.9 against 62.1 us with 64 contexts of 256 to 8191 tokens).  TERMS 2: so do the queries (fp16 rows, whose 11 bits a bf16 does not hold).
 template <typename T, int HD, int CT, int TERMS>
 __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
   constexpr int W = HD / 32, ND = HD / 16, KJ = HD / 32;        // code dwords, tiles of channels, products per score tile
@@ -279,8 +280,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
   static_assert(MINE >= 16 * LD * 4 && MINE % 16 == 0, "the sums take the ring's place");
   __shared__ __attribute__((aligned(16))) unsigned char s_mine[4][MINE];
   __shared__ float s_m[4][16], s_l[4][16];
-  __shared__ long long s_start[64];                             // every wave writes the same values before it reads them
-  __shared__ int4 s_req[64];
+  __shared__ long long s_start[4][64];                          // a wave's own: on its way to a later request another may be behind
+  __shared__ int4 s_req[4][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int bs = c.block_size;
 
@@ -298,8 +299,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
       if (lane >= o) start += t;
     }
     end = before + lane_value64(start, 63);
-    s_start[lane] = start + before - r.work;
-    s_req[lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
+    s_start[wave][lane] = start + before - r.work;
+    s_req[wave][lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
   };
   requests(0);
   long long all = end;
@@ -307,16 +308,17 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
   const long long per = kv4_run(all, gridDim.x), run0 = blockIdx.x * per, run1 = min(run0 + per, all);
 
   for (long long at = run0; at < run1;) {
-    while (at >= end) {
+    while (at >= end && first + 64 < b.batch) {
       first += 64;
       requests(end);
     }
-    const int local = 63 - __clzll(__ballot(s_start[lane] <= at));      // the last of those that begin here has the work
+    if (at >= end) break;                                       // not reached while the lengths stay as they are
+    const int local = 63 - __clzll(__ballot(s_start[wave][lane] <= at));      // the last of those that begin here has the work
     const int req = first + local;
-    const int4 rq = s_req[local];
+    const int4 rq = s_req[wave][local];
     const Span rows{__builtin_amdgcn_readfirstlane(rq.x), __builtin_amdgcn_readfirstlane(rq.y)};
     const int seq = __builtin_amdgcn_readfirstlane(rq.z), units = __builtin_amdgcn_readfirstlane(rq.w);
-    const long long in_req = at - lane_value64(s_start[lane], local);
+    const long long in_req = at - lane_value64(s_start[wave][lane], local);
     const int segment = __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
     const int u0 = __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
     const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
@@ -447,7 +449,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
           if (large || gone) ve[e >> 2] &= ~mask;
         }
       }
-      bf16x8 pf[CT][TERMS];
+      bf16x8 pf[CT][2];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         float top = x[ct][0];
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
           const float pr = exp2_fast(__builtin_fmaf(x[ct][e], a.scale_log2, -use));
           l[ct] += pr;
           pf[ct][0][e] = (__bf16)pr;
-          if constexpr (TERMS == 2) pf[ct][1][e] = (__bf16)(pr - (float)pf[ct][0][e]);
+          pf[ct][1][e] = (__bf16)(pr - (float)pf[ct][0][e]);
         }
       }
       float vs[2][4];
@@ -503,7 +505,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int e = 0; e < TERMS; ++e) {
+          for (int e = 0; e < 2; ++e) {
             acc[ct][2 * dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[ct][e], acc[ct][2 * dd], 0, 0, 0);
             acc[ct][2 * dd + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[ct][e], acc[ct][2 * dd + 1], 0, 0, 0);
           }

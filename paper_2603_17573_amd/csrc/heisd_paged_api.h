@@ -304,7 +304,7 @@ struct Kv4Plan {
 static int kv4_attention_sizes_ok(const char *who, int32_t kv_heads, int32_t q_heads, int32_t rows, int32_t max_q, int32_t max_seq) {
   if (q_heads < 1 || q_heads > 512 || q_heads % kv_heads)
     return fail(nullptr, HEISD_EINVAL, "%s: %d query heads over %d key heads", who, q_heads, kv_heads);
-  if (rows < 0 || max_q < 1 || max_seq < 1 || max_seq > (1 << 24) || (int64_t)rows * q_heads > 0x7FFFFFFF)
+  if (rows < 0 || max_q < 1 || max_seq < 1 || max_seq > (1 << 24) || (int64_t)rows * q_heads > 0x7FFFFF00)
     return fail(nullptr, HEISD_EINVAL, "%s: rows=%d max_q=%d max_seq=%d (1..2^24)", who, rows, max_q, max_seq);
   return HEISD_OK;
 }

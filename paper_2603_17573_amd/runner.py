@@ -257,7 +257,7 @@ class PagedCache:
             desc = rope if rope is not None else make_rope_desc(head_dim)
             self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]
             self.turns, self.magnitude = rope_table(desc, self.device)
-        self.rows = 0
+        self.rows, self._kv = 0, []
 
     def _call(self, fn, *args):
         with torch.cuda.device(self.device):
@@ -316,9 +316,10 @@ class PagedCache:
         cached rows are read back once and multiplied as a prompt's."""
         out = torch.empty_like(q) if out is None else out
         hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
-        if getattr(self, "_kv", None) is None or self._kv.shape[1] < total or self._kv.dtype != q.dtype:
-            self._kv = torch.empty((2, total, self.kv_heads, self.head_dim), dtype=q.dtype, device=self.device)
-        hk, hv = head_rows(self._kv[0]), head_rows(self._kv[1])
+        if not self._kv or self._kv[-1].shape[1] < total or self._kv[-1].dtype != q.dtype:
+            # a captured graph may still read and write the smaller ones: they stay
+            self._kv.append(torch.empty((2, total, self.kv_heads, self.head_dim), dtype=q.dtype, device=self.device))
+        hk, hv = head_rows(self._kv[-1][0]), head_rows(self._kv[-1][1])
         self._call(B.heisd_kv4_gather, self.descs[layer], self.batch, self.cu_seq.data_ptr(), total, hk, hv)
         self._call(B.heisd_prompt_attention, hq, hk, hv, ho, lse.data_ptr() if lse is not None else None, self.cu_rows.data_ptr(),
                    self.cu_seq.data_ptr(), self.table.shape[0], self.rows, total, self.head_dim,

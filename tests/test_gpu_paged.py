@@ -5,8 +5,8 @@ Tolerances.  A rounding to a dtype is off by at most half a step, u = eps / 2 of
 Whole numbers and what a 4-bit cache holds are exact.  Rotations: u of the result, and in fp32 two products, a sum (2^-24 each)
 and sine and cosine to 2^-22.  Attention: a score is a sum of head_dim products in fp32, each addition off by 2^-24 of what has been summed, so
 off by at most S = (head_dim + 8) 2^-24 * scale * sum |q_i k_i|, which makes a probability relatively off by exp(2 S) - 1 (its own
-score and the normalising sum); the probability's own rounding P adds u(bf16) (one bf16) or 2^-16 (a bf16 and a remainder of a
-bf16) or u(fp16), where fp16 probabilities below 2^-14 are off by 2^-25 at most; the sums of the output over t tokens
+score and the normalising sum); the probability's own rounding P adds 2^-16 (a bf16 and a remainder of a bf16: over the cache) or
+the rows' own u (in prompts), where fp16 probabilities below 2^-14 are off by 2^-25 at most; the sums of the output over t tokens
 add (t + 64) 2^-24.  All of these multiply the weighted mean of |v|; the result is rounded once."""
 import math
 
@@ -408,7 +408,7 @@ def check_attend(c, q, out, lse, cu_rows, k, v, scale, dtype, seq=None, gone=Non
     """k, v: what the cache holds, packed by request [sum(total), kv_heads, head_dim]."""
     seq = c.total if seq is None else seq
     q64, out, lse = host(q), host(out), host(lse)
-    p = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -16
+    p = 2.0 ** -16
     for i, n in enumerate(seq):
         a, b = cu_rows[i], cu_rows[i + 1]
         kk, vv = (x[c.cu_seq[i]:c.cu_seq[i] + max(n, 0)] for x in (k, v))
@@ -430,7 +430,7 @@ def check_attend_rows(q, out, k, v, scale, dtype, chunk=False):
     """The n rows of one request over all that it has cached; chunk: by way of packed rows in the queries' dtype."""
     n, t = q.shape[0], k.shape[0]
     want, _, mean, flat, size = ref.attention(q, k, v, [t - n + i + 1 for i in range(n)], scale)
-    p, tiny = (2.0 ** -8, 0.0) if dtype == "bf16" else (2.0 ** -11, 2.0 ** -25) if chunk else (2.0 ** -16, 0.0)
+    p, tiny = (2.0 ** -16, 0.0) if not chunk else (2.0 ** -8, 0.0) if dtype == "bf16" else (2.0 ** -11, 2.0 ** -25)
     over = np.abs(out - want) - tolerance(dtype, p, tiny, q.shape[2], t, want, mean, flat, size)
     assert over.max() <= 0, (chunk, n, t, float(over.max()), np.argwhere(over > 0)[:4].tolist())
 
@@ -506,7 +506,7 @@ def test_attention_of_long_runs(P):
             w = torch.softmax(s, 0)
             want, mean = w @ y, w @ y.abs()
             size = (x.abs() @ q[i, h].double().abs()).max() * 0.125
-            tol = tolerance("bf16", 2.0 ** -8, 0.0, hd, total[i], host(want), host(mean), 0.0, np.asarray(size.item())[None])
+            tol = tolerance("bf16", 2.0 ** -16, 0.0, hd, total[i], host(want), host(mean), 0.0, np.asarray(size.item())[None])
             assert np.all(np.abs(host(out[i, h]) - host(want)) <= tol.reshape(-1))
             assert abs(lse[i, h].item() - torch.logsumexp(s, 0).item()) <= lse_tolerance(hd, total[i], lse[i, h].item(), size.item())
 
