@@ -57,7 +57,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 }
 
 // Four lanes share a group of 32 values, 8 each (16 bytes per access).  gridDim.y: keys and values.  Reads every row once and
-// writes 17/64 of the bytes of a bf16 row; bound by memory.  VEC: rows are aligned for wide loads.
+// writes 17/64 of the bytes of a bf16 row; bound by memory (20963 rows of 8 heads of 128: 107 MB in 20 us).  VEC: rows are aligned
+// for wide loads.
 template <typename T, int HD, bool VEC>
 __global__ __launch_bounds__(256) void kv4_append(Kv4Cache c, HeadRows<const T> k, HeadRows<const T> v, const int32_t *slot,
                                                   int rows, int per_group, FastDiv by_row) {
@@ -126,7 +127,8 @@ constexpr int kGatherHeads = 4;
 
 // Some packed rows and heads per workgroup, head by head: the rows of a block that follow each other lie together in the cache.
 // A thread requests its values of all heads before it converts the first.  Rows of a block that the pool does not have are
-// zero.  Bound by memory, most of it the rows that are written.
+// zero.  Bound by memory, most of it the rows that are written: 4280 rows of 32 heads of 128 into fp32 (159 MB) take 26 us.  One group of all heads
+// per sixteen rows, stores of half lines in fp32 and ordinary ones took 55.
 template <typename T, int HD, bool VEC>
 __global__ __launch_bounds__(256) void kv4_gather(Kv4Cache c, PagedBatch b, const int32_t *cu_seq, int out_rows,
                                                   HeadRows<T> k, HeadRows<T> v) {
@@ -205,7 +207,9 @@ struct Kv4Pair {
 };
 // Where two tiles lie in LDS: key codes of both, value codes of both, then 64 bytes each of key exponents and of value exponents.  With heads of 128 the
 // pieces of a tile's key codes are in the order of the lanes that read them.
-constexpr int kKv4Ring = 2;                         // pairs of tiles on their way per wave
+// Two pairs are on their way per wave, none of them in registers (a pair held there while the next was fetched: 66 us against 59.5 with 64
+// long contexts).  What bounds the kernel then is memory: 246 MB in 50 us when most of them are in the last cache, 57 when none is.
+constexpr int kKv4Ring = 2;
 template <int HD>
 struct Kv4Slot {
   static constexpr int TILE = 16 * HD / 2, V = 2 * TILE, EXP = 4 * TILE, BYTES = EXP + 256;
@@ -222,6 +226,8 @@ struct Kv4Attend {
 
 // Work is counted in units: 128 tokens (a pair of tiles for each wave) of one request, key head and group of columns - a segment is all
 // units of such a three.  Every workgroup takes an equal run of the units of the whole call, whatever the requests' lengths are.
+// A workgroup per chunk of 1024 tokens instead: 71 us with 64 contexts of 256 to 8191 tokens, where runs took 62 (the last chunks left most of
+// the chip idle, and every chunk begins with three round trips to memory).
 constexpr int kKv4Unit = 128;
 
 // Workgroups of 256 threads that the registers of a compute unit hold: queries of two terms or two column tiles need more of them.

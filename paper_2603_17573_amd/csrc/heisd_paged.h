@@ -125,7 +125,8 @@ __device__ __forceinline__ void plan_row(const PlanArgs &a, int r, int cached, i
 // sums; then a block (or a row) per thread, which finds its request by bisection in LDS: with a wave per request, each waited for its own
 // few blocks (512 requests: 17.7 us).  SLOTS: the rows' slots too; otherwise plan_slots fills them.  Sums of rows are held in 64 bits; those
 // of blocks stay below 2^32 because a request has at most 2^20 and the carries are clamped.  Bound by latency: three sums and four
-// round trips to memory.
+// round trips to memory, 3.9 us for one request on one wave (10.7 on sixteen), 10.2 for 512 requests of which a quarter are prompts; plan_slots
+// takes 4.0 more for their 56260 rows.
 template <int W, bool SLOTS>
 __global__ __launch_bounds__(W * 64) void plan_books(PlanArgs a) {
   constexpr int N = W * 64;
@@ -286,7 +287,8 @@ __device__ __forceinline__ void store_vec_once(T *p, const float *x) {
 // (a, b) -> (a cos - b sin, b cos + a sin) for every pair of a row's heads.  The angle is position * frequency, reduced in 64
 // bits to a fraction of a turn (at position 100000 a 32-bit product is off by 1e-3 of a radian), then sine and cosine in 32.
 // They are the same for all heads of a row: a workgroup computes them once into LDS, then every thread turns V pairs at a
-// time, 16 bytes per access.  Bound by memory: 2 * heads * head_dim values per row.
+// time, 16 bytes per access.  Bound by memory: 2 * heads * head_dim values per row; 16384 rows of 40 heads of 128 in bf16 (336 MB) take
+// 64 us, 5.3 TB/s, the rate of a large copy.
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(kRopeThreads) void rope_rows(RopeArgs a, HeadRows<const T> q, HeadRows<T> q_out, HeadRows<const T> k,
                                                          HeadRows<T> k_out) {
