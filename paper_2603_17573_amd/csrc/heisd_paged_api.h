@@ -32,8 +32,9 @@ static int launched(const char *who) {
 
 // ---- block tables, slots and positions ---------------------------------------------------------------------------
 
-// Up to this many packed rows the one workgroup that keeps the books writes the slots as well.
-constexpr int kPlanOneGroupRows = 4096;
+// Up to this many packed rows the one workgroup that keeps the books writes the slots as well.  us, one launch / two: 8 requests, 1024 rows
+// 8.1 / 9.4, 4096 12.2 / 9.9, 8192 16.4 / 9.7; 64 requests, 1024 8.2 / 9.6, 4096 12.1 / 9.7; 512 requests, 4096 12.5 / 13.1, 8192 16.7 / 13.0.
+constexpr int kPlanOneGroupRows = 2048;
 
 extern "C" int heisd_paged_plan(const heisd_plan_desc *p, void *stream) {
   const char *who = "paged_plan";
@@ -281,7 +282,10 @@ extern "C" int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_b
 }
 
 // How a call is cut: column tiles per workgroup, and workgroups: as many as are resident at once (kv4_per_unit), fewer where there is
-// little to do - four units of 128 tokens for each, counted with the largest lengths.
+// little to do - four units of 128 tokens for each, counted with the largest lengths (one context of 4000 tokens, 8 key heads, 1 / 2 / 4 / 8 / 16
+// units each: 13.4 / 11.9 / 12.4 / 15.6 / 22.1 us; eight of them: 20.2 / 20.0 / 16.5 / 17.4 / 22.9).  More than 16 columns are two tiles, for which the
+// cache is read once, where the work fills the grid even so: drafts of seven, 4 query heads per key head, one tile / two: 64 contexts of 256 to 4000
+// tokens 64.3 / 62.4 us, 16 of up to 2000 30.4 / 26.8, one of 4000 15.5 / 21.0.
 constexpr int kKv4Units = 256;                       // compute units that the grid is made for (a fixed number: results do not depend on the device)
 struct Kv4Plan {
   int col_tiles, segments;
@@ -291,8 +295,8 @@ struct Kv4Plan {
     return (int)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, kv4_per_unit(head_dim, col_tiles, terms) * kKv4Units));
   }
   Kv4Plan(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, int64_t head_dim) {
-    const int64_t cols = max_q * group;
-    col_tiles = cols > 16 ? 2 : 1;
+    const int64_t cols = max_q * group, lengths = (max_seq + 4 * kKv4Unit - 1) / (4 * kKv4Unit);
+    col_tiles = cols > 16 && batch * kv_heads * ((cols + 15) / 16) * lengths >= kv4_per_unit((int)head_dim, 1, 1) * kKv4Units ? 2 : 1;
     segments = (int)std::min<int64_t>(kv_heads * ((cols + 16 * col_tiles - 1) / (16 * col_tiles)), 65535);
     units = batch * segments * ((max_seq + kKv4Unit - 1) / kKv4Unit);
     const size_t rows = (size_t)2 * groups(1, (int)head_dim) * 16 * col_tiles;       // (one term: the larger grid)

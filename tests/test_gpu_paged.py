@@ -453,8 +453,10 @@ def test_attention_over_the_cache(P, dtype, total, new, heads, head_dim, block):
     assert np.all(host(out)[cu[-1]:] == 7) and np.all(host(lse)[cu[-1]:] == 7)
     again, _ = attend(P, c, q, cu, max(new), max(total), scale, want_lse=False)
     assert torch.equal(again, out)
-    more, _ = attend(P, c, q, cu, 1, 4096, scale)                      # other bounds cut the work otherwise
-    check_attend(c, q, more, lse, cu, ref.held(host(k)), ref.held(host(v)), scale, dtype)
+    # other bounds cut the work otherwise; with the larger ones a workgroup takes 32 columns
+    for max_q, max_seq in ((1, 4096), (32, 1 << 20)):
+        more, lse = attend(P, c, q, cu, max_q, max_seq, scale)
+        check_attend(c, q, more, lse, cu, ref.held(host(k)), ref.held(host(v)), scale, dtype)
 
 
 def test_attention_of_long_contexts(P):
@@ -483,8 +485,9 @@ def test_attention_of_many_requests(P, batch, heads, head_dim):
     c.write(P, k, v)
     cu = np.concatenate([[0], np.cumsum(new)])
     q = randn(rng, (int(cu[-1]), heads[0], head_dim), "bf16")
-    out, lse = attend(P, c, q, cu, 2, 300, 0.1)
-    check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.1, "bf16")
+    for max_q in (2, 32):
+        out, lse = attend(P, c, q, cu, max_q, 300, 0.1)
+        check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.1, "bf16")
 
 
 def test_attention_of_long_runs(P):
@@ -529,8 +532,9 @@ def test_attention_with_holes(P, dtype):
     new = [3, 2, 7, 2, 1, 1]
     cu = np.concatenate([[0], np.cumsum(new)])
     q = randn(rng, (int(cu[-1]), 4, 64), dtype)
-    out, lse = attend(P, c, q, cu, 7, 64, 0.125)
-    check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.125, dtype, seq=seq, gone=gone)
+    for max_q, max_seq in ((32, 1 << 20), (7, 64)):
+        out, lse = attend(P, c, q, cu, max_q, max_seq, 0.125)
+        check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.125, dtype, seq=seq, gone=gone)
     assert np.all(host(out)[3:5] == 0) and np.all(np.isneginf(host(lse)[3:5]))
     assert np.all(host(out)[5:9] == 0) and np.all(np.isneginf(host(lse)[5:9]))   # rows 0..3 of 7 with three tokens
     out, lse = attend(P, c, q, cu, 7, 63, 0.125)
@@ -556,9 +560,10 @@ def test_attention_with_values_that_are_not_finite(P, dtype):
     c.write(P, k, v)
     cu = np.concatenate([[0], np.cumsum(new)])
     q = randn(rng, (int(cu[-1]), 4, 128), dtype)
-    out, lse = attend(P, c, q, cu, 7, 200, 0.09)
-    with np.errstate(invalid="ignore"):
-        check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.09, dtype)
+    for max_q, max_seq in ((32, 1 << 20), (7, 200)):
+        out, lse = attend(P, c, q, cu, max_q, max_seq, 0.09)
+        with np.errstate(invalid="ignore"):
+            check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.09, dtype)
     assert np.isfinite(host(out)[:3]).all() and np.isnan(host(out)[3:7, :, 32:64]).all() and np.isfinite(host(out)[3:7, :, :32]).all()
 
 
@@ -574,8 +579,9 @@ def test_attention_with_rubbish_in_unwritten_tokens(P, dtype, rubbish):
         k, v = (randn(rng, (sum(total), 2, hd), "bf16") for _ in range(2))
         c.write(P, k, v)
         q = randn(rng, (8, 4, hd), dtype)
-        out, lse = attend(P, c, q, [0, 1, 5, 6, 8], 4, 130, 0.1)
-        check_attend(c, q, out, lse, [0, 1, 5, 6, 8], ref.held(host(k)), ref.held(host(v)), 0.1, dtype)
+        for max_q, max_seq in ((4, 130), (32, 1 << 20)):
+            out, lse = attend(P, c, q, [0, 1, 5, 6, 8], max_q, max_seq, 0.1)
+            check_attend(c, q, out, lse, [0, 1, 5, 6, 8], ref.held(host(k)), ref.held(host(v)), 0.1, dtype)
 
 
 def test_attention_layouts(P):
