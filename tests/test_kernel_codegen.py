@@ -170,3 +170,14 @@ def test_hot_kernels_use_no_scratch(device_asm):
             seen += 1
             assert size <= 64, (name, size)
     assert seen >= 117, seen                # all instantiations of today: fewer means that a pattern no longer matches
+
+
+def test_paged_kernels_use_no_scratch(device_asm):
+    """The attention kernels count the transfers they wait for: a reload from scratch among them would be waited for as well."""
+    seen = 0
+    for m in re.finditer(r"\.amdhsa_kernel (\S+)(.*?)\.end_amdhsa_kernel", device_asm, flags=re.S):
+        name, block = m.group(1), m.group(2)
+        if re.search(r"heisd\d+(kv4_attend|kv4_join|kv4_append|kv4_gather|prompt_attend|rope_rows|plan_books|plan_slots)", name):
+            seen += 1
+            assert int(re.search(r"\.amdhsa_private_segment_fixed_size\s+(\d+)", block).group(1)) == 0, name
+    assert seen == 8 + 4 + 12 + 12 + 16 + 12 + 5 + 1, seen

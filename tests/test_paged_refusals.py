@@ -146,6 +146,8 @@ def test_prompt_refusals(P):
     f32 = rows(P, dtype=2)
     refused(P, call(q=f32, k=rows(P, heads=2, dtype=2), v=rows(P, heads=2, dtype=2), out=f32), P.HEISD_EUNSUPPORTED, "fp32")
     refused(P, call(head_dim=96), P.HEISD_EUNSUPPORTED, "head_dim")
+    for more in (dict(k=rows(P, heads=2, rs=(1 << 25) + 8)), dict(v=rows(P, heads=2, rs=1 << 40))):
+        refused(P, call(**more), P.HEISD_EUNSUPPORTED, "apart")
     assert call(n=0) == P.HEISD_OK
 
 
