@@ -484,7 +484,8 @@ int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_batch *batch
  *   workspace DEVICE, 256-byte aligned, heisd_kv4_attention_workspace_bytes(...) bytes (0: invalid sizes) for the same batch, rows,
  *             heads, max_q and max_seq; nothing in it has to be cleared, two calls that may overlap in time need one each
  * A row that sees a token with a value group that is not finite, or holds magnitudes of 2^127 or more, gives NaN or infinities in that
- * group's channels; rows that do not see it are unaffected.  Scores, sums and the softmax are fp32; bf16 queries
+ * group's channels; with a key group that is not finite, or from a query with NaN, NaN in all channels and in lse.  Rows that do
+ * not see such a token are unaffected.  Scores, sums and the softmax are fp32; bf16 queries
  * enter the matrix products as they are, fp16 queries and all probabilities as a bf16 and a bf16 remainder.
  * Errors: EINVAL, EUNSUPPORTED (head_dim, fp32), ENOMEM (workspace), EHIP.
  */

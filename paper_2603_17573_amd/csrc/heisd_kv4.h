@@ -270,6 +270,12 @@ constexpr float kKv4Lazy = 8.f;                     // the maximum is moved only
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A part (a wave's or a workgroup's) with maximum m and sum l saw some token.  A maximum of minus infinity alone does not say that it saw none: where all
+// scores are NaN nothing moves the maximum, and the sum is NaN.
+__device__ __forceinline__ bool kv4_saw(float m, float l) { return m != -INFINITY || l != 0.f; }
+// What such a part's sums are multiplied by where the maximum over all parts is `top`.
+__device__ __forceinline__ float kv4_weight(float m, float top) { return m == -INFINITY ? 1.f : exp2_fast(m - top); }
+
 // softmax(q K^T) V over the tokens of segments.  The query rows of the heads that share the key head are the columns of the matrix products (CT tiles of
 // 16): scores^T = K q^T (tokens are rows), out^T = V^T p^T.  A lane holds the scores of one column and four tokens of each tile, which are
 // its summed indices of the second product, so the probabilities never leave their lane.  Four waves take pairs of tiles in turn,
@@ -580,8 +586,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(K
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-          if (s_m[w][n] != -INFINITY) {             // a wave that saw nothing holds nothing
-            const float by = exp2_fast(s_m[w][n] - top);
+          if (kv4_saw(s_m[w][n], s_l[w][n])) {
+            const float by = kv4_weight(s_m[w][n], top);
             sum += s_l[w][n] * by;
             o += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_mine[w]) + n * LD + d) * by;
           }
@@ -639,20 +645,19 @@ __global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRo
           const long long at = (long long)(wi == w0 ? first_slot : 2 * wi) * a.cols + n;
           ml[i] = *reinterpret_cast<const float2 *>(a.part_ml + at * 2);
           x[i] = *reinterpret_cast<const f32x4 *>(a.part + at * HD + d);
-          if (w + i > w1) ml[i].x = -INFINITY;
+          if (w + i > w1) ml[i] = make_float2(-INFINITY, 0.f);
         }
         float next = top;
 #pragma unroll
         for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
-        if (next == -INFINITY) continue;
-        const float keep = exp2_fast(top - next);
+        const float keep = kv4_weight(top, next);
         sum *= keep;
         o *= keep;
         top = next;
 #pragma unroll
         for (int i = 0; i < K; ++i)
-          if (ml[i].x != -INFINITY) {
-            const float by = exp2_fast(ml[i].x - top);
+          if (kv4_saw(ml[i].x, ml[i].y)) {
+            const float by = kv4_weight(ml[i].x, top);
             sum += ml[i].y * by;
             o += x[i] * by;
           }

@@ -1,0 +1,63 @@
+"""The operators on paged requests where their parts meet: rows and pieces of a context that hold nothing but NaN, lengths between
+max_len and the end of the last block, requests that the plan left out, steps without rows, weights far below the largest.
+Tolerances are those of test_gpu_paged.py unless said otherwise."""
+import math
+
+import numpy as np
+import pytest
+
+import paged_reference as ref
+from test_gpu_paged import (DEV, DTYPES, Cache, attend, check_attend, check_attend_rows, check_prompt, host, i32, lse_tolerance, ok, prompt, randn,
+                            stream, tolerance)
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2603_17573_amd as P
+    return P
+
+
+# ---- attention over the cache: nothing but NaN --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("total,head_dim", [(1, 64), (33, 128), (129, 64), (1537, 128), (1537, 64)])
+def test_a_key_that_is_nan_alone_in_its_part(P, dtype, total, head_dim):
+    """The last token's key has a group that is not finite and is all that a wave, or a workgroup, has of the context."""
+    rng = np.random.default_rng(total)
+    c = Cache(P, rng, [total, 40], 1, head_dim, 16)
+    k, v = (randn(rng, (total + 40, 1, head_dim), "f32") for _ in range(2))
+    k[total - 1, 0, 3] = math.inf
+    c.write(P, k, v)
+    q = randn(rng, (3, 2, head_dim), dtype)
+    cu = [0, 2, 3] if total > 1 else [0, 1, 3]
+    for max_q, max_seq in ((2, max(total, 40)), (32, 1 << 16)):
+        out, lse = attend(P, c, q, cu, max_q, max_seq, 0.1)
+        check_attend(c, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.1, dtype)
+    last = cu[1] - 1
+    assert np.isnan(host(out)[last]).all() and np.isnan(host(lse)[last]).all()
+    assert np.isfinite(host(out)[[r for r in range(3) if r != last]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("total,head_dim", [(1, 128), (50, 64), (3000, 64), (3000, 128)])
+def test_a_query_that_is_nan(P, dtype, total, head_dim):
+    """All scores of a row are NaN, in one workgroup and in several: NaN, not the answer of a row that sees nothing."""
+    rng = np.random.default_rng(total)
+    c = Cache(P, rng, [total, total], 2, head_dim, 32)
+    k, v = (randn(rng, (2 * total, 2, head_dim), "f32") for _ in range(2))
+    c.write(P, k, v)
+    q = randn(rng, (2, 4, head_dim), dtype)
+    q[0, 1, 5] = math.nan
+    for max_seq in (total, 1 << 16):
+        out, lse = attend(P, c, q, [0, 1, 2], 1, max_seq, 0.1)
+        check_attend(c, q, out, lse, [0, 1, 2], ref.held(host(k)), ref.held(host(v)), 0.1, dtype)
+    assert np.isnan(host(out)[0, 1]).all() and np.isnan(host(lse)[0, 1]) and np.isfinite(host(out)[0, [0, 2, 3]]).all()
