@@ -174,9 +174,10 @@ def head_rows(t: torch.Tensor) -> B.heisd_head_rows:
     return B.heisd_head_rows(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _DTYPE[t.dtype])
 
 
-def _ints(t, shape, what):
-    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s: expected contiguous int32 %s, got %s %s" % (what, tuple(shape), t.dtype, tuple(t.shape)))
+def _ints(t, shape, what, device):
+    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_cuda:
+        raise ValueError("%s: expected contiguous int32 %s on %s, got %s %s on %s"
+                         % (what, tuple(shape), device if device.type == "cuda" else "a GPU", t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
@@ -190,9 +191,9 @@ def make_plan_desc(block_size, n_blocks, cached_len, new_len, owned_in, owned_ou
                            ("free_ids", free_ids, (n_blocks,)), ("free_count_in", free_count_in, (1,)),
                            ("free_count_out", free_count_out, (1,)), ("cu_rows", cu_rows, (b + 1,)), ("seq_len", seq_len, (b,)),
                            ("slot", slot, (rows,)), ("position", position, (rows,))):
-        setattr(d, name, _ints(t, shape, name))
+        setattr(d, name, _ints(t, shape, name, cached_len.device))
     if cu_seq is not None:
-        d.cu_seq = _ints(cu_seq, (b + 1,), "cu_seq")
+        d.cu_seq = _ints(cu_seq, (b + 1,), "cu_seq", cached_len.device)
     return d
 
 
@@ -212,15 +213,15 @@ def rope_table(desc: B.heisd_rope_desc, device):
 def make_kv4_desc(pool: torch.Tensor, block_size, kv_heads, head_dim) -> B.heisd_kv4_desc:
     """pool: contiguous uint8 whose size is that of a whole number of blocks; it must stay alive as long as the descriptor is used."""
     cell = block_size * (head_dim + head_dim // 16) * kv_heads
-    if pool.dtype != torch.uint8 or not pool.is_contiguous() or cell <= 0 or pool.numel() % cell:
-        raise ValueError("pool: expected contiguous uint8 of a multiple of %d bytes" % cell)
+    if pool.dtype != torch.uint8 or not pool.is_contiguous() or cell <= 0 or pool.numel() % cell or not pool.is_cuda:
+        raise ValueError("pool: expected contiguous uint8 of a multiple of %d bytes on a GPU" % cell)
     return B.heisd_kv4_desc(pool.data_ptr(), pool.numel() // cell, block_size, kv_heads, head_dim)
 
 
 def make_paged_batch(block_table, seq_len, cu_rows, rows) -> B.heisd_paged_batch:
-    b, most = block_table.shape
-    return B.heisd_paged_batch(_ints(block_table, (b, most), "block_table"), _ints(seq_len, (b,), "seq_len"),
-                               _ints(cu_rows, (b + 1,), "cu_rows") if cu_rows is not None else None, b, most, rows)
+    (b, most), dev = block_table.shape, block_table.device
+    return B.heisd_paged_batch(_ints(block_table, (b, most), "block_table", dev), _ints(seq_len, (b,), "seq_len", dev),
+                               _ints(cu_rows, (b + 1,), "cu_rows", dev) if cu_rows is not None else None, b, most, rows)
 
 
 class PagedCache:

@@ -61,3 +61,23 @@ def test_a_query_that_is_nan(P, dtype, total, head_dim):
         out, lse = attend(P, c, q, [0, 1, 2], 1, max_seq, 0.1)
         check_attend(c, q, out, lse, [0, 1, 2], ref.held(host(k)), ref.held(host(v)), 0.1, dtype)
     assert np.isnan(host(out)[0, 1]).all() and np.isnan(host(lse)[0, 1]) and np.isfinite(host(out)[0, [0, 2, 3]]).all()
+
+
+# ---- a cache with its calls in order --------------------------------------------------------------------------------------
+
+def fill(c, rng, layer, rows, heads, kv_heads, hd, dtype):
+    """Rows of a step, rotated and appended."""
+    q, k, v = randn(rng, (rows, heads, hd), dtype), randn(rng, (rows, kv_heads, hd), dtype), randn(rng, (rows, kv_heads, hd), dtype)
+    c.rotate(q, k)
+    c.append(layer, k, v)
+    return q, k, v
+
+
+def test_host_lengths_are_refused(P):
+    c = P.PagedCache(1, 4, 2, 64, 2, 64, 8, n_blocks=6, block_size=16)
+    here, there = i32([3, 5]), torch.tensor([3, 5], dtype=torch.int32)
+    for a, b in ((there, there), (there, here), (here, there)):
+        with pytest.raises(ValueError, match="expected"):
+            c.begin(a, b, 8)
+    torch.cuda.synchronize()
+    assert int(c.free_count[0]) == 6
