@@ -272,6 +272,14 @@ class PagedCache:
                                                                               tuple(t.shape), t.device))
         return head_rows(t)
 
+    def _lse(self, t):
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or tuple(t.shape) != (self.rows, self.q_heads) or not t.is_contiguous() or t.device != self.device:
+            raise ValueError("lse: expected contiguous float32 [%d, %d] on %s, got %s %s strides %s on %s"
+                             % (self.rows, self.q_heads, self.device, t.dtype, tuple(t.shape), t.stride(), t.device))
+        return t.data_ptr()
+
     def begin(self, cached_len, new_len, rows):
         """cached_len, new_len i32[max_batch] on the device (a negative cached_len: the request is finished and gives its blocks back);
         rows: packed rows of this step, at least the sum of new_len.  A request that does not fit has seq_len -1 afterwards."""
@@ -297,7 +305,7 @@ class PagedCache:
         """Attention of this step's rows over everything their requests have cached, the rows themselves included."""
         out = torch.empty_like(q) if out is None else out
         hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
-        self._call(B.heisd_kv4_attention, self.descs[layer], self.batch, hq, ho, lse.data_ptr() if lse is not None else None,
+        self._call(B.heisd_kv4_attention, self.descs[layer], self.batch, hq, ho, self._lse(lse),
                    self.head_dim ** -0.5 if scale is None else scale, self.max_new, self.max_len, self.workspace.data_ptr(),
                    self.workspace.numel())
         return out
@@ -307,7 +315,7 @@ class PagedCache:
         out = torch.empty_like(q) if out is None else out
         hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
         hk, hv = self._of_step(k, self.kv_heads, "k"), self._of_step(v, self.kv_heads, "v")
-        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, lse.data_ptr() if lse is not None else None, self.cu_rows.data_ptr(),
+        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, self._lse(lse), self.cu_rows.data_ptr(),
                    self.cu_rows.data_ptr(), self.table.shape[0], self.rows, self.rows, self.head_dim,
                    self.head_dim ** -0.5 if scale is None else scale, 1)
         return out
@@ -322,7 +330,7 @@ class PagedCache:
             self._kv.append(torch.empty((2, total, self.kv_heads, self.head_dim), dtype=q.dtype, device=self.device))
         hk, hv = head_rows(self._kv[-1][0]), head_rows(self._kv[-1][1])
         self._call(B.heisd_kv4_gather, self.descs[layer], self.batch, self.cu_seq.data_ptr(), total, hk, hv)
-        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, lse.data_ptr() if lse is not None else None, self.cu_rows.data_ptr(),
+        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, self._lse(lse), self.cu_rows.data_ptr(),
                    self.cu_seq.data_ptr(), self.table.shape[0], self.rows, total, self.head_dim,
                    self.head_dim ** -0.5 if scale is None else scale, 1)
         return out

@@ -81,3 +81,19 @@ def test_host_lengths_are_refused(P):
             c.begin(a, b, 8)
     torch.cuda.synchronize()
     assert int(c.free_count[0]) == 6
+
+
+def test_log_sums_of_another_kind_are_refused(P):
+    """attend(), prompt() and chunk() write lse as float32 [rows, q_heads]: anything else would be written past its end."""
+    c = P.PagedCache(1, 4, 2, 64, 2, 64, 8, n_blocks=6, block_size=16)
+    c.begin(i32([0, 0]), i32([3, 5]), 8)
+    q, k, v = fill(c, np.random.default_rng(1), 0, 8, 4, 2, 64, "bf16")
+    for lse in (torch.zeros(8, 4, dtype=torch.float16, device=DEV), torch.zeros(8, 4, dtype=torch.float64, device=DEV), torch.zeros(7, 4, device=DEV),
+                torch.zeros(32, device=DEV), torch.zeros(8, 8, device=DEV)[:, ::2], torch.zeros(4, 8, device=DEV).t(), torch.zeros(8, 4)):
+        for call in (lambda: c.attend(0, q, lse=lse), lambda: c.prompt(q, k, v, lse=lse), lambda: c.chunk(0, q, 8, lse=lse)):
+            with pytest.raises(ValueError, match="lse"):
+                call()
+    same = [torch.full((8, 4), 7.0, device=DEV) for _ in range(3)]
+    c.attend(0, q, lse=same[0]), c.prompt(q, k, v, lse=same[1]), c.chunk(0, q, 8, lse=same[2])
+    torch.cuda.synchronize()
+    assert all(np.isfinite(host(x)).all() and np.all(host(x) != 7) for x in same)
