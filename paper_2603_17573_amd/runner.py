@@ -229,21 +229,22 @@ class PagedCache:
     the order a decoder makes them: begin() once, then for every layer rotate(), append() and one of attend() (single
     tokens and drafts), prompt() (whole prompts into empty caches) or chunk() (chunks behind cached rows).
 
-    max_batch requests of at most max_len tokens; a step has at most max_rows packed rows.  Everything the calls need is allocated
+    max_batch requests of at most max_len tokens (rounded up to whole blocks); a step has at most max_rows packed rows.  Everything the calls need is allocated
     here, so a step can be captured into a HIP graph (chunk() too, once its buffers have been made by a first call)."""
 
     def __init__(self, n_layers, q_heads, kv_heads, head_dim, max_batch, max_len, max_rows, n_blocks, block_size=64, rope=None,
                  layout="half", max_new=1, device="cuda:0"):
         self.device = torch.device(device)
-        self.q_heads, self.kv_heads, self.head_dim, self.max_new, self.max_len = q_heads, kv_heads, head_dim, max_new, max_len
+        self.q_heads, self.kv_heads, self.head_dim, self.max_new = q_heads, kv_heads, head_dim, max_new
         self.block_size, self.n_blocks = block_size, n_blocks
+        self.max_len = -(-max_len // block_size) * block_size      # what begin() takes: the plan knows blocks only
         nbytes = B.heisd_kv4_pool_bytes(n_blocks, block_size, kv_heads, head_dim)
         if nbytes == 0:
             raise ValueError("invalid cache: %d blocks of %d tokens, %d heads of %d" % (n_blocks, block_size, kv_heads, head_dim))
         i32 = dict(dtype=torch.int32, device=self.device)
         with torch.cuda.device(self.device):
             self.pools = torch.empty((n_layers, nbytes), dtype=torch.uint8, device=self.device)
-            self.table = torch.full((max_batch, -(-max_len // block_size)), -1, **i32)
+            self.table = torch.full((max_batch, self.max_len // block_size), -1, **i32)
             self.owned = torch.zeros(max_batch, **i32)
             self.free_ids = torch.arange(n_blocks, **i32)
             self.free_count = torch.full((1,), n_blocks, **i32)
@@ -251,9 +252,9 @@ class PagedCache:
             self.cu_rows, self.cu_seq = torch.zeros(max_batch + 1, **i32), torch.zeros(max_batch + 1, **i32)
             self.slot, self.position = torch.full((max_rows,), -1, **i32), torch.full((max_rows,), -1, **i32)
             self.descs = [make_kv4_desc(p, block_size, kv_heads, head_dim) for p in self.pools]
-            n = B.heisd_kv4_attention_workspace_bytes(self.descs[0], max_batch, max_rows, q_heads, max_new, max_len)
+            n = B.heisd_kv4_attention_workspace_bytes(self.descs[0], max_batch, max_rows, q_heads, max_new, self.max_len)
             if n == 0:
-                raise ValueError("invalid attention: %d query heads, %d rows, max_new %d, max_len %d" % (q_heads, max_rows, max_new, max_len))
+                raise ValueError("invalid attention: %d query heads, %d rows, max_new %d, max_len %d" % (q_heads, max_rows, max_new, self.max_len))
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
             desc = rope if rope is not None else make_rope_desc(head_dim)
             self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]

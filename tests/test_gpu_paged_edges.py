@@ -97,3 +97,22 @@ def test_log_sums_of_another_kind_are_refused(P):
     c.attend(0, q, lse=same[0]), c.prompt(q, k, v, lse=same[1]), c.chunk(0, q, 8, lse=same[2])
     torch.cuda.synchronize()
     assert all(np.isfinite(host(x)).all() and np.all(host(x) != 7) for x in same)
+
+
+@pytest.mark.parametrize("length", [200, 201, 255, 256, 257])
+def test_lengths_up_to_the_end_of_the_last_block(P, length):
+    """max_len 200 in blocks of 64: what begin() takes, attend() and chunk() compute alike; what it does not take is left out."""
+    rng = np.random.default_rng(length)
+    c = P.PagedCache(1, 2, 1, 64, 2, 200, 300, n_blocks=8, block_size=64)
+    c.begin(i32([0, 0]), i32([length, 3]), length + 3)
+    q, k, v = fill(c, rng, 0, length + 3, 2, 1, 64, "bf16")
+    outs = c.attend(0, q), c.chunk(0, q, length + 3)
+    torch.cuda.synchronize()
+    fits = length <= 256
+    assert host(c.seq_len).tolist() == [length if fits else -1, 3]
+    for out, chunk in zip(outs, (False, True)):
+        for a, b, there in ((0, length, fits), (length, length + 3, True)):
+            if there:
+                check_attend_rows(host(q)[a:b], host(out)[a:b], ref.held(host(k)[a:b]), ref.held(host(v)[a:b]), 0.125, "bf16", chunk=chunk)
+            else:
+                assert np.all(host(out)[a:b] == 0)
