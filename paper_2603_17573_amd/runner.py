@@ -237,10 +237,10 @@ class PagedCache:
         self.device = torch.device(device)
         self.q_heads, self.kv_heads, self.head_dim, self.max_new = q_heads, kv_heads, head_dim, max_new
         self.block_size, self.n_blocks = block_size, n_blocks
-        self.max_len = -(-max_len // block_size) * block_size      # what begin() takes: the plan knows blocks only
         nbytes = B.heisd_kv4_pool_bytes(n_blocks, block_size, kv_heads, head_dim)
         if nbytes == 0:
             raise ValueError("invalid cache: %d blocks of %d tokens, %d heads of %d" % (n_blocks, block_size, kv_heads, head_dim))
+        self.max_len = -(-max_len // block_size) * block_size      # what begin() takes: the plan knows blocks only
         i32 = dict(dtype=torch.int32, device=self.device)
         with torch.cuda.device(self.device):
             self.pools = torch.empty((n_layers, nbytes), dtype=torch.uint8, device=self.device)

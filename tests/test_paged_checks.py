@@ -27,3 +27,9 @@ def test_host_tensors_are_refused(P):
         P.make_paged_batch(i(2, 4), i(2), None, 0)
     with pytest.raises(ValueError, match="on a GPU"):
         P.make_kv4_desc(torch.zeros(16 * 68, dtype=torch.uint8), 16, 1, 64)
+
+
+def test_a_cache_of_no_tokens_per_block_is_refused(P):
+    for size in (0, -16, 24):
+        with pytest.raises(ValueError, match="invalid cache"):
+            P.PagedCache(1, 2, 1, 64, 2, 200, 300, n_blocks=8, block_size=size)
