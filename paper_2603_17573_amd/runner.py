@@ -259,7 +259,7 @@ class PagedCache:
             desc = rope if rope is not None else make_rope_desc(head_dim)
             self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]
             self.turns, self.magnitude = rope_table(desc, self.device)
-        self.rows, self._kv = 0, []
+        self.rows, self._kv, self._captured = 0, {}, []
 
     def _call(self, fn, *args):
         with torch.cuda.device(self.device):
@@ -321,15 +321,27 @@ class PagedCache:
                    self.head_dim ** -0.5 if scale is None else scale, 1)
         return out
 
+    def _chunk_rows(self, total, dtype):
+        """[2, at least total, kv_heads, head_dim] for cached rows read back: a pair per dtype, of twice the size when it gets too small."""
+        kv = self._kv.get(dtype)
+        with torch.cuda.device(self.device):
+            if kv is None or kv.shape[1] < total:
+                rows = total if kv is None else max(total, min(2 * kv.shape[1], self.n_blocks * self.block_size))
+                kv = self._kv[dtype] = None                        # the smaller one goes first
+                kv = self._kv[dtype] = torch.empty((2, rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+            if not torch.cuda.is_current_stream_capturing():
+                kv.record_stream(torch.cuda.current_stream())
+            elif all(kv is not t for t in self._captured):         # the graph goes on reading and writing it, whatever comes after
+                self._captured.append(kv)
+        return kv
+
     def chunk(self, layer, q, total, scale=None, out=None, lse=None):
         """Causal attention of many rows per request over everything cached (total: at least the sum of the requests' lengths): the
         cached rows are read back once and multiplied as a prompt's."""
         out = torch.empty_like(q) if out is None else out
         hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
-        if not self._kv or self._kv[-1].shape[1] < total or self._kv[-1].dtype != q.dtype:
-            # a captured graph may still read and write the smaller ones: they stay
-            self._kv.append(torch.empty((2, total, self.kv_heads, self.head_dim), dtype=q.dtype, device=self.device))
-        hk, hv = head_rows(self._kv[-1][0]), head_rows(self._kv[-1][1])
+        kv = self._chunk_rows(total, q.dtype)
+        hk, hv = head_rows(kv[0]), head_rows(kv[1])
         self._call(B.heisd_kv4_gather, self.descs[layer], self.batch, self.cu_seq.data_ptr(), total, hk, hv)
         self._call(B.heisd_prompt_attention, hq, hk, hv, ho, self._lse(lse), self.cu_rows.data_ptr(),
                    self.cu_seq.data_ptr(), self.table.shape[0], self.rows, total, self.head_dim,

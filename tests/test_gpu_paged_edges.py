@@ -116,3 +116,51 @@ def test_lengths_up_to_the_end_of_the_last_block(P, length):
                 check_attend_rows(host(q)[a:b], host(out)[a:b], ref.held(host(k)[a:b]), ref.held(host(v)[a:b]), 0.125, "bf16", chunk=chunk)
             else:
                 assert np.all(host(out)[a:b] == 0)
+
+
+# ---- the buffers that chunks are read back into ------------------------------------------------------------------------------
+
+def test_chunk_buffers_do_not_pile_up(P):
+    """Totals that grow step by step, and dtypes in turn: at most twice the largest need per dtype stays."""
+    rng = np.random.default_rng(3)
+    heads, hd = 2, 64
+    c = P.PagedCache(1, 2, heads, hd, 1, 4096, 64, n_blocks=64, block_size=64)
+    c.begin(i32([0]), i32([64]), 64)
+    q, k, v = fill(c, rng, 0, 64, 2, heads, hd, "bf16")
+    want = c.chunk(0, q, 64)
+    torch.cuda.synchronize()
+    before, need = torch.cuda.memory_allocated(), 0
+    for total in range(64, 4097, 64):
+        for dtype in (torch.bfloat16, torch.float16):
+            c.chunk(0, q.to(dtype), total)
+        need = 2 * 2 * total * heads * hd * 2                          # two dtypes, keys and values
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() - before <= 2 * need
+    assert torch.equal(c.chunk(0, q, 64), want)
+    check_attend_rows(host(q), host(c.chunk(0, q, 4096)), ref.held(host(k)), ref.held(host(v)), 0.125, "bf16", chunk=True)
+
+
+def test_a_captured_chunk_keeps_its_buffers(P):
+    """A graph with a chunk in it, larger chunks of other sizes afterwards, and memory taken by others: every replay gives the same."""
+    rng = np.random.default_rng(5)
+    heads, hd = (4, 2), 64
+    c = P.PagedCache(1, *heads, hd, 2, 2048, 64, n_blocks=64, block_size=64)
+    c.begin(i32([0, 0]), i32([20, 40]), 60)
+    q, k, v = fill(c, rng, 0, 60, *heads, hd, "bf16")
+    out = torch.empty_like(q)
+    want = c.chunk(0, q, 60).clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            c.chunk(0, q, 60, out=out)
+    for n in range(4):
+        c.chunk(0, q, 200 * (n + 1))
+        other = [torch.full((1 << 14,), 255, dtype=torch.uint8, device=DEV) for _ in range(40)]
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), n
+        assert all(bool((x == 255).all()) for x in other)
