@@ -341,8 +341,8 @@ int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int32_t d, con
  * attention of packed prompts with grouped heads.  These calls serve decoders (or batches of episodes) whose caches do not
  * fit the contiguous bf16 layout of heisd_kv_desc: contexts of different lengths share a pool of blocks, several query heads
  * share a key head, and a cached row takes 17/64 of its bf16 bytes.  Used together, per step and layer:
- *   heisd_paged_plan (once per step) -> heisd_rope -> heisd_kv4_append -> heisd_kv4_attention (single tokens, drafts) or
- *   heisd_prompt_attention (prompts; with heisd_kv4_gather, chunks behind cached rows).
+ *   heisd_paged_plan (once per step) -> heisd_rope -> heisd_kv4_append -> heisd_kv4_attention (single tokens, drafts),
+ *   heisd_paged_prompt_attention (prompts) or heisd_kv4_gather and heisd_prompt_attention (chunks behind cached rows).
  * All are asynchronous on `stream`, allocate nothing, keep nothing between calls, and run on the current device, whose memory
  * every DEVICE pointer must belong to.  Results do not depend on timing (no floating-point atomics).  Errors are found before
  * anything is enqueued; heisd_last_error(NULL) has the text.  Calls with no rows return OK and enqueue nothing (heisd_paged_plan always runs).
@@ -507,6 +507,14 @@ int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *ba
 int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out, float *lse,
                            const int32_t *cu_q, const int32_t *cu_k, int32_t batch, int32_t rows, int32_t k_rows, int32_t head_dim, float scale,
                            int32_t causal, void *stream);
+
+/*
+ * The same, causal, for a step's rows as heisd_paged_plan packs them: the sequences of q, k, v and out are the requests of `batch`
+ * (cu_rows; rows in each), over their own rows and nothing cached.  A request with a negative seq_len (finished, or left out by the plan)
+ * sees nothing: its rows give zeros and lse -inf, as from heisd_kv4_attention.  block_table is not read (and not NULL).
+ */
+int heisd_paged_prompt_attention(const heisd_paged_batch *batch, const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v,
+                                 const heisd_head_rows *out, float *lse, int32_t head_dim, float scale, void *stream);
 
 /*
  * Per-kernel timing for measurement runs (not part of the method).  With profiling enabled,

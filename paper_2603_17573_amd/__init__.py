@@ -12,7 +12,7 @@ from .binding import (heisd_model_desc, heisd_kv_desc, heisd_accept_desc, heisd_
                       heisd_retrieve_topk_static, heisd_debug_trace, heisd_verify_set_handover, heisd_verify_set_activations, heisd_verify_release_projections, heisd_debug_set_wait_limits, heisd_debug_projection_plan, HEISD_ACT_SPLIT, HEISD_ACT_BF16, heisd_measure_read,
                       heisd_head_rows, heisd_plan_desc, heisd_rope_desc, heisd_kv4_desc, heisd_paged_batch,
                       heisd_paged_plan, heisd_rope_table, heisd_rope, heisd_kv4_pool_bytes, heisd_kv4_append, heisd_kv4_gather,
-                      heisd_kv4_attention_workspace_bytes, heisd_kv4_attention, heisd_prompt_attention,
+                      heisd_kv4_attention_workspace_bytes, heisd_kv4_attention, heisd_prompt_attention, heisd_paged_prompt_attention,
                       HEISD_DTYPE_BF16, HEISD_DTYPE_F16, HEISD_DTYPE_F32, ROPE_LAYOUT, ROPE_SCALING,
                       heisd_measure_empty_launch, heisd_free, heisd_last_error,
                       heisd_verify_profile_enable, heisd_verify_profile_read, KERNEL_CLASSES,

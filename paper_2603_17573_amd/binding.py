@@ -138,6 +138,8 @@ def load():
         lib.heisd_prompt_attention.argtypes = [rows_p, rows_p, rows_p, rows_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
                                                c_int32, c_float, c_int32, c_void_p]
         lib.heisd_prompt_attention.restype = ctypes.c_int
+        lib.heisd_paged_prompt_attention.argtypes = [paged_p, rows_p, rows_p, rows_p, rows_p, c_void_p, c_int32, c_float, c_void_p]
+        lib.heisd_paged_prompt_attention.restype = ctypes.c_int
         lib.heisd_free.argtypes = [c_void_p]
         lib.heisd_free.restype = None
         lib.heisd_verify_profile_enable.argtypes = [c_void_p, ctypes.c_int]
@@ -302,6 +304,11 @@ def heisd_prompt_attention(q: heisd_head_rows, k: heisd_head_rows, v: heisd_head
                            head_dim, scale, causal, stream) -> int:
     return load().heisd_prompt_attention(_ref(q), _ref(k), _ref(v), _ref(out), lse, cu_q, cu_k, batch, rows, k_rows, head_dim, scale, causal,
                                          stream)
+
+
+def heisd_paged_prompt_attention(batch: heisd_paged_batch, q: heisd_head_rows, k: heisd_head_rows, v: heisd_head_rows, out: heisd_head_rows, lse,
+                                 head_dim, scale, stream) -> int:
+    return load().heisd_paged_prompt_attention(_ref(batch), _ref(q), _ref(k), _ref(v), _ref(out), lse, head_dim, scale, stream)
 
 
 def heisd_free(ctx) -> None:

@@ -405,10 +405,9 @@ static hipError_t prompt_launch(const PromptArgs &a, const heisd_head_rows *q, c
   return split ? prompt_launch_one<T, HD, CAUSAL, 2>(a, q, k, v, out, st) : prompt_launch_one<T, HD, CAUSAL, 1>(a, q, k, v, out, st);
 }
 
-extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out,
-                                      float *lse, const int32_t *cu_q, const int32_t *cu_k, int32_t batch, int32_t rows, int32_t k_rows,
-                                      int32_t head_dim, float scale, int32_t causal, void *stream) {
-  const char *who = "prompt_attention";
+static int prompt_attention(const char *who, const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out,
+                            float *lse, const int32_t *cu_q, const int32_t *cu_k, const int32_t *seq_len, int32_t batch, int32_t rows, int32_t k_rows,
+                            int32_t head_dim, float scale, int32_t causal, void *stream) {
   int rc = rows_ok(who, "q", q);
   if (rc == HEISD_OK) rc = rows_ok(who, "k", k);
   if (rc == HEISD_OK) rc = rows_ok(who, "v", v);
@@ -428,7 +427,7 @@ extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head
   const int64_t tiles = (int64_t)rows / kPromptRows + batch;
   if (tiles * q->heads > 0x7FFFFFFF) return fail(nullptr, HEISD_EINVAL, "%s: rows=%d too many", who, rows);
   if (rows == 0) return HEISD_OK;
-  const PromptArgs a{cu_q, cu_k, batch, rows, k_rows, q->heads, k->heads, q->heads / k->heads, (int)tiles,
+  const PromptArgs a{cu_q, cu_k, seq_len, batch, rows, k_rows, q->heads, k->heads, q->heads / k->heads, (int)tiles,
                      std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f),   // not 0: minus infinity stands for masked scores
                      scale < 0 ? 0x80008000u : 0u, lse};
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -443,4 +442,20 @@ extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head
   }
   if (e != hipSuccess) return fail(nullptr, HEISD_EHIP, "%s: %s", who, hipGetErrorString(e));
   return launched(who);
+}
+
+extern "C" int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out,
+                                      float *lse, const int32_t *cu_q, const int32_t *cu_k, int32_t batch, int32_t rows, int32_t k_rows,
+                                      int32_t head_dim, float scale, int32_t causal, void *stream) {
+  return prompt_attention("prompt_attention", q, k, v, out, lse, cu_q, cu_k, nullptr, batch, rows, k_rows, head_dim, scale, causal, stream);
+}
+
+extern "C" int heisd_paged_prompt_attention(const heisd_paged_batch *batch, const heisd_head_rows *q, const heisd_head_rows *k,
+                                            const heisd_head_rows *v, const heisd_head_rows *out, float *lse, int32_t head_dim, float scale,
+                                            void *stream) {
+  const char *who = "paged_prompt_attention";
+  PagedBatch b;
+  const int rc = batch_ok(who, batch, true, &b);
+  if (rc != HEISD_OK) return rc;
+  return prompt_attention(who, q, k, v, out, lse, b.cu_rows, b.cu_rows, b.seq_len, b.batch, b.rows, b.rows, head_dim, scale, 1, stream);
 }

@@ -46,6 +46,7 @@ __device__ __forceinline__ int prompt_swizzle(int r) {
 
 struct PromptArgs {
   const int32_t *cu_q, *cu_k;
+  const int32_t *seq_len;                           // NULL, or negative for sequences that are to see nothing
   int batch, rows, k_rows, q_heads, kv_heads, group;
   int tiles;                                        // row tiles in the grid
   float scale_log2;                                 // magnitude of the softmax scale times log2(e)
@@ -106,7 +107,9 @@ __global__ __launch_bounds__(256 * SPLIT, HD == 64 && SPLIT == 1 ? 3 : 2) void p
   const int head = kvh * a.group + rest % a.group, tile = a.tiles - 1 - rest / a.group;
   // which sequence: sequence i is given tiles floor(cu[i] / 128) + i and on, enough for any length
   const int seq = wave_search(a.batch, tile, [&](int i) { return (long long)max(a.cu_q[i], 0) / kPromptRows + i; });
-  const Span rows = wave_span(a.cu_q, seq, a.rows), keys = wave_span(a.cu_k, seq, a.k_rows);
+  const Span rows = wave_span(a.cu_q, seq, a.rows);
+  Span keys = wave_span(a.cu_k, seq, a.k_rows);
+  if (a.seq_len && __builtin_amdgcn_readfirstlane(a.seq_len[seq]) < 0) keys.count = 0;
   const int first = (tile - (rows.begin / kPromptRows + seq)) * kPromptRows;
   if (first < 0 || first >= rows.count) return;
   const int shift = CAUSAL ? keys.count - rows.count : 0;                          // row i sees keys 0 .. shift + i

@@ -316,9 +316,8 @@ class PagedCache:
         out = torch.empty_like(q) if out is None else out
         hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
         hk, hv = self._of_step(k, self.kv_heads, "k"), self._of_step(v, self.kv_heads, "v")
-        self._call(B.heisd_prompt_attention, hq, hk, hv, ho, self._lse(lse), self.cu_rows.data_ptr(),
-                   self.cu_rows.data_ptr(), self.table.shape[0], self.rows, self.rows, self.head_dim,
-                   self.head_dim ** -0.5 if scale is None else scale, 1)
+        self._call(B.heisd_paged_prompt_attention, self.batch, hq, hk, hv, ho, self._lse(lse), self.head_dim,
+                   self.head_dim ** -0.5 if scale is None else scale)
         return out
 
     def _chunk_rows(self, total, dtype):

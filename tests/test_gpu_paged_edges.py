@@ -164,3 +164,27 @@ def test_a_captured_chunk_keeps_its_buffers(P):
         torch.cuda.synchronize()
         assert torch.equal(out, want), n
         assert all(bool((x == 255).all()) for x in other)
+
+
+def test_prompts_that_were_left_out(P):
+    """A request that got no blocks has rows in the step: zeros and minus infinity from prompt() as from attend() and chunk(), its
+    neighbours as ever, rows of nobody as they were."""
+    rng = np.random.default_rng(2)
+    for dtype, hd in (("bf16", 128), ("f16", 64)):
+        new = [150, 20, 300, 7, 40]
+        c = P.PagedCache(1, 4, 2, hd, 5, 320, 520, n_blocks=16, block_size=16)     # 10 + 2 blocks, then 19 of 4, 1, 3
+        cached = [0, 0, 0, -1, 0]
+        c.begin(i32(cached), i32(new), 520)
+        q, k, v = fill(c, rng, 0, 520, 4, 2, hd, dtype)
+        out, lse = torch.full_like(q, 7.0), torch.full((520, 4), 7.0, device=DEV)
+        c.prompt(q, k, v, out=out, lse=lse)
+        torch.cuda.synchronize()
+        assert host(c.seq_len).tolist() == [150, 20, -1, -1, -1]
+        cu = np.concatenate([[0], np.cumsum(new)])
+        for i in range(2):
+            rows = slice(cu[i], cu[i + 1])
+            check_prompt(q[rows], k[rows], v[rows], out[rows], lse[rows], [0, new[i]], [0, new[i]], hd ** -0.5, True, dtype)
+        assert np.all(host(out)[170:517] == 0) and np.all(np.isneginf(host(lse)[170:517]))
+        assert np.all(host(out)[517:] == 7) and np.all(host(lse)[517:] == 7)
+        alike = c.attend(0, q, out=torch.full_like(q, 7.0))
+        assert np.all(host(alike)[170:517] == 0) and np.all(host(alike)[517:] == 7)

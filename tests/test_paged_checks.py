@@ -33,3 +33,29 @@ def test_a_cache_of_no_tokens_per_block_is_refused(P):
     for size in (0, -16, 24):
         with pytest.raises(ValueError, match="invalid cache"):
             P.PagedCache(1, 2, 1, 64, 2, 200, 300, n_blocks=8, block_size=size)
+
+
+FAKE = 0x10000      # never dereferenced: every call below ends before any device access
+
+
+def rows(P, data=FAKE, rs=1024, hs=128, heads=8, dtype=0):
+    return P.heisd_head_rows(data, rs, hs, heads, dtype)
+
+
+def refused(P, rc, code, *words):
+    assert rc == code, (rc, P.heisd_last_error(None))
+    text = P.heisd_last_error(None)
+    for w in words:
+        assert w in text, text
+
+
+def test_paged_prompt_refusals(P):
+    def call(q=None, k=None, v=None, out=None, head_dim=128, scale=0.1, **b):
+        desc = P.heisd_paged_batch(*[b.get(n, x) for n, x in (("table", FAKE), ("seq", FAKE), ("cu", FAKE), ("batch", 2), ("max_blocks", 4), ("rows", 6))])
+        return P.heisd_paged_prompt_attention(desc, q or rows(P), k or rows(P, heads=2), v or rows(P, heads=2), out or rows(P, 0x20000), None, head_dim, scale, None)
+    for more in (dict(table=None), dict(seq=None), dict(cu=None), dict(batch=0), dict(batch=65536), dict(rows=-1), dict(scale=float("nan")), dict(q=rows(P, heads=7)),
+                 dict(k=rows(P, heads=2, dtype=1)), dict(v=rows(P, heads=4)), dict(q=rows(P, FAKE + 8)), dict(out=rows(P, FAKE + 2)), dict(q=rows(P, 0))):
+        refused(P, call(**more), P.HEISD_EINVAL, "paged_prompt_attention")
+    refused(P, call(head_dim=96), P.HEISD_EUNSUPPORTED, "head_dim")
+    refused(P, P.heisd_paged_prompt_attention(None, rows(P), rows(P), rows(P), rows(P), None, 128, 0.1, None), P.HEISD_EINVAL, "NULL")
+    assert call(rows=0) == P.HEISD_OK
