@@ -345,7 +345,8 @@ int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int32_t d, con
  *   heisd_paged_prompt_attention (prompts) or heisd_kv4_gather and heisd_prompt_attention (chunks behind cached rows).
  * All are asynchronous on `stream`, allocate nothing, keep nothing between calls, and run on the current device, whose memory
  * every DEVICE pointer must belong to.  Results do not depend on timing (no floating-point atomics).  Errors are found before
- * anything is enqueued; heisd_last_error(NULL) has the text.  Calls with no rows return OK and enqueue nothing (heisd_paged_plan always runs).
+ * anything is enqueued; heisd_last_error(NULL) has the text.  Calls with no rows return OK and enqueue nothing (heisd_paged_plan always runs);
+ * rows that there are none of may lie at NULL.
  */
 #define HEISD_DTYPE_BF16 0
 #define HEISD_DTYPE_F16 1

@@ -14,8 +14,9 @@ static bool rows_aligned(const heisd_head_rows &r, size_t bytes) {
   return ((uintptr_t)r.data & (bytes - 1)) == 0 && r.row_stride % n == 0 && r.head_stride % n == 0;
 }
 
-static int rows_ok(const char *who, const char *name, const heisd_head_rows *r) {
-  if (!r || !r->data) return fail(nullptr, HEISD_EINVAL, "%s: NULL %s", who, name);
+// rows: how many there are (without any, there need not be memory for them).
+static int rows_ok(const char *who, const char *name, const heisd_head_rows *r, int64_t rows) {
+  if (!r || (!r->data && rows > 0)) return fail(nullptr, HEISD_EINVAL, "%s: NULL %s", who, name);
   if (!dtype_bytes(r->dtype)) return fail(nullptr, HEISD_EINVAL, "%s: %s has unknown dtype %d", who, name, r->dtype);
   if (r->heads < 1 || r->heads > 512) return fail(nullptr, HEISD_EINVAL, "%s: %s has %d heads (1..512)", who, name, r->heads);
   if (r->row_stride < 0 || r->head_stride < 0) return fail(nullptr, HEISD_EINVAL, "%s: %s has a negative stride", who, name);
@@ -127,7 +128,7 @@ extern "C" int heisd_rope(const double *turns, float magnitude, int32_t rotary_d
   bool wide = true, copies = false;
   const int per = 16 / (q && dtype_bytes(q->dtype) ? (int)dtype_bytes(q->dtype) : 2);
   for (int i = 0; i < (k ? 4 : 2); ++i) {
-    const int rc = rows_ok(who, names[i], all[i]);
+    const int rc = rows_ok(who, names[i], all[i], rows);
     if (rc != HEISD_OK) return rc;
     if (all[i]->dtype != q->dtype) return fail(nullptr, HEISD_EINVAL, "%s: dtypes differ", who);
     wide = wide && rows_aligned(*all[i], 16);
@@ -220,8 +221,8 @@ extern "C" int heisd_kv4_append(const heisd_kv4_desc *cache, const heisd_head_ro
   const char *who = "kv4_append";
   Kv4Cache c;
   int rc = kv4_ok(who, cache, &c);
-  if (rc == HEISD_OK) rc = rows_ok(who, "k", k);
-  if (rc == HEISD_OK) rc = rows_ok(who, "v", v);
+  if (rc == HEISD_OK) rc = rows_ok(who, "k", k, rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "v", v, rows);
   if (rc != HEISD_OK) return rc;
   if (k->dtype != v->dtype || k->heads != c.kv_heads || v->heads != c.kv_heads)
     return fail(nullptr, HEISD_EINVAL, "%s: k and v differ in dtype, or in heads from the cache", who);
@@ -258,8 +259,8 @@ extern "C" int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_b
   PagedBatch b;
   int rc = kv4_ok(who, cache, &c);
   if (rc == HEISD_OK) rc = batch_ok(who, batch, false, &b);
-  if (rc == HEISD_OK) rc = rows_ok(who, "k_out", k_out);
-  if (rc == HEISD_OK) rc = rows_ok(who, "v_out", v_out);
+  if (rc == HEISD_OK) rc = rows_ok(who, "k_out", k_out, out_rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "v_out", v_out, out_rows);
   if (rc != HEISD_OK) return rc;
   if (k_out->dtype != v_out->dtype || k_out->heads != c.kv_heads || v_out->heads != c.kv_heads)
     return fail(nullptr, HEISD_EINVAL, "%s: k_out and v_out differ in dtype, or in heads from the cache", who);
@@ -341,8 +342,8 @@ extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_page
   PagedBatch b;
   int rc = kv4_ok(who, cache, &c);
   if (rc == HEISD_OK) rc = batch_ok(who, batch, true, &b);
-  if (rc == HEISD_OK) rc = rows_ok(who, "q", q);
-  if (rc == HEISD_OK) rc = rows_ok(who, "out", out);
+  if (rc == HEISD_OK) rc = rows_ok(who, "q", q, b.rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "out", out, b.rows);
   if (rc == HEISD_OK) rc = kv4_attention_sizes_ok(who, c.kv_heads, q->heads, b.rows, max_q, max_seq);
   if (rc != HEISD_OK) return rc;
   if (q->dtype != out->dtype || q->heads != out->heads) return fail(nullptr, HEISD_EINVAL, "%s: q and out differ in dtype or heads", who);
@@ -408,10 +409,10 @@ static hipError_t prompt_launch(const PromptArgs &a, const heisd_head_rows *q, c
 static int prompt_attention(const char *who, const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out,
                             float *lse, const int32_t *cu_q, const int32_t *cu_k, const int32_t *seq_len, int32_t batch, int32_t rows, int32_t k_rows,
                             int32_t head_dim, float scale, int32_t causal, void *stream) {
-  int rc = rows_ok(who, "q", q);
-  if (rc == HEISD_OK) rc = rows_ok(who, "k", k);
-  if (rc == HEISD_OK) rc = rows_ok(who, "v", v);
-  if (rc == HEISD_OK) rc = rows_ok(who, "out", out);
+  int rc = rows_ok(who, "q", q, rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "k", k, k_rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "v", v, k_rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "out", out, rows);
   if (rc != HEISD_OK) return rc;
   if (head_dim != 64 && head_dim != 128) return fail(nullptr, HEISD_EUNSUPPORTED, "%s: head_dim %d (64 or 128)", who, head_dim);
   if (q->dtype == HEISD_DTYPE_F32) return fail(nullptr, HEISD_EUNSUPPORTED, "%s: fp32 rows (bf16 or fp16)", who);

@@ -260,6 +260,7 @@ class PagedCache:
             self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]
             self.turns, self.magnitude = rope_table(desc, self.device)
         self.rows, self._kv, self._captured = 0, {}, []
+        self.batch = make_paged_batch(self.table, self.seq_len, self.cu_rows, 0)
 
     def _call(self, fn, *args):
         with torch.cuda.device(self.device):

@@ -188,3 +188,38 @@ def test_prompts_that_were_left_out(P):
         assert np.all(host(out)[517:] == 7) and np.all(host(lse)[517:] == 7)
         alike = c.attend(0, q, out=torch.full_like(q, 7.0))
         assert np.all(host(alike)[170:517] == 0) and np.all(host(alike)[517:] == 7)
+
+
+def test_steps_without_rows(P):
+    """A step in which requests only end: every call of it is taken and gives nothing."""
+    c = P.PagedCache(1, 4, 2, 64, 3, 64, 8, n_blocks=6, block_size=16)
+    c.begin(i32([0, 0, -1]), i32([3, 5, 0]), 8)
+    c.begin(i32([-1, -1, -1]), i32([0, 0, 0]), 0)
+    q, k, v = (torch.empty(0, n, 64, dtype=torch.bfloat16, device=DEV) for n in (4, 2, 2))
+    c.rotate(q, k)
+    c.append(0, k, v)
+    for out in (c.attend(0, q), c.prompt(q, k, v), c.chunk(0, q, 0)):
+        assert tuple(out.shape) == (0, 4, 64)
+    torch.cuda.synchronize()
+    assert int(c.free_count[0]) == 6
+
+
+def test_no_keys_at_all(P):
+    """Queries over no key rows whose tensors have no memory: zeros and minus infinity.  Reading back no rows: nothing."""
+    for dtype in ("bf16", "f16"):
+        q = torch.ones(5, 2, 128, dtype=DTYPES[dtype], device=DEV)
+        k = torch.empty(0, 1, 128, dtype=DTYPES[dtype], device=DEV)
+        assert k.data_ptr() == 0
+        for causal in (False, True):
+            out, lse = prompt(P, q, k, k, [0, 2, 5], [0, 0, 0], 0.1, causal)
+            assert np.all(host(out) == 0) and np.all(np.isneginf(host(lse)))
+    c = Cache(P, np.random.default_rng(1), [0, 0], 1, 64, 16)
+    k, _ = c.read(P)
+    assert k.shape[0] == 0
+
+
+def test_before_the_first_step(P):
+    """Without a begin() there are no rows."""
+    c = P.PagedCache(1, 4, 2, 64, 3, 64, 8, n_blocks=6, block_size=16)
+    q = torch.empty(0, 4, 64, dtype=torch.bfloat16, device=DEV)
+    assert c.attend(0, q).shape[0] == 0 and c.chunk(0, q, 0).shape[0] == 0

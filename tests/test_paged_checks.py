@@ -59,3 +59,21 @@ def test_paged_prompt_refusals(P):
     refused(P, call(head_dim=96), P.HEISD_EUNSUPPORTED, "head_dim")
     refused(P, P.heisd_paged_prompt_attention(None, rows(P), rows(P), rows(P), rows(P), None, 128, 0.1, None), P.HEISD_EINVAL, "NULL")
     assert call(rows=0) == P.HEISD_OK
+
+
+def test_rows_that_there_are_none_of_need_no_memory(P):
+    """What an empty tensor gives: NULL."""
+    none, one = rows(P, 0), rows(P, 0, heads=2)
+    cache, slot = P.heisd_kv4_desc(FAKE, 10, 16, 8, 128), None
+    assert P.heisd_rope(FAKE, 1.0, 64, 0, 0, None, 0, 128, none, none, one, one, None) == P.HEISD_OK
+    assert P.heisd_kv4_append(cache, none, none, slot, 0, None) == P.HEISD_OK
+    b = P.heisd_paged_batch(FAKE, FAKE, FAKE, 2, 4, 0)
+    assert P.heisd_kv4_gather(cache, b, FAKE, 0, none, none, None) == P.HEISD_OK
+    assert P.heisd_kv4_attention(cache, b, none, none, None, 0.1, 1, 64, FAKE, 0, None) == P.HEISD_OK
+    assert P.heisd_prompt_attention(none, one, one, none, None, FAKE, FAKE, 2, 0, 0, 128, 0.1, 1, None) == P.HEISD_OK
+    assert P.heisd_paged_prompt_attention(b, none, one, one, none, None, 128, 0.1, None) == P.HEISD_OK
+    # what there is must lie somewhere
+    refused(P, P.heisd_rope(FAKE, 1.0, 64, 0, 0, FAKE, 1, 128, none, none, None, None, None), P.HEISD_EINVAL, "NULL q")
+    refused(P, P.heisd_prompt_attention(rows(P), one, one, rows(P), None, FAKE, FAKE, 2, 4, 1, 128, 0.1, 1, None), P.HEISD_EINVAL, "NULL k")
+    refused(P, P.heisd_prompt_attention(none, one, one, none, None, FAKE, FAKE, 2, 4, 0, 128, 0.1, 1, None), P.HEISD_EINVAL, "NULL q")
+    refused(P, P.heisd_kv4_append(cache, none, none, FAKE, -1, None), P.HEISD_EINVAL, "rows=-1")
