@@ -287,11 +287,10 @@ class PagedCache:
         rows: packed rows of this step, at least the sum of new_len.  A request that does not fit has seq_len -1 afterwards."""
         if not 0 <= rows <= self.slot.shape[0]:
             raise ValueError("rows=%d, made for at most %d" % (rows, self.slot.shape[0]))
-        self.rows = rows
         self._call(B.heisd_paged_plan, make_plan_desc(self.block_size, self.n_blocks, cached_len, new_len, self.owned, self.owned, self.table,
                                                       self.free_ids, self.free_count, self.free_count, self.seq_len, self.cu_rows,
                                                       self.slot[:rows], self.position[:rows], self.cu_seq))
-        self.batch = make_paged_batch(self.table, self.seq_len, self.cu_rows, rows)
+        self.rows, self.batch = rows, make_paged_batch(self.table, self.seq_len, self.cu_rows, rows)
 
     def rotate(self, q, k):
         """q and k of this step's rows, in place."""

@@ -223,3 +223,16 @@ def test_before_the_first_step(P):
     c = P.PagedCache(1, 4, 2, 64, 3, 64, 8, n_blocks=6, block_size=16)
     q = torch.empty(0, 4, 64, dtype=torch.bfloat16, device=DEV)
     assert c.attend(0, q).shape[0] == 0 and c.chunk(0, q, 0).shape[0] == 0
+
+
+def test_a_refused_step_leaves_the_last_one(P):
+    """begin() with lengths that it refuses: the calls go on with the step before."""
+    rng = np.random.default_rng(6)
+    c = P.PagedCache(1, 4, 2, 64, 2, 64, 16, n_blocks=6, block_size=16)
+    c.begin(i32([0, 0]), i32([3, 5]), 8)
+    q, k, v = fill(c, rng, 0, 8, 4, 2, 64, "bf16")
+    want = c.attend(0, q)
+    for bad in (i32([0, 0, 0]), i32([[0, 0]]), i32([0, 0]).long(), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            c.begin(i32([3, 5]), bad, 12)
+    assert torch.equal(c.attend(0, q), want) and c.rows == 8
