@@ -235,6 +235,8 @@ class PagedCache:
     def __init__(self, n_layers, q_heads, kv_heads, head_dim, max_batch, max_len, max_rows, n_blocks, block_size=64, rope=None,
                  layout="half", max_new=1, device="cuda:0"):
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.q_heads, self.kv_heads, self.head_dim, self.max_new = q_heads, kv_heads, head_dim, max_new
         self.block_size, self.n_blocks = block_size, n_blocks
         nbytes = B.heisd_kv4_pool_bytes(n_blocks, block_size, kv_heads, head_dim)

@@ -236,3 +236,14 @@ def test_a_refused_step_leaves_the_last_one(P):
         with pytest.raises(ValueError):
             c.begin(i32([3, 5]), bad, 12)
     assert torch.equal(c.attend(0, q), want) and c.rows == 8
+
+
+def test_a_device_without_a_number(P):
+    """"cuda" is the current device."""
+    rng = np.random.default_rng(1)
+    c = P.PagedCache(1, 4, 2, 64, 1, 64, 8, n_blocks=6, block_size=16, device="cuda")
+    c.begin(i32([0]), i32([5]), 5)
+    q, k, v = fill(c, rng, 0, 5, 4, 2, 64, "bf16")
+    out = c.attend(0, q)
+    torch.cuda.synchronize()
+    check_attend_rows(host(q), host(out), ref.held(host(k)), ref.held(host(v)), 0.125, "bf16")
