@@ -502,7 +502,8 @@ int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *ba
  * left as they were.  What a masked row of k or v holds (infinities, NaN) has no influence.
  *   q, k, v, out  bf16 or fp16 (all the same); q, k, v 16-byte aligned in pointer and strides, out 8
  *   lse           DEVICE f32 [rows][q heads] out, optional     rows, k_rows  rows in q and out, in k and v
- * head_dim 64 or 128.  Scores, sums and the softmax are fp32, probabilities enter the second product in the rows' dtype.
+ * head_dim 64 or 128.  Scores, sums and the softmax are fp32, probabilities enter the second product in the rows' dtype (fp16: off by
+ * half a step, or by 2^-36 of the largest).
  * Errors: EINVAL, EUNSUPPORTED (head_dim, fp32, rows of k or v more than 2^25 elements apart), EHIP.
  */
 int heisd_prompt_attention(const heisd_head_rows *q, const heisd_head_rows *k, const heisd_head_rows *v, const heisd_head_rows *out, float *lse,

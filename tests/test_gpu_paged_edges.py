@@ -247,3 +247,45 @@ def test_a_device_without_a_number(P):
     out = c.attend(0, q)
     torch.cuda.synchronize()
     check_attend_rows(host(q), host(out), ref.held(host(k)), ref.held(host(v)), 0.125, "bf16")
+
+
+# ---- prompts: weights far below the largest ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_many_small_weights_beside_a_large_one(P, dtype, head_dim):
+    """One key takes nearly all of the weight and has values of zero, 65536 others have exp(-17) = 2^-24.5 of its weight each and
+    values of one: the result is their share, 2^-8.5.  A weight is rounded to the rows' dtype relative to itself down to 2^-25 of the
+    largest (fp16 numbers are normal from 2^-14 on and weights are held as 2^11 of their ratio), which leaves the usual tolerance without
+    an absolute term; the sum over so many keys adds (t + 64) 2^-24 of it."""
+    n = 1 << 16
+    q = torch.zeros(3, 2, head_dim, dtype=DTYPES[dtype], device=DEV)
+    q[..., 0] = 1
+    k = torch.zeros(n + 1, 1, head_dim, dtype=DTYPES[dtype], device=DEV)
+    v = torch.ones(n + 1, 1, head_dim, dtype=DTYPES[dtype], device=DEV)
+    for at in (0, 700, n):                                             # met first, in the middle, last
+        k.zero_()
+        v.fill_(1)
+        k[at, 0, 0], v[at] = 17.0, 0
+        out, lse = prompt(P, q, k, v, [0, 3], [0, n + 1], 1.0, False)
+        small = n * math.exp(-17.0)
+        want = np.full((3, 2, head_dim), small / (1 + small))
+        size = np.full((3, 2), 17.0)
+        tol = tolerance(dtype, ref.half_step(dtype), 0.0, head_dim, n + 1, want, want, 0.0, size)
+        assert np.all(np.abs(host(out) - want) <= tol), (at, host(out).min(), host(out).max(), want.max(), tol.max())
+        assert np.all(np.abs(host(lse) - 17.0 - math.log1p(small)) <= lse_tolerance(head_dim, n + 1, 17.0, size))
+
+
+@pytest.mark.parametrize("head_dim,causal", [(64, True), (128, False)])
+def test_fp16_weights_at_their_largest(P, head_dim, causal):
+    """Scores that creep up by less than what moves the maximum, and large values: nothing overflows."""
+    rng = np.random.default_rng(9)
+    n = 900
+    q = torch.zeros(n, 1, head_dim, dtype=torch.float16, device=DEV)
+    q[..., 0] = 1
+    v = (randn(rng, (n, 1, head_dim), "f32") * 9000).clamp(-65000, 65000).to(torch.float16)
+    for step in (0.69 / 64, 1.3 / 64, 5.5 / 64, -0.02):
+        k = torch.zeros(n, 1, head_dim, dtype=torch.float16, device=DEV)
+        k[:, 0, 0] = torch.arange(n, device=DEV) * step
+        out, lse = prompt(P, q, k, v, [0, n], [0, n], 1.0, causal)
+        check_prompt(q, k, v, out, lse, [0, n], [0, n], 1.0, causal, "f16")
