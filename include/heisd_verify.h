@@ -346,7 +346,8 @@ int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int32_t d, con
  * All are asynchronous on `stream`, allocate nothing, keep nothing between calls, and run on the current device, whose memory
  * every DEVICE pointer must belong to.  Results do not depend on timing (no floating-point atomics).  Errors are found before
  * anything is enqueued; heisd_last_error(NULL) has the text.  Calls with no rows return OK and enqueue nothing (heisd_paged_plan always runs);
- * rows that there are none of may lie at NULL.
+ * rows that there are none of may lie at NULL.  More rows than one launch takes are EINVAL: heisd_rope and heisd_kv4_append take 2^24 - 1
+ * and more (narrow rows), heisd_kv4_gather 2^27 - 8, heisd_prompt_attention (rows / 128 + batch) * query heads up to 2^24 - 1.
  */
 #define HEISD_DTYPE_BF16 0
 #define HEISD_DTYPE_F16 1

@@ -31,6 +31,13 @@ static int launched(const char *who) {
   return HEISD_OK;
 }
 
+// A launch has fewer than 2^32 threads in each direction: this many workgroups of 256.
+constexpr int64_t kMostGroups = 0xFFFFFFFFll / 256;
+static int groups_ok(const char *who, int64_t groups) {
+  if (groups <= kMostGroups) return HEISD_OK;
+  return fail(nullptr, HEISD_EINVAL, "%s: too many rows for one call (%lld workgroups, at most %lld)", who, (long long)groups, (long long)kMostGroups);
+}
+
 // ---- block tables, slots and positions ---------------------------------------------------------------------------
 
 // Up to this many packed rows the one workgroup that keeps the books writes the slots as well.  us, one launch / two: 8 requests, 1024 rows
@@ -106,7 +113,7 @@ extern "C" int heisd_rope_table(const heisd_rope_desc *d, double *turns, float *
 template <typename T, int V>
 static void rope_launch(const RopeArgs &a, const heisd_head_rows *q, const heisd_head_rows *q_out, const heisd_head_rows *k,
                         const heisd_head_rows *k_out, bool half, hipStream_t st) {
-  const dim3 grid((a.rows + a.per_group - 1) / a.per_group), block(kRopeThreads);
+  const dim3 grid((unsigned)(((int64_t)a.rows + a.per_group - 1) / a.per_group)), block(kRopeThreads);
   const HeadRows<T> ki = k ? head_rows<T>(*k) : HeadRows<T>{}, ko = k ? head_rows<T>(*k_out) : HeadRows<T>{};
   const HeadRows<T> qi = head_rows<T>(*q), qo = head_rows<T>(*q_out);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs}, kc{ki.p, ki.rs, ki.hs};
@@ -150,6 +157,7 @@ extern "C" int heisd_rope(const double *turns, float magnitude, int32_t rotary_d
   const int64_t per_row = (int64_t)heads * units;
   int64_t group = std::min<int64_t>(kRopePairs / pairs, (rows + 2047) / 2048);
   group = std::max<int64_t>(1, std::min<int64_t>(group, wide ? (int64_t)0xFFFFFFFF / (per_row * per_row) : group));
+  if (const int rc = groups_ok(who, (rows + group - 1) / group)) return rc;
   const RopeArgs a{turns, magnitude, inverse ? -magnitude : magnitude, position, rows, pairs, rest, q->heads, heads, (int)group,
                    FastDiv((uint32_t)units), units, FastDiv((uint32_t)per_row)};
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -205,11 +213,9 @@ static int rows_per_group(int64_t per_row, int rounds) {
 }
 
 template <typename T, int HD>
-static void kv4_append_launch(const Kv4Cache &c, const heisd_head_rows *k, const heisd_head_rows *v, const int32_t *slot, int rows, bool wide,
-                              hipStream_t st) {
-  const int64_t per_row = (int64_t)c.kv_heads * (HD / 8);
-  const int per = rows_per_group(per_row, rows * per_row > (1 << 20) ? 4 : 1);
-  const dim3 grid((rows + per - 1) / per, 2), block(256);
+static void kv4_append_launch(const Kv4Cache &c, const heisd_head_rows *k, const heisd_head_rows *v, const int32_t *slot, int rows, int per,
+                              int64_t per_row, bool wide, hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)rows + per - 1) / per), 2), block(256);
   const HeadRows<T> ki = head_rows<T>(*k), vi = head_rows<T>(*v);
   const HeadRows<const T> kc{ki.p, ki.rs, ki.hs}, vc{vi.p, vi.rs, vi.hs};
   if (wide) kv4_append<T, HD, true><<<grid, block, 0, st>>>(c, kc, vc, slot, rows, per, FastDiv((uint32_t)per_row));
@@ -228,18 +234,21 @@ extern "C" int heisd_kv4_append(const heisd_kv4_desc *cache, const heisd_head_ro
     return fail(nullptr, HEISD_EINVAL, "%s: k and v differ in dtype, or in heads from the cache", who);
   if (rows < 0 || (rows > 0 && !slot)) return fail(nullptr, HEISD_EINVAL, "%s: rows=%d or NULL slots", who, rows);
   if (rows == 0) return HEISD_OK;
+  const int64_t per_row = (int64_t)c.kv_heads * (cache->head_dim / 8);
+  const int per = rows_per_group(per_row, rows * per_row > (1 << 20) ? 4 : 1);
+  if ((rc = groups_ok(who, ((int64_t)rows + per - 1) / per)) != HEISD_OK) return rc;
   const bool wide = rows_aligned(*k, 16) && rows_aligned(*v, 16), big = cache->head_dim == 128;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (k->dtype == HEISD_DTYPE_F32) {
-    if (big) kv4_append_launch<float, 128>(c, k, v, slot, rows, wide, st);
-    else kv4_append_launch<float, 64>(c, k, v, slot, rows, wide, st);
+    if (big) kv4_append_launch<float, 128>(c, k, v, slot, rows, per, per_row, wide, st);
+    else kv4_append_launch<float, 64>(c, k, v, slot, rows, per, per_row, wide, st);
   } else if (k->dtype == HEISD_DTYPE_BF16) {
-    if (big) kv4_append_launch<__bf16, 128>(c, k, v, slot, rows, wide, st);
-    else kv4_append_launch<__bf16, 64>(c, k, v, slot, rows, wide, st);
+    if (big) kv4_append_launch<__bf16, 128>(c, k, v, slot, rows, per, per_row, wide, st);
+    else kv4_append_launch<__bf16, 64>(c, k, v, slot, rows, per, per_row, wide, st);
   } else {
-    if (big) kv4_append_launch<_Float16, 128>(c, k, v, slot, rows, wide, st);
-    else kv4_append_launch<_Float16, 64>(c, k, v, slot, rows, wide, st);
+    if (big) kv4_append_launch<_Float16, 128>(c, k, v, slot, rows, per, per_row, wide, st);
+    else kv4_append_launch<_Float16, 64>(c, k, v, slot, rows, per, per_row, wide, st);
   }
   return launched(who);
 }
@@ -247,7 +256,7 @@ extern "C" int heisd_kv4_append(const heisd_kv4_desc *cache, const heisd_head_ro
 template <typename T, int HD>
 static void kv4_gather_launch(const Kv4Cache &c, const PagedBatch &b, const int32_t *cu_seq, int out_rows, const heisd_head_rows *k,
                               const heisd_head_rows *v, bool wide, hipStream_t st) {
-  const dim3 grid((out_rows + kGatherRows<T> - 1) / kGatherRows<T>, (c.kv_heads + kGatherHeads - 1) / kGatherHeads, 2), block(256);
+  const dim3 grid((unsigned)(((int64_t)out_rows + kGatherRows<T> - 1) / kGatherRows<T>), (c.kv_heads + kGatherHeads - 1) / kGatherHeads, 2), block(256);
   if (wide) kv4_gather<T, HD, true><<<grid, block, 0, st>>>(c, b, cu_seq, out_rows, head_rows<T>(*k), head_rows<T>(*v));
   else kv4_gather<T, HD, false><<<grid, block, 0, st>>>(c, b, cu_seq, out_rows, head_rows<T>(*k), head_rows<T>(*v));
 }
@@ -266,6 +275,8 @@ extern "C" int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_b
     return fail(nullptr, HEISD_EINVAL, "%s: k_out and v_out differ in dtype, or in heads from the cache", who);
   if (out_rows < 0 || !cu_seq) return fail(nullptr, HEISD_EINVAL, "%s: out_rows=%d or NULL cu_seq", who, out_rows);
   if (out_rows == 0) return HEISD_OK;
+  const int per = k_out->dtype == HEISD_DTYPE_F32 ? kGatherRows<float> : kGatherRows<__bf16>;
+  if ((rc = groups_ok(who, ((int64_t)out_rows + per - 1) / per)) != HEISD_OK) return rc;
   const bool wide = rows_aligned(*k_out, 16) && rows_aligned(*v_out, 16), big = cache->head_dim == 128;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
@@ -426,8 +437,8 @@ static int prompt_attention(const char *who, const heisd_head_rows *q, const hei
   if (k->row_stride > (1 << 25) || v->row_stride > (1 << 25))                       // 16 rows apart stays below 2^32 bytes
     return fail(nullptr, HEISD_EUNSUPPORTED, "%s: rows of k or v more than 2^25 elements apart", who);
   const int64_t tiles = (int64_t)rows / kPromptRows + batch;
-  if (tiles * q->heads > 0x7FFFFFFF) return fail(nullptr, HEISD_EINVAL, "%s: rows=%d too many", who, rows);
   if (rows == 0) return HEISD_OK;
+  if ((rc = groups_ok(who, tiles * q->heads)) != HEISD_OK) return rc;
   const PromptArgs a{cu_q, cu_k, seq_len, batch, rows, k_rows, q->heads, k->heads, q->heads / k->heads, (int)tiles,
                      std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f),   // not 0: minus infinity stands for masked scores
                      scale < 0 ? 0x80008000u : 0u, lse};

@@ -77,3 +77,21 @@ def test_rows_that_there_are_none_of_need_no_memory(P):
     refused(P, P.heisd_prompt_attention(rows(P), one, one, rows(P), None, FAKE, FAKE, 2, 4, 1, 128, 0.1, 1, None), P.HEISD_EINVAL, "NULL k")
     refused(P, P.heisd_prompt_attention(none, one, one, none, None, FAKE, FAKE, 2, 4, 0, 128, 0.1, 1, None), P.HEISD_EINVAL, "NULL q")
     refused(P, P.heisd_kv4_append(cache, none, none, FAKE, -1, None), P.HEISD_EINVAL, "rows=-1")
+
+
+def test_more_rows_than_a_launch_takes(P):
+    """2^32 threads or more in one direction of a grid, and counts next to the end of 32 bits."""
+    most, cache = 2 ** 31 - 1, P.heisd_kv4_desc(FAKE, 10, 16, 8, 128)
+    for heads, dim, n in ((1, 256, most), (1, 256, 2 ** 25), (8, 64, most)):      # 256 / pairs rows per workgroup
+        q = rows(P, rs=heads * dim, hs=dim, heads=heads)
+        refused(P, P.heisd_rope(FAKE, 1.0, dim, 0, 0, FAKE, n, dim, q, q, None, None, None), P.HEISD_EINVAL, "too many rows")
+    for heads, n in ((512, most), (512, 2 ** 24), (16, most), (16, 2 ** 28)):
+        c, k = P.heisd_kv4_desc(FAKE, 10, 16, heads, 128), rows(P, heads=heads)
+        refused(P, P.heisd_kv4_append(c, k, k, FAKE, n, None), P.HEISD_EINVAL, "too many rows")
+    b = P.heisd_paged_batch(FAKE, FAKE, FAKE, 2, 4, 6)
+    for dtype, n in ((0, most), (0, 2 ** 28), (2, 2 ** 27)):
+        k = rows(P, dtype=dtype)
+        refused(P, P.heisd_kv4_gather(cache, b, FAKE, n, k, k, None), P.HEISD_EINVAL, "too many rows")
+    for heads, batch, n in ((512, 1, 2 ** 22), (512, 65535, 1), (2, 1, most), (1, 1, most)):
+        q = rows(P, heads=heads)
+        refused(P, P.heisd_prompt_attention(q, q, q, q, None, FAKE, FAKE, batch, n, n, 128, 0.1, 1, None), P.HEISD_EINVAL, "too many rows")
