@@ -354,7 +354,8 @@ int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int32_t d, con
 #define HEISD_DTYPE_F32 2
 
 /* Rows of heads: element i of head h of row r is data[r * row_stride + h * head_stride + i] (strides in elements, at least
- * 0).  Any order of rows and heads fits; the values of a head are adjacent. */
+ * 0).  Any order of rows and heads fits; the values of a head are adjacent.  Rows that are written must not lie on each other (strides below
+ * head_dim, where there is more than one row or head: EINVAL). */
 typedef struct {
   void *data;                       /* DEVICE */
   int64_t row_stride, head_stride;

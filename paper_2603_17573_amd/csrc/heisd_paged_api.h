@@ -24,6 +24,15 @@ static int rows_ok(const char *who, const char *name, const heisd_head_rows *r, 
   return HEISD_OK;
 }
 
+// Rows that are written must not lie on each other (a broadcast tensor's do): workgroups would write, or read and write, the same bytes at
+// once.
+static int apart_ok(const char *who, const char *name, const heisd_head_rows &r, int64_t rows, int head_dim) {
+  if ((rows > 1 && r.row_stride < head_dim) || (r.heads > 1 && r.head_stride < head_dim))
+    return fail(nullptr, HEISD_EINVAL, "%s: rows or heads of %s lie on each other (strides %lld and %lld, head_dim %d)", who, name,
+                (long long)r.row_stride, (long long)r.head_stride, head_dim);
+  return HEISD_OK;
+}
+
 static int launched(const char *who) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(nullptr, HEISD_EHIP, "%s: %s", who, hipGetErrorString(e));
@@ -146,6 +155,7 @@ extern "C" int heisd_rope(const double *turns, float magnitude, int32_t rotary_d
     if (same && (all[i]->row_stride != all[i + 1]->row_stride || all[i]->head_stride != all[i + 1]->head_stride))
       return fail(nullptr, HEISD_EINVAL, "%s: %s is rotated in place with other strides", who, names[i]);
     copies = copies || !same;
+    if (const int rc = apart_ok(who, names[i + 1], *all[i + 1], rows, head_dim)) return rc;
   }
   if (rows == 0) return HEISD_OK;
   if (!position) return fail(nullptr, HEISD_EINVAL, "%s: NULL positions", who);
@@ -275,6 +285,8 @@ extern "C" int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_b
     return fail(nullptr, HEISD_EINVAL, "%s: k_out and v_out differ in dtype, or in heads from the cache", who);
   if (out_rows < 0 || !cu_seq) return fail(nullptr, HEISD_EINVAL, "%s: out_rows=%d or NULL cu_seq", who, out_rows);
   if (out_rows == 0) return HEISD_OK;
+  if ((rc = apart_ok(who, "k_out", *k_out, out_rows, cache->head_dim)) != HEISD_OK) return rc;
+  if ((rc = apart_ok(who, "v_out", *v_out, out_rows, cache->head_dim)) != HEISD_OK) return rc;
   const int per = k_out->dtype == HEISD_DTYPE_F32 ? kGatherRows<float> : kGatherRows<__bf16>;
   if ((rc = groups_ok(who, ((int64_t)out_rows + per - 1) / per)) != HEISD_OK) return rc;
   const bool wide = rows_aligned(*k_out, 16) && rows_aligned(*v_out, 16), big = cache->head_dim == 128;
@@ -362,6 +374,7 @@ extern "C" int heisd_kv4_attention(const heisd_kv4_desc *cache, const heisd_page
   if (!rows_aligned(*q, 16) || !rows_aligned(*out, 8)) return fail(nullptr, HEISD_EINVAL, "%s: q (16 bytes) or out (8 bytes) misaligned", who);
   if (!std::isfinite(scale)) return fail(nullptr, HEISD_EINVAL, "%s: scale %g", who, scale);
   if (b.rows == 0) return HEISD_OK;
+  if ((rc = apart_ok(who, "out", *out, b.rows, cache->head_dim)) != HEISD_OK) return rc;
   const Kv4Plan plan(b.batch, c.kv_heads, q->heads / c.kv_heads, max_q, max_seq, cache->head_dim);
   const size_t need = plan.total;
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned workspace", who);
@@ -439,6 +452,7 @@ static int prompt_attention(const char *who, const heisd_head_rows *q, const hei
   const int64_t tiles = (int64_t)rows / kPromptRows + batch;
   if (rows == 0) return HEISD_OK;
   if ((rc = groups_ok(who, tiles * q->heads)) != HEISD_OK) return rc;
+  if ((rc = apart_ok(who, "out", *out, rows, head_dim)) != HEISD_OK) return rc;
   const PromptArgs a{cu_q, cu_k, seq_len, batch, rows, k_rows, q->heads, k->heads, q->heads / k->heads, (int)tiles,
                      std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f),   // not 0: minus infinity stands for masked scores
                      scale < 0 ? 0x80008000u : 0u, lse};

@@ -289,3 +289,29 @@ def test_fp16_weights_at_their_largest(P, head_dim, causal):
         k[:, 0, 0] = torch.arange(n, device=DEV) * step
         out, lse = prompt(P, q, k, v, [0, n], [0, n], 1.0, causal)
         check_prompt(q, k, v, out, lse, [0, n], [0, n], 1.0, causal, "f16")
+
+
+def test_one_row_or_head_has_any_stride(P):
+    """What lies on nothing else is taken whatever its strides say; so are broadcast inputs."""
+    rng = np.random.default_rng(4)
+    q = randn(rng, (1, 4, 64), "bf16")
+    k = randn(rng, (1, 1, 64), "bf16")
+    one = torch.full((1, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV).as_strided((1, 4, 64), (8, 64, 1))
+    out, lse = prompt(P, q, k, k, [0, 1], [0, 1], 0.125, True, out=one)
+    check_prompt(q, k, k, out, lse, [0, 1], [0, 1], 0.125, True, "bf16")
+    q = randn(rng, (5, 1, 64), "bf16")
+    k = randn(rng, (1, 1, 64), "bf16").expand(40, 1, 64)
+    one = torch.full((5, 1, 64), 7.0, dtype=torch.bfloat16, device=DEV).as_strided((5, 1, 64), (64, 8, 1))
+    out, lse = prompt(P, q, k, k, [0, 5], [0, 40], 0.125, True, out=one)
+    check_prompt(q, k, k, out, lse, [0, 5], [0, 40], 0.125, True, "bf16")
+    x = randn(rng, (1, 2, 64), "f32").expand(6, 2, 64)
+    turns, size = P.rope_table(P.make_rope_desc(64), DEV)
+    y, pos = torch.empty(6, 2, 64, device=DEV), i32(range(6))
+    ok(P, P.heisd_rope(turns.data_ptr(), size, 64, 0, 0, pos.data_ptr(), 6, 64, P.head_rows(x), P.head_rows(y), None, None, stream()))
+    torch.cuda.synchronize()
+    freq, _ = ref.frequencies(64, 10000.0)
+    assert np.abs(host(y) - ref.rope(host(x), np.arange(6), freq, 1.0, "half", False)).max() <= 2.0 ** -20 * float(x.abs().max())
+    with pytest.raises(RuntimeError, match="on each other"):
+        c = P.PagedCache(1, 2, 2, 64, 1, 64, 8, n_blocks=6, block_size=16)
+        c.begin(i32([0]), i32([6]), 6)
+        c.rotate(x, y)

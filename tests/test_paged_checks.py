@@ -95,3 +95,17 @@ def test_more_rows_than_a_launch_takes(P):
     for heads, batch, n in ((512, 1, 2 ** 22), (512, 65535, 1), (2, 1, most), (1, 1, most)):
         q = rows(P, heads=heads)
         refused(P, P.heisd_prompt_attention(q, q, q, q, None, FAKE, FAKE, batch, n, n, 128, 0.1, 1, None), P.HEISD_EINVAL, "too many rows")
+
+
+def test_outputs_on_each_other_are_refused(P):
+    """What a broadcast or overlapping view gives; inputs may be broadcast."""
+    cache, b = P.heisd_kv4_desc(FAKE, 10, 16, 8, 128), P.heisd_paged_batch(FAKE, FAKE, FAKE, 2, 4, 6)
+    good, ws = rows(P, 0x20000), P.heisd_kv4_attention_workspace_bytes(cache, 2, 6, 8, 1, 64)
+    for bad in (rows(P, rs=0), rows(P, hs=0), rows(P, hs=64), rows(P, rs=120, hs=1024), rows(P, rs=0, hs=0)):
+        refused(P, P.heisd_rope(FAKE, 1.0, 64, 0, 0, FAKE, 6, 128, bad, bad, None, None, None), P.HEISD_EINVAL, "q_out lie on each other")
+        refused(P, P.heisd_rope(FAKE, 1.0, 64, 0, 0, FAKE, 6, 128, good, good, bad, bad, None), P.HEISD_EINVAL, "k_out lie on each other")
+        refused(P, P.heisd_kv4_gather(cache, b, FAKE, 6, bad, good, None), P.HEISD_EINVAL, "k_out lie on each other")
+        refused(P, P.heisd_kv4_gather(cache, b, FAKE, 6, good, bad, None), P.HEISD_EINVAL, "v_out lie on each other")
+        refused(P, P.heisd_kv4_attention(cache, b, good, bad, None, 0.1, 1, 64, FAKE, ws, None), P.HEISD_EINVAL, "out lie on each other")
+        refused(P, P.heisd_prompt_attention(good, good, good, bad, None, FAKE, FAKE, 2, 6, 6, 128, 0.1, 1, None), P.HEISD_EINVAL, "out lie on each other")
+        refused(P, P.heisd_paged_prompt_attention(b, good, good, good, bad, None, 128, 0.1, None), P.HEISD_EINVAL, "out lie on each other")
