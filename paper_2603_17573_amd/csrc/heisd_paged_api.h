@@ -318,8 +318,9 @@ struct Kv4Plan {
   int groups(int terms, int head_dim) const {
     return (int)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, kv4_per_unit(head_dim, col_tiles, terms) * kKv4Units));
   }
+  // (With 2^22 columns the products stay below 2^59, and more change nothing: there are 65535 segments already.)
   Kv4Plan(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, int64_t head_dim) {
-    const int64_t cols = max_q * group, lengths = (max_seq + 4 * kKv4Unit - 1) / (4 * kKv4Unit);
+    const int64_t cols = std::min<int64_t>(max_q * group, 1 << 22), lengths = (max_seq + 4 * kKv4Unit - 1) / (4 * kKv4Unit);
     col_tiles = cols > 16 && batch * kv_heads * ((cols + 15) / 16) * lengths >= kv4_per_unit((int)head_dim, 1, 1) * kKv4Units ? 2 : 1;
     segments = (int)std::min<int64_t>(kv_heads * ((cols + 16 * col_tiles - 1) / (16 * col_tiles)), 65535);
     units = batch * segments * ((max_seq + kKv4Unit - 1) / kKv4Unit);

@@ -109,3 +109,16 @@ def test_outputs_on_each_other_are_refused(P):
         refused(P, P.heisd_kv4_attention(cache, b, good, bad, None, 0.1, 1, 64, FAKE, ws, None), P.HEISD_EINVAL, "out lie on each other")
         refused(P, P.heisd_prompt_attention(good, good, good, bad, None, FAKE, FAKE, 2, 6, 6, 128, 0.1, 1, None), P.HEISD_EINVAL, "out lie on each other")
         refused(P, P.heisd_paged_prompt_attention(b, good, good, good, bad, None, 128, 0.1, None), P.HEISD_EINVAL, "out lie on each other")
+
+
+def test_bounds_at_their_largest_do_not_wrap(P):
+    """Workspaces do not shrink where the bounds grow, up to the largest that are taken: 65535 requests, 512 key heads, 2^31 - 1 rows, 2^24
+    tokens, whose product passes 64 bits."""
+    for heads in (1, 512):
+        cache, last = P.heisd_kv4_desc(FAKE, 10, 16, heads, 128), 0
+        for max_q in (1, 33, 1 << 10, 1 << 20, 1 << 27, 1 << 30, 2 ** 31 - 1):
+            n = P.heisd_kv4_attention_workspace_bytes(cache, 65535, 6, 512, max_q, 1 << 24)
+            assert n > 0 and n >= last, (heads, max_q, n, last)
+            last = n
+        # as many workgroups and columns as there ever are
+        assert last == P.heisd_kv4_attention_workspace_bytes(cache, 65535, 6, 512, 64, 1 << 24)
