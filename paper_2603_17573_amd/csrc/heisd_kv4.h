@@ -15,7 +15,8 @@
 // A tile of 16 tokens is what a matrix instruction takes.  Keys are its first operand with tokens as rows: lane l holds token
 // l % 16 and a quarter of the head, contiguous.  Values are the first operand with channels as rows and tokens as the summed
 // index: lane l holds the four tokens 4 * (l / 16) + 0..3 and head_dim / 16 channels, which this order of bytes makes
-// contiguous.  So every lane fetches its part of a tile in one load, a wave's loads are consecutive, and nothing passes through LDS.
+// contiguous.  So the part of a tile that a lane uses lies together, a tile's codes are 1 KB (heads of 128) that follow each other, and the attention
+// brings them into LDS by direct transfers of 16 bytes a lane, from where every lane reads its part at once.
 #pragma once
 #include <type_traits>
 
@@ -230,8 +231,9 @@ struct Kv4Attend {
 // the chip idle, and every chunk begins with three round trips to memory).
 constexpr int kKv4Unit = 128;
 
-// Workgroups of 256 threads that the registers of a compute unit hold: queries of two terms or two column tiles need more of them.
-__host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles, int terms) { return col_tiles == 2 ? 2 : head_dim == 64 ? 4 : 3; }
+// Workgroups of 256 threads that the registers of a compute unit hold: two column tiles need more of them, heads of 64 fewer.  Queries of two terms
+// fit as those of one do.
+__host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles) { return col_tiles == 2 ? 2 : head_dim == 64 ? 4 : 3; }
 
 // What a request asks for: its rows, its tokens, units per segment, units in all.
 struct Kv4Request {
@@ -280,11 +282,11 @@ __device__ __forceinline__ float kv4_weight(float m, float top) { return m == -I
 // 16): scores^T = K q^T (tokens are rows), out^T = V^T p^T.  A lane holds the scores of one column and four tokens of each tile, which are
 // its summed indices of the second product, so the probabilities never leave their lane.  Four waves take pairs of tiles in turn,
 // each with a running maximum and sum of its own, joined through LDS at the end of a segment; what a workgroup has of a segment that it
-// shares with others goes to kv4_join.  A probability enters as a bf16 and a bf16 remainder: one bf16 alone (off by 2^-9, and with few
+// shares with others goes to kv4_join.  A probability enters as a bf16 and a bf16 remainder: one bf16 alone (off by up to 2^-8, and with few
 // large probabilities nothing averages that out) made the results of single tokens 1.4 times as inexact as their own rounding does, for 3 % of the
 // time (59.9 against 62.1 us with 64 contexts of 256 to 8191 tokens).  TERMS 2: so do the queries (fp16 rows, whose 11 bits a bf16 does not hold).
 template <typename T, int HD, int CT, int TERMS>
-__global__ __launch_bounds__(256, kv4_per_unit(HD, CT, TERMS)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
+__global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
   constexpr int W = HD / 32, ND = HD / 16, KJ = HD / 32;        // code dwords, tiles of channels, products per score tile
   constexpr int LD = HD + 4;
   typedef Kv4Slot<HD> Slot;

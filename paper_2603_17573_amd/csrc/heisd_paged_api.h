@@ -315,16 +315,16 @@ struct Kv4Plan {
   int col_tiles, segments;
   int64_t units;
   size_t part_ml, total;
-  int groups(int terms, int head_dim) const {
-    return (int)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, kv4_per_unit(head_dim, col_tiles, terms) * kKv4Units));
+  int groups(int head_dim) const {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, kv4_per_unit(head_dim, col_tiles) * kKv4Units));
   }
   // (With 2^22 columns the products stay below 2^59, and more change nothing: there are 65535 segments already.)
   Kv4Plan(int64_t batch, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, int64_t head_dim) {
     const int64_t cols = std::min<int64_t>(max_q * group, 1 << 22), lengths = (max_seq + 4 * kKv4Unit - 1) / (4 * kKv4Unit);
-    col_tiles = cols > 16 && batch * kv_heads * ((cols + 15) / 16) * lengths >= kv4_per_unit((int)head_dim, 1, 1) * kKv4Units ? 2 : 1;
+    col_tiles = cols > 16 && batch * kv_heads * ((cols + 15) / 16) * lengths >= kv4_per_unit((int)head_dim, 1) * kKv4Units ? 2 : 1;
     segments = (int)std::min<int64_t>(kv_heads * ((cols + 16 * col_tiles - 1) / (16 * col_tiles)), 65535);
     units = batch * segments * ((max_seq + kKv4Unit - 1) / kKv4Unit);
-    const size_t rows = (size_t)2 * groups(1, (int)head_dim) * 16 * col_tiles;       // (one term: the larger grid)
+    const size_t rows = (size_t)2 * groups((int)head_dim) * 16 * col_tiles;
     part_ml = align256(rows * (size_t)head_dim * sizeof(float));
     total = part_ml + align256(rows * 2 * sizeof(float));
   }
@@ -352,7 +352,7 @@ static void kv4_attention_launch(const Kv4Cache &c, const PagedBatch &b, const h
   const HeadRows<T> qi = head_rows<T>(*q), o = head_rows<T>(*out);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
   const dim3 block(256);
-  const int groups = plan.groups(TERMS, HD);
+  const int groups = plan.groups(HD);
   if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
   else kv4_attend<T, HD, 1, TERMS><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
   if (groups > 1) kv4_join<T, HD><<<dim3(plan.segments, b.batch), block, 0, st>>>(c, b, o, a, groups);
