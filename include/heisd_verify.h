@@ -415,7 +415,7 @@ int heisd_paged_plan(const heisd_plan_desc *plan, void *stream);
  *   q -> q_out, k -> k_out (k and k_out may be NULL together): the same heads and dtype (any of the three); in place when the
  *   data pointers and strides are equal, otherwise not overlapping.  16-byte aligned rows (pointers, strides) with parts of a multiple of 16
  *   bytes are fastest; anything else works element by element.
- * head_dim <= 256, rotary_dim even and <= head_dim.  Angles are reduced in 64 bits: exact to fp32 rounding at any position.
+ * head_dim <= 256, rotary_dim even and <= head_dim.  Angles are reduced in 64 bits, sine and cosine are fp32 (to 2^-22), at any position.
  * Errors: EINVAL, EHIP.
  */
 #define HEISD_ROPE_HALF 0
@@ -478,11 +478,12 @@ int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_batch *batch
 /*
  * Attention over that cache: out[r][h] = softmax(scale * q[r][h] . K) V over the tokens that row r sees, with K and V of key head
  * h / (q heads / kv_heads).  Row i of the n rows of request b sees tokens 0 .. seq_len[b] - n + i (the new rows are in the cache
- * already and are its last n tokens).  A row that sees no token gives zeros and lse -inf; packed rows behind the last request are left
+ * already and are its last n tokens).  A row that sees no token (or whose scores are all minus infinity) gives zeros and lse -inf; packed rows behind the last request are left
  * as they were.  One token per request, drafts of several, whole chunks: any number of rows, at its best with few per request.
  *   q, out    bf16 or fp16 (the same); q 16-byte aligned in pointer and strides, out 8
  *   lse       DEVICE f32 [rows][q heads] out, optional (NULL ok): log of the sum of exp(scale * q . K)
  *   max_q     at least the largest number of rows of a request (larger ones are computed too, more slowly)
+ *             rows * query heads: at most 2^31 - 256
  *   max_seq   at least the largest seq_len, at most 2^24; a request with more is treated as one without tokens
  *   workspace DEVICE, 256-byte aligned, heisd_kv4_attention_workspace_bytes(...) bytes (0: invalid sizes) for the same batch, rows,
  *             heads, max_q and max_seq; nothing in it has to be cleared, two calls that may overlap in time need one each

@@ -285,7 +285,8 @@ __device__ __forceinline__ void store_vec_once(T *p, const float *x) {
 }
 
 // (a, b) -> (a cos - b sin, b cos + a sin) for every pair of a row's heads.  The angle is position * frequency, reduced in 64
-// bits to a fraction of a turn (at position 100000 a 32-bit product is off by 1e-3 of a radian), then sine and cosine in 32.
+// bits to a fraction of a turn (at position 100000 a 32-bit product is off by 1e-3 of a radian), then sine and cosine in 32 (off by 2^-22
+// at most: fp32 rows come out 3.7e-8 off, with sines of 64 bits 3.0e-8).
 // They are the same for all heads of a row: a workgroup computes them once into LDS, then every thread turns V pairs at a
 // time, 16 bytes per access.  Bound by memory: 2 * heads * head_dim values per row; 16384 rows of 40 heads of 128 in bf16 (336 MB) take
 // 64 us, 5.3 TB/s, the rate of a large copy.

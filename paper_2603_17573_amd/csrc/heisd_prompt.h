@@ -98,11 +98,11 @@ __device__ __forceinline__ void prompt_rows_plain(HeadRows<const T> q, HeadRows<
 // the row's number so that neither read meets bank conflicts.  SPLIT 2: two such sets of four waves, each with buffers of its own, take every
 // other block of keys and are joined through LDS: half as many steps one after the other, for calls too small to fill the chip.
 // A probability enters the second product as one number of the rows' type.  That rounding is as large as the result's own and makes the error against
-// 64 bits 1.3 times what a single rounding leaves (bf16 prompts 0.0021 for 0.0016, fp16 chunks 0.00028 for 0.00021); a remainder as a second product, as the
+// 64 bits up to 1.3 times what a single rounding leaves (bf16 prompts 0.0021 for 0.0016, fp16 chunks 0.00026 for 0.00021); a remainder as a second product, as the
 // attention over the cache has it, would take 477 us for 363 with packed prompts and 22.4 for 16.7 with chunks, for it is bound by these products.
-// Packed causal prompts of 15805 rows, 32 heads of 128 over 8, bf16: 355 to 367 us (872 to 903 TFLOP/s at 1.95 to 2.1 GHz, which is what the chip
-// clocks meanwhile).  The matrix cores are busy 44 % of that, the vector units (exponents, sums, maxima) about as much, LDS 22 % without
-// conflicts: a wave does one after the other, and the two waves of a SIMD fall into step.
+// Packed causal prompts of 15805 rows, 32 heads of 128 over 8, bf16: 362 to 370 us (866 to 885 TFLOP/s at 1.95 to 2.1 GHz, which is what the chip
+// clocks meanwhile).  The matrix cores are busy 44 % of that, the vector units (exponents, sums, maxima) about as much, LDS 23 % without
+// conflicts: a wave does one after the other, the two waves of a SIMD fall into step, and a quarter of the wave cycles is waiting for data or a barrier.
 template <typename T, int HD, bool CAUSAL, int SPLIT>
 __global__ __launch_bounds__(256 * SPLIT, HD == 64 && SPLIT == 1 ? 3 : 2) void prompt_attend(HeadRows<const T> q, HeadRows<const T> k, HeadRows<const T> v,
                                                                                              HeadRows<T> out, PromptArgs a) {
