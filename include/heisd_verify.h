@@ -484,7 +484,8 @@ int heisd_kv4_gather(const heisd_kv4_desc *cache, const heisd_paged_batch *batch
  *   lse       DEVICE f32 [rows][q heads] out, optional (NULL ok): log of the sum of exp(scale * q . K)
  *   max_q     at least the largest number of rows of a request (larger ones are computed too, more slowly)
  *             rows * query heads: at most 2^31 - 256
- *   max_seq   at least the largest seq_len, at most 2^24; a request with more is treated as one without tokens
+ *   max_seq   at least the largest seq_len, at most 2^24; a request with more (or with more than max_blocks blocks hold) is treated as one without
+ *             tokens
  *   workspace DEVICE, 256-byte aligned, heisd_kv4_attention_workspace_bytes(...) bytes (0: invalid sizes) for the same batch, rows,
  *             heads, max_q and max_seq; nothing in it has to be cleared, two calls that may overlap in time need one each
  * A row that sees a token with a value group that is not finite, or holds magnitudes of 2^127 or more, gives NaN or infinities in that

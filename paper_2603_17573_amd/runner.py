@@ -279,8 +279,8 @@ class PagedCache:
     def _lse(self, t):
         if t is None:
             return None
-        if t.dtype != torch.float32 or tuple(t.shape) != (self.rows, self.q_heads) or not t.is_contiguous() or t.device != self.device:
-            raise ValueError("lse: expected contiguous float32 [%d, %d] on %s, got %s %s strides %s on %s"
+        if t.dtype != torch.float32 or t.dim() != 2 or t.shape[0] < self.rows or t.shape[1] != self.q_heads or not t.is_contiguous() or t.device != self.device:
+            raise ValueError("lse: expected contiguous float32 [%d or more, %d] on %s, got %s %s strides %s on %s"
                              % (self.rows, self.q_heads, self.device, t.dtype, tuple(t.shape), t.stride(), t.device))
         return t.data_ptr()
 

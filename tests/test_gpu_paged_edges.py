@@ -315,3 +315,15 @@ def test_one_row_or_head_has_any_stride(P):
         c = P.PagedCache(1, 2, 2, 64, 1, 64, 8, n_blocks=6, block_size=16)
         c.begin(i32([0]), i32([6]), 6)
         c.rotate(x, y)
+
+
+def test_log_sums_made_for_larger_steps(P):
+    """An lse of more rows than the step has: the first ones are written, the others left."""
+    c = P.PagedCache(1, 4, 2, 64, 2, 64, 16, n_blocks=6, block_size=16)
+    c.begin(i32([0, 0]), i32([3, 5]), 8)
+    q, k, v = fill(c, np.random.default_rng(1), 0, 8, 4, 2, 64, "bf16")
+    for call in (lambda x: c.attend(0, q, lse=x), lambda x: c.prompt(q, k, v, lse=x), lambda x: c.chunk(0, q, 8, lse=x)):
+        exact, more = torch.full((8, 4), 7.0, device=DEV), torch.full((16, 4), 7.0, device=DEV)
+        call(exact), call(more)
+        torch.cuda.synchronize()
+        assert torch.equal(more[:8], exact) and bool((more[8:] == 7).all()) and bool((exact != 7).all())
