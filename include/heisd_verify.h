@@ -523,6 +523,129 @@ int heisd_paged_prompt_attention(const heisd_paged_batch *batch, const heisd_hea
                                  const heisd_head_rows *out, float *lse, int32_t head_dim, float scale, void *stream);
 
 /*
+ * Requests that continue others: several continuations of one context (beams, candidates of an episode), and contexts that are kept small.
+ * Used together, per step:
+ *   heisd_beam_select -> heisd_paged_reorder -> heisd_kv4_copy (all layers) -> heisd_paged_plan -> heisd_paged_offset, then per layer
+ *   heisd_rope -> heisd_kv4_append -> heisd_kv4_shared_attention -> heisd_kv4_weigh, and from time to time heisd_kv4_evict (all layers).
+ * What is said above of the calls on paged requests holds for these, too.
+ *
+ * Beam search's choice: of every group of `beams` beams the `width` best continuations, by score / length^length_power.
+ *   score of token v behind beam i: score_in[i] + logits[i][v] - log(sum over v of exp(logits[i][v])), in 64 bits, rounded once in score_out;
+ *   its length is length_in[i] + 1.  A beam with done_in != 0 goes on once, as it is (score, length), in the place of end_token.
+ *   Equal ones: the lowest beam, then the lowest token.  NaN and minus infinity are no continuations (and add nothing to the sum); a
+ *   beam whose score is minus infinity or NaN has none, nor has one with a logit of plus infinity.  Where there are fewer than `width`: beam and token -1, score
+ *   minus infinity, length 0, done 1.
+ *   logits     DEVICE [groups * beams][vocab], any dtype, row_stride elements apart (at any address that suits the dtype)
+ *   score_in   DEVICE f32 [groups * beams]      score_out, beam, token [groups][width] out (beam: 0 .. beams - 1)
+ *   length_in, length_out  DEVICE i32, both or neither (then lengths are 1 and length_power has to be 0)
+ *   done_in, done_out      DEVICE i32, both or neither (then end_token has to be -1); done_out: was done, or token is end_token (-1: none is)
+ *   parent     DEVICE i32 out, optional: parent[first + group * stride + n] = first + group * stride + beam (-1: none), for heisd_paged_reorder
+ *              where a group's requests follow each other; other entries stay as they are
+ * score, length and done may be in place where width is beams; other buffers may not overlap.
+ * beams, width 1 .. 64, vocab 1 .. 524280, 65535 beams in all.  Two calls that may overlap in time need a workspace each; nothing in it has to be
+ * cleared.  Errors: EINVAL, ENOMEM (workspace), EHIP.
+ */
+typedef struct {
+  const void *logits;
+  int64_t row_stride;
+  int32_t dtype, groups, beams, width, vocab, end_token;
+  double length_power;
+  const float *score_in;
+  const int32_t *length_in, *done_in;
+  float *score_out;
+  int32_t *beam, *token, *length_out, *done_out, *parent;
+  int32_t first, stride;
+} heisd_beam_desc;
+size_t heisd_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t width, int32_t vocab);
+int heisd_beam_select(const heisd_beam_desc *beams, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Requests go on as continuations of others: request b continues what was request parent[b] (outside 0 .. batch - 1: it ends).  One continuation of a
+ * request takes its blocks over - the request's own (parent[b] = b), else the lowest; nothing of it is copied.  Blocks of requests that nobody
+ * continues go on top of the free ones (in request and table order; trim != 0: also those behind the blocks that len_in[b] tokens need, of
+ * every request).  The other continuations take the blocks that their tokens need from there, in request order, first come, first served as in
+ * heisd_paged_plan; one that gets none, or whose tokens do not fit max_blocks blocks, ends (length -1).
+ *   parent, len_in, owned_in  DEVICE i32 [batch]     len_in: cached tokens (negative ones are passed on)
+ *   table_in                  DEVICE i32 [batch][max_blocks]
+ *   len_out, owned_out        DEVICE i32 [batch] out; table_out [batch][max_blocks] out: -1 behind the owned blocks
+ *   copy_from                 DEVICE i32 [batch] out: the request (in the new order) whose tokens have to be copied, -1: none
+ *   free_ids, free_count_in, free_count_out: as in heisd_paged_plan
+ * free_count_out may be free_count_in; no other buffers may overlap.  With parent[b] = b for all b and trim, blocks that an eviction
+ * left empty are given back.
+ * Errors: EINVAL, EHIP.
+ */
+typedef struct {
+  int32_t batch, block_size, max_blocks, n_blocks, trim;
+  const int32_t *parent, *len_in, *owned_in, *table_in;
+  int32_t *len_out, *owned_out, *table_out, *copy_from, *free_ids;
+  const int32_t *free_count_in;
+  int32_t *free_count_out;
+} heisd_reorder_desc;
+int heisd_paged_reorder(const heisd_reorder_desc *reorder, void *stream);
+
+/*
+ * heisd_kv4_copy copies the tokens 0 .. seq_len[b] - 1 of request copy_from[b] to request b (both by the batch's block table), in every layer, for every b with
+ * copy_from[b] in 0 .. batch - 1 and not b.  No block may be copied to twice, nor from and to.  Blocks outside the pool are left out.
+ *   cache      the first layer; layer n's pool is layer_bytes * n bytes behind (a multiple of 16; not used for one layer)
+ *   weight     DEVICE f32 [layers][n_blocks][kv_heads][block_size], optional: weights of tokens (below) that are copied with them
+ *   max_seq    at least the longest of those requests; what lies behind is not copied.  cu_rows of the batch may be NULL.
+ * heisd_paged_offset adds offset[b] to the positions of request b's rows (behind a shared prefix: its length; after evictions: the number of tokens
+ * that are gone), so that heisd_rope turns them as if nothing was missing.  Negative positions stay; sums outside 0 .. 2^31 - 1 become -1.
+ *   offset     DEVICE i32 [batch]       position  DEVICE i32 [rows] in, out
+ * Errors: EINVAL, EUNSUPPORTED (head_dim), EHIP.
+ */
+int heisd_kv4_copy(const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes, const heisd_paged_batch *batch, const int32_t *copy_from,
+                   float *weight, int32_t max_seq, void *stream);
+int heisd_paged_offset(const heisd_paged_batch *batch, const int32_t *offset, int32_t *position, void *stream);
+
+/*
+ * Attention over a prefix that several requests share: every row of the requests first[g] .. first[g + 1] - 1 sees all tokens of request prefix[g], and
+ * behind them its own request's as in heisd_kv4_attention (whose other arguments, limits and results these are).  A prefix is read once for all of its group's
+ * rows.  It is a request of the same batch, usually one without rows in this step.
+ *   first, prefix   DEVICE i32 [groups + 1], [groups].  A group describes nothing (its requests see their own tokens alone) where first decreases or leaves
+ *                   0 .. batch, or where prefix is not a request, one of the group itself, one without tokens, or one of more than max_prefix tokens.
+ *                   Entries of first must not decrease between two groups that describe something.
+ *   max_rows        at least the largest number of rows of a group; max_prefix (at most 2^24) at least the longest prefix
+ *   groups          may be 0 or the description NULL: nobody shares anything
+ * Requests with a negative seq_len (or one above max_seq) see nothing, their prefix neither: zeros and lse -inf.
+ */
+typedef struct {
+  const int32_t *first, *prefix;
+  int32_t groups, max_rows, max_prefix;
+} heisd_prefix_groups;
+size_t heisd_kv4_shared_attention_workspace_bytes(const heisd_kv4_desc *cache, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_q,
+                                                  int32_t max_seq, const heisd_prefix_groups *groups);
+int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_prefix_groups *groups,
+                               const heisd_head_rows *q, const heisd_head_rows *out, float *lse, float scale, int32_t max_q, int32_t max_seq,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The attention weight that cached tokens receive, and eviction of those that received least.  Weights are f32 [n_blocks][kv_heads][block_size], a token's where its
+ * cell is.
+ * heisd_kv4_weigh: weight_out = decay * weight_in + the sum, over the rows that see the token (its request's, or those of the groups whose prefix its
+ * request is) and the query heads of the key head, of exp(scale * q . k - lse), for every token of every request.  The last n tokens of a request
+ * with n rows are new: their weight_in is not read and counts as zero, so nothing has to be cleared.
+ *   lse        DEVICE f32 [rows][q heads], as heisd_kv4_attention or heisd_kv4_shared_attention of the same rows gave it; -inf: the row adds nothing
+ *   weight_in, weight_out   the same buffer or different ones
+ *   max_seq    as in the attention: requests of more tokens have no weights written (up to max_prefix if that is larger, for their groups' rows)
+ *   groups     optional
+ * Scores and sums are fp32; queries enter the matrix products as in heisd_kv4_attention.
+ * heisd_kv4_evict cuts every request of more than keep[b] tokens to keep[b] (negative: it stays as it is): the last `recent` tokens stay (at most keep[b]), and of those before
+ * them the keep[b] - recent heaviest, in each layer and head for itself (equal ones: the lowest token first; NaN is the lightest).  Tokens that stay and
+ * lie behind the first keep[b] - recent places fill, in order, the places that get free, and the last ones follow in order.  Attention over
+ * the whole cache does not depend on the order.  Blocks stay with their requests (heisd_paged_reorder with trim gives them back).
+ *   cache, layers, layer_bytes   as in heisd_kv4_copy     keep  DEVICE i32 [batch]      seq_out  DEVICE i32 [batch] out, not seq_len
+ *   weight_in, weight_out        DEVICE f32 [layers][n_blocks][kv_heads][block_size], the same buffer or different ones: weights move with their tokens
+ *   max_seq    at most 2^24; requests of more tokens, or with blocks outside the pool, stay as they are
+ * No two requests may have a block in common.  cu_rows of the batch may be NULL.
+ * Errors: EINVAL, EUNSUPPORTED (head_dim, fp32 rows), EHIP.
+ */
+int heisd_kv4_weigh(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_prefix_groups *groups, const heisd_head_rows *q,
+                    const float *lse, float scale, float decay, const float *weight_in, float *weight_out, int32_t max_seq, void *stream);
+int heisd_kv4_evict(const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes, const heisd_paged_batch *batch, const int32_t *keep,
+                    int32_t recent, const float *weight_in, float *weight_out, int32_t *seq_out, int32_t max_seq, void *stream);
+
+/*
  * Per-kernel timing for measurement runs (not part of the method).  With profiling enabled,
  * heisd_verify_step brackets every kernel launch with HIP events on the caller's stream;
  * heisd_verify_profile_read waits for the recorded events, adds the elapsed milliseconds

@@ -63,6 +63,23 @@ class heisd_paged_batch(Structure):
     _fields_ = [(n, c_void_p) for n in ("block_table", "seq_len", "cu_rows")] + [(n, c_int32) for n in ("batch", "max_blocks", "rows")]
 
 
+class heisd_beam_desc(Structure):
+    _fields_ = [("logits", c_void_p), ("row_stride", ctypes.c_int64)] + \
+        [(n, c_int32) for n in ("dtype", "groups", "beams", "width", "vocab", "end_token")] + [("length_power", ctypes.c_double)] + \
+        [(n, c_void_p) for n in ("score_in", "length_in", "done_in", "score_out", "beam", "token", "length_out", "done_out", "parent")] + \
+        [("first", c_int32), ("stride", c_int32)]
+
+
+class heisd_reorder_desc(Structure):
+    _fields_ = [(n, c_int32) for n in ("batch", "block_size", "max_blocks", "n_blocks", "trim")] + \
+        [(n, c_void_p) for n in ("parent", "len_in", "owned_in", "table_in", "len_out", "owned_out", "table_out", "copy_from", "free_ids",
+                                 "free_count_in", "free_count_out")]
+
+
+class heisd_prefix_groups(Structure):
+    _fields_ = [("first", c_void_p), ("prefix", c_void_p)] + [(n, c_int32) for n in ("groups", "max_rows", "max_prefix")]
+
+
 HEISD_DTYPE_BF16, HEISD_DTYPE_F16, HEISD_DTYPE_F32 = 0, 1, 2
 ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
@@ -140,6 +157,27 @@ def load():
         lib.heisd_prompt_attention.restype = ctypes.c_int
         lib.heisd_paged_prompt_attention.argtypes = [paged_p, rows_p, rows_p, rows_p, rows_p, c_void_p, c_int32, c_float, c_void_p]
         lib.heisd_paged_prompt_attention.restype = ctypes.c_int
+        groups_p = POINTER(heisd_prefix_groups)
+        lib.heisd_beam_select_workspace_bytes.argtypes = [c_int32, c_int32, c_int32, c_int32]
+        lib.heisd_beam_select_workspace_bytes.restype = c_size_t
+        lib.heisd_beam_select.argtypes = [POINTER(heisd_beam_desc), c_void_p, c_size_t, c_void_p]
+        lib.heisd_beam_select.restype = ctypes.c_int
+        lib.heisd_paged_reorder.argtypes = [POINTER(heisd_reorder_desc), c_void_p]
+        lib.heisd_paged_reorder.restype = ctypes.c_int
+        lib.heisd_kv4_copy.argtypes = [kv4_p, c_int32, ctypes.c_int64, paged_p, c_void_p, c_void_p, c_int32, c_void_p]
+        lib.heisd_kv4_copy.restype = ctypes.c_int
+        lib.heisd_paged_offset.argtypes = [paged_p, c_void_p, c_void_p, c_void_p]
+        lib.heisd_paged_offset.restype = ctypes.c_int
+        lib.heisd_kv4_shared_attention_workspace_bytes.argtypes = [kv4_p, c_int32, c_int32, c_int32, c_int32, c_int32, groups_p]
+        lib.heisd_kv4_shared_attention_workspace_bytes.restype = c_size_t
+        lib.heisd_kv4_shared_attention.argtypes = [kv4_p, paged_p, groups_p, rows_p, rows_p, c_void_p, c_float, c_int32, c_int32, c_void_p,
+                                                   c_size_t, c_void_p]
+        lib.heisd_kv4_shared_attention.restype = ctypes.c_int
+        lib.heisd_kv4_weigh.argtypes = [kv4_p, paged_p, groups_p, rows_p, c_void_p, c_float, c_float, c_void_p, c_void_p, c_int32, c_void_p]
+        lib.heisd_kv4_weigh.restype = ctypes.c_int
+        lib.heisd_kv4_evict.argtypes = [kv4_p, c_int32, ctypes.c_int64, paged_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32,
+                                        c_void_p]
+        lib.heisd_kv4_evict.restype = ctypes.c_int
         lib.heisd_free.argtypes = [c_void_p]
         lib.heisd_free.restype = None
         lib.heisd_verify_profile_enable.argtypes = [c_void_p, ctypes.c_int]
@@ -309,6 +347,47 @@ def heisd_prompt_attention(q: heisd_head_rows, k: heisd_head_rows, v: heisd_head
 def heisd_paged_prompt_attention(batch: heisd_paged_batch, q: heisd_head_rows, k: heisd_head_rows, v: heisd_head_rows, out: heisd_head_rows, lse,
                                  head_dim, scale, stream) -> int:
     return load().heisd_paged_prompt_attention(_ref(batch), _ref(q), _ref(k), _ref(v), _ref(out), lse, head_dim, scale, stream)
+
+
+def heisd_beam_select_workspace_bytes(groups, beams, width, vocab) -> int:
+    return int(load().heisd_beam_select_workspace_bytes(groups, beams, width, vocab))
+
+
+def heisd_beam_select(beams: heisd_beam_desc, workspace, workspace_bytes, stream) -> int:
+    return load().heisd_beam_select(_ref(beams), workspace, workspace_bytes, stream)
+
+
+def heisd_paged_reorder(reorder: heisd_reorder_desc, stream) -> int:
+    return load().heisd_paged_reorder(_ref(reorder), stream)
+
+
+def heisd_kv4_copy(cache: heisd_kv4_desc, layers, layer_bytes, batch: heisd_paged_batch, copy_from, weight, max_seq, stream) -> int:
+    """copy_from, weight: integer device addresses (weight may be None)."""
+    return load().heisd_kv4_copy(_ref(cache), layers, layer_bytes, _ref(batch), copy_from, weight, max_seq, stream)
+
+
+def heisd_paged_offset(batch: heisd_paged_batch, offset, position, stream) -> int:
+    return load().heisd_paged_offset(_ref(batch), offset, position, stream)
+
+
+def heisd_kv4_shared_attention_workspace_bytes(cache: heisd_kv4_desc, batch, rows, q_heads, max_q, max_seq, groups: heisd_prefix_groups) -> int:
+    return int(load().heisd_kv4_shared_attention_workspace_bytes(_ref(cache), batch, rows, q_heads, max_q, max_seq, _ref(groups)))
+
+
+def heisd_kv4_shared_attention(cache: heisd_kv4_desc, batch: heisd_paged_batch, groups: heisd_prefix_groups, q: heisd_head_rows,
+                               out: heisd_head_rows, lse, scale, max_q, max_seq, workspace, workspace_bytes, stream) -> int:
+    return load().heisd_kv4_shared_attention(_ref(cache), _ref(batch), _ref(groups), _ref(q), _ref(out), lse, scale, max_q, max_seq, workspace,
+                                             workspace_bytes, stream)
+
+
+def heisd_kv4_weigh(cache: heisd_kv4_desc, batch: heisd_paged_batch, groups: heisd_prefix_groups, q: heisd_head_rows, lse, scale, decay, weight_in,
+                    weight_out, max_seq, stream) -> int:
+    return load().heisd_kv4_weigh(_ref(cache), _ref(batch), _ref(groups), _ref(q), lse, scale, decay, weight_in, weight_out, max_seq, stream)
+
+
+def heisd_kv4_evict(cache: heisd_kv4_desc, layers, layer_bytes, batch: heisd_paged_batch, keep, recent, weight_in, weight_out, seq_out, max_seq,
+                    stream) -> int:
+    return load().heisd_kv4_evict(_ref(cache), layers, layer_bytes, _ref(batch), keep, recent, weight_in, weight_out, seq_out, max_seq, stream)
 
 
 def heisd_free(ctx) -> None:

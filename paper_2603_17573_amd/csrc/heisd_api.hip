@@ -27,6 +27,9 @@
 #include "heisd_paged.h"
 #include "heisd_kv4.h"
 #include "heisd_prompt.h"
+#include "heisd_beam.h"
+#include "heisd_keep.h"
+#include "heisd_shared.h"
 
 using namespace heisd;
 
@@ -2205,6 +2208,7 @@ extern "C" int heisd_retrieve_topk_static(const void *db, int64_t n_vectors, int
 }
 
 #include "heisd_paged_api.h"
+#include "heisd_branch_api.h"
 
 // ---- reference measurements (not part of the method) ---------------------------------------------
 

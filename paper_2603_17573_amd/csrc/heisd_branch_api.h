@@ -1,0 +1,295 @@
+// C ABI of the operators on requests that continue others: argument checks and launches (part of heisd_api.hip).
+#pragma once
+
+// ---- the next beams --------------------------------------------------------------------------------------------------
+
+// A lane of beam_join takes a chunk; a row's address may cut its first vector, so that it needs up to a vector more.
+constexpr int kBeamMostVocab = kBeamMost * kBeamChunk - 8;
+static int beam_chunks(int32_t vocab) { return (vocab + 7 + kBeamChunk - 1) / kBeamChunk; }
+
+static int beam_sizes_ok(const char *who, int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
+  if (groups < 1 || groups > 65535 || beams < 1 || beams > kBeamMost || width < 1 || width > kBeamMost || vocab < 1 || vocab > kBeamMostVocab)
+    return fail(nullptr, HEISD_EINVAL, "%s: groups=%d (1..65535) beams=%d width=%d (1..%d) vocab=%d (1..%d)", who, groups, beams, width, kBeamMost,
+                vocab, kBeamMostVocab);
+  if ((int64_t)groups * beams > 65535) return fail(nullptr, HEISD_EINVAL, "%s: %lld beams in all (at most 65535)", who, (long long)groups * beams);
+  return HEISD_OK;
+}
+struct BeamLayout {
+  size_t value, index, total;
+  BeamLayout(int64_t rows, int chunks, int width) {
+    value = align256((size_t)rows * chunks * 2 * sizeof(float));
+    index = value + align256((size_t)rows * chunks * width * sizeof(float));
+    total = index + align256((size_t)rows * chunks * width * sizeof(int32_t));
+  }
+};
+
+extern "C" size_t heisd_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
+  if (beam_sizes_ok("beam_select_workspace_bytes", groups, beams, width, vocab) != HEISD_OK) return 0;
+  return BeamLayout((int64_t)groups * beams, beam_chunks(vocab), width).total;
+}
+
+template <typename T>
+static void beam_launch(const BeamArgs &a, hipStream_t st) {
+  beam_rows<T><<<dim3(a.chunks, a.groups * a.beams), dim3(256), 0, st>>>(a);
+  beam_join<4><<<dim3(a.groups), dim3(256), 0, st>>>(a);
+}
+
+extern "C" int heisd_beam_select(const heisd_beam_desc *d, void *workspace, size_t workspace_bytes, void *stream) {
+  const char *who = "beam_select";
+  if (!d) return fail(nullptr, HEISD_EINVAL, "%s: NULL description", who);
+  if (const int rc = beam_sizes_ok(who, d->groups, d->beams, d->width, d->vocab)) return rc;
+  const size_t size = dtype_bytes(d->dtype);
+  if (!size) return fail(nullptr, HEISD_EINVAL, "%s: logits have unknown dtype %d", who, d->dtype);
+  if (!d->logits || (uintptr_t)d->logits % size || d->row_stride < 0)
+    return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned logits, or a negative stride", who);
+  if (!d->score_in || !d->score_out || !d->beam || !d->token) return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer", who);
+  if (!d->length_in != !d->length_out || !d->done_in != !d->done_out)
+    return fail(nullptr, HEISD_EINVAL, "%s: length_in without length_out, done_in without done_out, or the other way round", who);
+  if (d->end_token < -1 || d->end_token >= d->vocab || (d->end_token >= 0 && !d->done_in))
+    return fail(nullptr, HEISD_EINVAL, "%s: end_token %d (-1..vocab - 1; with done_in)", who, d->end_token);
+  if (!std::isfinite(d->length_power) || (d->length_power != 0 && !d->length_in))
+    return fail(nullptr, HEISD_EINVAL, "%s: length_power %g (with length_in)", who, d->length_power);
+  if (d->parent && (d->first < 0 || d->stride < d->width || d->first + (int64_t)d->groups * d->stride > 0x7FFFFFFF))
+    return fail(nullptr, HEISD_EINVAL, "%s: parents from %d on, %d apart", who, d->first, d->stride);
+  const void *in[3] = {d->score_in, d->length_in, d->done_in}, *out[3] = {d->score_out, d->length_out, d->done_out};
+  for (int i = 0; i < 3; ++i)
+    if (in[i] && in[i] == out[i] && d->width != d->beams) return fail(nullptr, HEISD_EINVAL, "%s: in place with another number of beams", who);
+  const int chunks = beam_chunks(d->vocab);
+  const BeamLayout lay((int64_t)d->groups * d->beams, chunks, d->width);
+  if (!workspace || ((uintptr_t)workspace & 255)) return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned workspace", who);
+  if (workspace_bytes < lay.total) return fail(nullptr, HEISD_ENOMEM, "%s: workspace %zu bytes < %zu needed", who, workspace_bytes, lay.total);
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  const BeamArgs a{d->logits, d->row_stride, d->groups, d->beams, d->width, d->vocab, chunks, d->end_token, d->length_power, d->score_in, d->length_in,
+                   d->done_in, d->score_out, d->beam, d->token, d->length_out, d->done_out, d->parent, d->first, d->stride,
+                   reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + lay.value), reinterpret_cast<int32_t *>(ws + lay.index)};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (d->dtype == HEISD_DTYPE_F32) beam_launch<float>(a, st);
+  else if (d->dtype == HEISD_DTYPE_BF16) beam_launch<__bf16>(a, st);
+  else beam_launch<_Float16>(a, st);
+  return launched(who);
+}
+
+// ---- requests that continue others --------------------------------------------------------------------------------------
+
+extern "C" int heisd_paged_reorder(const heisd_reorder_desc *d, void *stream) {
+  const char *who = "paged_reorder";
+  if (!d) return fail(nullptr, HEISD_EINVAL, "%s: NULL description", who);
+  if (d->batch < 1 || d->batch > 65535) return fail(nullptr, HEISD_EINVAL, "%s: batch=%d (1..65535)", who, d->batch);
+  if (d->block_size < 1 || d->n_blocks < 1 || d->max_blocks < 1 || d->max_blocks > (1 << 20) ||
+      (int64_t)d->n_blocks * d->block_size > 0x7FFFFFFF || (int64_t)d->max_blocks * d->block_size > 0x7FFFFFFF)
+    return fail(nullptr, HEISD_EINVAL, "%s: block_size=%d n_blocks=%d max_blocks=%d (at most 2^31 - 1 slots, 2^20 blocks per request)", who,
+                d->block_size, d->n_blocks, d->max_blocks);
+  if (!d->parent || !d->len_in || !d->owned_in || !d->table_in || !d->len_out || !d->owned_out || !d->table_out || !d->copy_from || !d->free_ids ||
+      !d->free_count_in || !d->free_count_out)
+    return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer", who);
+  if (d->len_out == d->len_in || d->owned_out == d->owned_in || d->table_out == d->table_in)
+    return fail(nullptr, HEISD_EINVAL, "%s: lengths, owned blocks or tables in place", who);
+  const ReorderArgs a{d->batch, d->block_size, d->max_blocks, d->n_blocks, d->trim != 0, d->parent, d->len_in, d->owned_in, d->table_in, d->len_out,
+                      d->owned_out, d->table_out, d->copy_from, d->free_ids, d->free_count_in, d->free_count_out};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (d->batch <= 64 && (int64_t)d->batch * d->max_blocks <= 4096) reorder_books<4, true><<<dim3(1), dim3(256), 0, st>>>(a);
+  else {
+    if (d->batch <= 256) reorder_books<4, false><<<dim3(1), dim3(256), 0, st>>>(a);
+    else reorder_books<16, false><<<dim3(1), dim3(1024), 0, st>>>(a);
+    reorder_tables<<<dim3((d->batch + 3) / 4), dim3(256), 0, st>>>(a);
+  }
+  return launched(who);
+}
+
+// Layers of a cache: `layer_bytes` from one pool to the next.
+static int layers_ok(const char *who, const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes) {
+  if (layers < 1 || layers > 65535) return fail(nullptr, HEISD_EINVAL, "%s: %d layers (1..65535)", who, layers);
+  const size_t pool = heisd_kv4_pool_bytes(cache->n_blocks, cache->block_size, cache->kv_heads, cache->head_dim);
+  if (layers > 1 && (layer_bytes < (int64_t)pool || (layer_bytes & 15) || layer_bytes > (int64_t)1 << 42))
+    return fail(nullptr, HEISD_EINVAL, "%s: layers %lld bytes apart (at least %zu, a multiple of 16)", who, (long long)layer_bytes, pool);
+  return HEISD_OK;
+}
+static int64_t kv4_weights(const Kv4Cache &c) { return (int64_t)c.n_blocks * c.kv_heads * c.block_size; }
+
+extern "C" int heisd_kv4_copy(const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes, const heisd_paged_batch *batch, const int32_t *copy_from,
+                              float *weight, int32_t max_seq, void *stream) {
+  const char *who = "kv4_copy";
+  Kv4Cache c;
+  PagedBatch b;
+  int rc = kv4_ok(who, cache, &c);
+  if (rc == HEISD_OK) rc = batch_ok(who, batch, false, &b);
+  if (rc == HEISD_OK) rc = layers_ok(who, cache, layers, layer_bytes);
+  if (rc != HEISD_OK) return rc;
+  if (!copy_from || max_seq < 1) return fail(nullptr, HEISD_EINVAL, "%s: NULL copy_from or max_seq=%d", who, max_seq);
+  const int64_t blocks = std::min<int64_t>(((int64_t)max_seq + c.block_size - 1) / c.block_size, b.max_blocks);
+  const int64_t pieces = c.kv_heads * (c.cell / 16), per_block = (pieces + 256 * kCopyPieces - 1) / (256 * kCopyPieces);
+  if ((rc = groups_ok(who, blocks * per_block)) != HEISD_OK) return rc;
+  const CopyArgs a{copy_from, weight, layer_bytes, kv4_weights(c), max_seq, cache->head_dim};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  kv4_copy_blocks<<<dim3((unsigned)(blocks * per_block), b.batch, layers), dim3(256), 0, st>>>(c, b, a, (int)per_block);
+  return launched(who);
+}
+
+// ---- attention over a shared prefix ---------------------------------------------------------------------------------------
+
+static int groups_desc_ok(const char *who, const heisd_prefix_groups *g, PrefixGroups *out) {
+  if (!g || !g->groups) {                            // nobody shares anything
+    *out = PrefixGroups{nullptr, nullptr, 0, 0, 0};
+    return HEISD_OK;
+  }
+  if (!g->first || !g->prefix) return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer of the groups", who);
+  if (g->groups < 0 || g->groups > 65535 || g->max_rows < 1 || g->max_prefix < 1 || g->max_prefix > (1 << 24))
+    return fail(nullptr, HEISD_EINVAL, "%s: groups=%d (0..65535) max_rows=%d max_prefix=%d (1..2^24)", who, g->groups, g->max_rows, g->max_prefix);
+  *out = PrefixGroups{g->first, g->prefix, g->groups, g->max_rows, g->max_prefix};
+  return HEISD_OK;
+}
+
+// As Kv4Plan, with the groups' work beside the requests'.
+struct SharedPlan {
+  int col_tiles;
+  int64_t groups;
+  size_t part_ml, whole, whole_ml, total;
+  SharedPlan(int64_t batch, int64_t rows, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, const PrefixGroups &p, int64_t head_dim) {
+    const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::max<int64_t>(own_cols, std::min<int64_t>((int64_t)p.max_rows * group, 1 << 22));
+    col_tiles = cols > 16 ? 2 : 1;
+    const int64_t tile = 16 * col_tiles, most = kv4_per_unit((int)head_dim, col_tiles) * kKv4Units;
+    const int64_t own = batch * std::min<int64_t>(kv_heads * ((own_cols + tile - 1) / tile), 65535) * ((max_seq + kKv4Unit - 1) / kKv4Unit);
+    const int64_t shared = (int64_t)p.groups * std::min<int64_t>(kv_heads * ((cols + tile - 1) / tile), 65535) * ((p.max_prefix + kKv4Unit - 1) / kKv4Unit);
+    groups = std::max<int64_t>(1, std::min<int64_t>((own + shared + 1) / 2, most));
+    part_ml = align256((size_t)2 * groups * tile * head_dim * sizeof(float));
+    whole = part_ml + align256((size_t)2 * groups * tile * 2 * sizeof(float));
+    whole_ml = whole + align256((size_t)2 * rows * group * kv_heads * head_dim * sizeof(float));
+    total = whole_ml + align256((size_t)2 * rows * group * kv_heads * 2 * sizeof(float));
+  }
+};
+
+extern "C" size_t heisd_kv4_shared_attention_workspace_bytes(const heisd_kv4_desc *cache, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_q,
+                                                             int32_t max_seq, const heisd_prefix_groups *groups) {
+  const char *who = "kv4_shared_attention_workspace_bytes";
+  PrefixGroups p;
+  if (!cache || !kv4_shape_ok(cache->n_blocks, cache->block_size, cache->kv_heads, cache->head_dim) || batch < 1 || batch > 65535 ||
+      kv4_attention_sizes_ok(who, cache->kv_heads, q_heads, rows, max_q, max_seq) != HEISD_OK || groups_desc_ok(who, groups, &p) != HEISD_OK)
+    return 0;
+  return SharedPlan(batch, rows, cache->kv_heads, q_heads / cache->kv_heads, max_q, max_seq, p, cache->head_dim).total;
+}
+
+template <typename T, int HD, int TERMS>
+static void kv4_shared_launch(const Kv4Cache &c, const PagedBatch &b, const heisd_head_rows *q, const heisd_head_rows *out, const Kv4SharedAttend &a,
+                              const SharedPlan &plan, int max_q, hipStream_t st) {
+  const HeadRows<T> qi = head_rows<T>(*q), o = head_rows<T>(*out);
+  const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
+  const dim3 block(256), grid((unsigned)plan.groups);
+  if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
+  else kv4_attend<T, HD, 1, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
+  const int64_t per = 256 / (HD / 4), cols = std::min<int64_t>((int64_t)max_q * a.q_heads, (int64_t)b.rows * a.q_heads);
+  kv4_shared_join<T, HD><<<dim3((unsigned)std::min<int64_t>((cols + per - 1) / per, 65535), b.batch), block, 0, st>>>(c, b, o, a, (int)plan.groups);
+}
+
+extern "C" int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_prefix_groups *groups,
+                                          const heisd_head_rows *q, const heisd_head_rows *out, float *lse, float scale, int32_t max_q,
+                                          int32_t max_seq, void *workspace, size_t workspace_bytes, void *stream) {
+  const char *who = "kv4_shared_attention";
+  Kv4Cache c;
+  PagedBatch b;
+  PrefixGroups p;
+  int rc = kv4_ok(who, cache, &c);
+  if (rc == HEISD_OK) rc = batch_ok(who, batch, true, &b);
+  if (rc == HEISD_OK) rc = groups_desc_ok(who, groups, &p);
+  if (rc == HEISD_OK) rc = rows_ok(who, "q", q, b.rows);
+  if (rc == HEISD_OK) rc = rows_ok(who, "out", out, b.rows);
+  if (rc == HEISD_OK) rc = kv4_attention_sizes_ok(who, c.kv_heads, q->heads, b.rows, max_q, max_seq);
+  if (rc != HEISD_OK) return rc;
+  if (q->dtype != out->dtype || q->heads != out->heads) return fail(nullptr, HEISD_EINVAL, "%s: q and out differ in dtype or heads", who);
+  if (q->dtype == HEISD_DTYPE_F32) return fail(nullptr, HEISD_EUNSUPPORTED, "%s: q in fp32 (bf16 or fp16)", who);
+  if (!rows_aligned(*q, 16) || !rows_aligned(*out, 8)) return fail(nullptr, HEISD_EINVAL, "%s: q (16 bytes) or out (8 bytes) misaligned", who);
+  if (!std::isfinite(scale)) return fail(nullptr, HEISD_EINVAL, "%s: scale %g", who, scale);
+  if (b.rows == 0) return HEISD_OK;
+  if ((rc = apart_ok(who, "out", *out, b.rows, cache->head_dim)) != HEISD_OK) return rc;
+  const SharedPlan plan(b.batch, b.rows, c.kv_heads, q->heads / c.kv_heads, max_q, max_seq, p, cache->head_dim);
+  if (!workspace || ((uintptr_t)workspace & 255)) return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned workspace", who);
+  if (workspace_bytes < plan.total) return fail(nullptr, HEISD_ENOMEM, "%s: workspace %zu bytes < %zu needed", who, workspace_bytes, plan.total);
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  Kv4SharedAttend a;
+  static_cast<Kv4Attend &>(a) = Kv4Attend{std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f),      // not 0: minus infinity stands for masked scores
+                                          scale < 0, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
+                                          reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + plan.part_ml), lse};
+  a.prefix = p;
+  a.whole = reinterpret_cast<float *>(ws + plan.whole);
+  a.whole_ml = reinterpret_cast<float *>(ws + plan.whole_ml);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (q->dtype == HEISD_DTYPE_BF16) {
+    if (cache->head_dim == 128) kv4_shared_launch<__bf16, 128, 1>(c, b, q, out, a, plan, max_q, st);
+    else kv4_shared_launch<__bf16, 64, 1>(c, b, q, out, a, plan, max_q, st);
+  } else {
+    if (cache->head_dim == 128) kv4_shared_launch<_Float16, 128, 2>(c, b, q, out, a, plan, max_q, st);
+    else kv4_shared_launch<_Float16, 64, 2>(c, b, q, out, a, plan, max_q, st);
+  }
+  return launched(who);
+}
+
+extern "C" int heisd_paged_offset(const heisd_paged_batch *batch, const int32_t *offset, int32_t *position, void *stream) {
+  const char *who = "paged_offset";
+  PagedBatch b;
+  if (const int rc = batch_ok(who, batch, true, &b)) return rc;
+  if (!offset || (!position && b.rows > 0)) return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer", who);
+  if (b.rows == 0) return HEISD_OK;
+  (void)hipGetLastError();
+  offset_positions<<<dim3((b.rows + 255) / 256), dim3(256), 0, static_cast<hipStream_t>(stream)>>>(b, offset, position);
+  return launched(who);
+}
+
+// ---- attention weights and eviction ----------------------------------------------------------------------------------------
+
+extern "C" int heisd_kv4_weigh(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_prefix_groups *groups, const heisd_head_rows *q,
+                               const float *lse, float scale, float decay, const float *weight_in, float *weight_out, int32_t max_seq, void *stream) {
+  const char *who = "kv4_weigh";
+  Kv4Cache c;
+  PagedBatch b;
+  PrefixGroups p;
+  int rc = kv4_ok(who, cache, &c);
+  if (rc == HEISD_OK) rc = batch_ok(who, batch, true, &b);
+  if (rc == HEISD_OK) rc = groups_desc_ok(who, groups, &p);
+  if (rc == HEISD_OK) rc = rows_ok(who, "q", q, b.rows);
+  if (rc == HEISD_OK) rc = kv4_attention_sizes_ok(who, c.kv_heads, q->heads, b.rows, 1, max_seq);
+  if (rc != HEISD_OK) return rc;
+  if (q->dtype == HEISD_DTYPE_F32) return fail(nullptr, HEISD_EUNSUPPORTED, "%s: q in fp32 (bf16 or fp16)", who);
+  if (!rows_aligned(*q, 16)) return fail(nullptr, HEISD_EINVAL, "%s: q (16 bytes) misaligned", who);
+  if ((!lse && b.rows > 0) || !weight_in || !weight_out || !std::isfinite(scale) || !std::isfinite(decay))
+    return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer, scale %g or decay %g", who, scale, decay);
+  const WeighArgs a{scale * 1.4426950408889634f, decay, q->heads / c.kv_heads, q->heads, max_seq, lse, weight_in, weight_out};
+  const int64_t tiles = ((int64_t)std::max(max_seq, p.max_prefix) + kWeighTokens - 1) / kWeighTokens;
+  const dim3 grid((unsigned)tiles, c.kv_heads, b.batch), block(256);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const HeadRows<__bf16> qb = head_rows<__bf16>(*q);
+  const HeadRows<const __bf16> qc{qb.p, qb.rs, qb.hs};
+  const HeadRows<const _Float16> qh{reinterpret_cast<const _Float16 *>(qb.p), qb.rs, qb.hs};
+  if (q->dtype == HEISD_DTYPE_BF16) {
+    if (cache->head_dim == 128) kv4_weigh<__bf16, 128, 1><<<grid, block, 0, st>>>(c, b, p, qc, a);
+    else kv4_weigh<__bf16, 64, 1><<<grid, block, 0, st>>>(c, b, p, qc, a);
+  } else {
+    if (cache->head_dim == 128) kv4_weigh<_Float16, 128, 2><<<grid, block, 0, st>>>(c, b, p, qh, a);
+    else kv4_weigh<_Float16, 64, 2><<<grid, block, 0, st>>>(c, b, p, qh, a);
+  }
+  return launched(who);
+}
+
+extern "C" int heisd_kv4_evict(const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes, const heisd_paged_batch *batch, const int32_t *keep,
+                               int32_t recent, const float *weight_in, float *weight_out, int32_t *seq_out, int32_t max_seq, void *stream) {
+  const char *who = "kv4_evict";
+  Kv4Cache c;
+  PagedBatch b;
+  int rc = kv4_ok(who, cache, &c);
+  if (rc == HEISD_OK) rc = batch_ok(who, batch, false, &b);
+  if (rc == HEISD_OK) rc = layers_ok(who, cache, layers, layer_bytes);
+  if (rc != HEISD_OK) return rc;
+  if (!keep || !weight_in || !weight_out || !seq_out || recent < 0 || max_seq < 1 || max_seq > (1 << 24))
+    return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer, recent=%d or max_seq=%d (1..2^24)", who, recent, max_seq);
+  if (seq_out == b.seq_len) return fail(nullptr, HEISD_EINVAL, "%s: lengths in place", who);
+  const EvictArgs a{keep, recent, max_seq, layer_bytes, kv4_weights(c), weight_in, weight_out, seq_out};
+  const dim3 grid(c.kv_heads, b.batch, layers), block(kEvictThreads);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (cache->head_dim == 128) kv4_evict<128><<<grid, block, 0, st>>>(c, b, a);
+  else kv4_evict<64><<<grid, block, 0, st>>>(c, b, a);
+  return launched(who);
+}

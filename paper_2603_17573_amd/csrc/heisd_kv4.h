@@ -50,6 +50,25 @@ struct PagedBatch {
   int batch, max_blocks, rows;
 };
 
+// Groups of requests that share a prefix: group g is requests first[g] .. first[g + 1] - 1, prefix[g] the request whose tokens they all see.
+struct PrefixGroups {
+  const int32_t *first, *prefix;
+  int groups, max_rows, max_prefix;
+};
+// What a group asks for: its rows and its prefix (request -1: none).
+struct PrefixSpan {
+  Span rows;
+  int request, tokens;
+};
+__device__ __forceinline__ PrefixSpan prefix_span(const Kv4Cache &c, const PagedBatch &b, const PrefixGroups &p, int g) {
+  PrefixSpan s{{0, 0}, -1, 0};
+  const int r0 = p.first[g], r1 = p.first[g + 1], at = p.prefix[g];
+  if (r0 < 0 || r1 <= r0 || r1 > b.batch || at < 0 || at >= b.batch || (at >= r0 && at < r1)) return s;
+  const int a = b.cu_rows[r0], e = b.cu_rows[r1], n = b.seq_len[at];
+  if (a < 0 || e <= a || e > b.rows || n <= 0 || n > p.max_prefix || (long long)n > (long long)b.max_blocks * c.block_size) return s;
+  return PrefixSpan{{a, e - a}, at, n};
+}
+
 // ---- rows into the cache ------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
@@ -224,6 +243,12 @@ struct Kv4Attend {
   float *part, *part_ml;                            // sums of unfinished segments [2 * workgroups][cols][HD], their maxima and sums [..][cols][2]
   float *lse;
 };
+// With groups that share a prefix: they come behind the requests, as if they were requests whose rows are all of the group's and that see all of
+// their tokens.  A row has two parts then, and what a segment gives is always kept: [own, prefix][rows][q_heads] sums, maxima and sums.
+struct Kv4SharedAttend : Kv4Attend {
+  PrefixGroups prefix;
+  float *whole, *whole_ml;
+};
 
 // Work is counted in units: 128 tokens (a pair of tiles for each wave) of one request, key head and group of columns - a segment is all
 // units of such a three.  Every workgroup takes an equal run of the units of the whole call, whatever the requests' lengths are.
@@ -248,6 +273,16 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const Paged
   if (r.seq < 0 || r.seq > a.max_seq || (long long)r.seq > (long long)b.max_blocks * c.block_size) r.seq = 0;
   r.units = max((r.seq + kKv4Unit - 1) / kKv4Unit, 1);          // one even without tokens: somebody writes the zeros
   r.work = (long long)r.units * ((r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads);
+  return r;
+}
+
+__device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4Attend &) { return b.batch; }
+__device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4SharedAttend &a) { return b.batch + a.prefix.groups; }
+__device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int i) {
+  if (i < b.batch) return kv4_request(c, b, static_cast<const Kv4Attend &>(a), i);
+  const PrefixSpan s = prefix_span(c, b, a.prefix, i - b.batch);
+  Kv4Request r{s.rows, s.tokens, max((s.tokens + kKv4Unit - 1) / kKv4Unit, 1), 0};
+  r.work = (long long)r.units * ((r.rows.count * (long long)a.group + a.cols - 1) / a.cols * c.kv_heads);
   return r;
 }
 
@@ -285,8 +320,9 @@ __device__ __forceinline__ float kv4_weight(float m, float top) { return m == -I
 // shares with others goes to kv4_join.  A probability enters as a bf16 and a bf16 remainder: one bf16 alone (off by up to 2^-8, and with few
 // large probabilities nothing averages that out) made the results of single tokens 1.4 times as inexact as their own rounding does, for 3 % of the
 // time (59.9 against 62.1 us with 64 contexts of 256 to 8191 tokens).  TERMS 2: so do the queries (fp16 rows, whose 11 bits a bf16 does not hold).
-template <typename T, int HD, int CT, int TERMS>
-__global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
+template <typename T, int HD, int CT, int TERMS, typename A>
+__global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, A a) {
+  constexpr bool SHARED = std::is_same_v<A, Kv4SharedAttend>;
   constexpr int W = HD / 32, ND = HD / 16, KJ = HD / 32;        // code dwords, tiles of channels, products per score tile
   constexpr int LD = HD + 4;
   typedef Kv4Slot<HD> Slot;
@@ -301,11 +337,12 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
 
   // This workgroup's run of units.  Every wave finds it for itself: 64 requests are at hand (in LDS, a request per lane), 64 more while the
   // run lies behind them.
+  const int n_requests = kv4_requests(b, a);
   int first = 0;
   long long end;                                                // units before the end of these 64
   auto requests = [&](long long before) {
-    Kv4Request r = kv4_request(c, b, a, min(first + lane, b.batch - 1));
-    if (first + lane >= b.batch) r.work = 0;
+    Kv4Request r = kv4_request(c, b, a, min(first + lane, n_requests - 1));
+    if (first + lane >= n_requests) r.work = 0;
     long long start = r.work;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -318,11 +355,11 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
   };
   requests(0);
   long long all = end;
-  for (int i = 64; i < b.batch; i += 64) all += wave_sum64(i + lane < b.batch ? kv4_request(c, b, a, i + lane).work : 0);
+  for (int i = 64; i < n_requests; i += 64) all += wave_sum64(i + lane < n_requests ? kv4_request(c, b, a, i + lane).work : 0);
   const long long per = kv4_run(all, gridDim.x), run0 = blockIdx.x * per, run1 = min(run0 + per, all);
 
   for (long long at = run0; at < run1;) {
-    while (at >= end && first + 64 < b.batch) {
+    while (at >= end && first + 64 < n_requests) {
       first += 64;
       requests(end);
     }
@@ -341,6 +378,10 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     const long long slot = 2 * (long long)blockIdx.x + (at != run0);
     const int n_cols = rows.count * a.group;
     const int t1 = min(seq, u1 * kKv4Unit);
+    int owner = req, few = seq - rows.count + 1;                  // whose blocks; tokens that every row sees
+    if constexpr (SHARED)
+      if (req >= b.batch) owner = __builtin_amdgcn_readfirstlane(a.prefix.prefix[req - b.batch]), few = seq;
+    const int32_t *table = b.table + (long long)owner * b.max_blocks;
 
     // the columns' queries and how many tokens each may see
     typename VecOf<T, 8>::type qr[CT][KJ];
@@ -348,7 +389,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       const int n = min(col0 + ct * 16 + col, n_cols - 1), i = n / a.group;       // columns past the end: the last again, not stored
-      seen[ct] = seq - rows.count + i + 1;
+      seen[ct] = min(few + i, seq);
       const T *p = q.at(rows.begin + i, head * a.group + (n - i * a.group)) + quad * (HD / 4);
 #pragma unroll
       for (int j = 0; j < KJ; ++j) qr[ct][j] = *reinterpret_cast<const typename VecOf<T, 8>::type *>(p + j * 8);
@@ -448,7 +489,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[ct][e] = s[ct][e >> 2][e & 3];
-      if (gone0 || gone1 || base + 32 > seq - rows.count + 1) {
+      if (gone0 || gone1 || base + 32 > few) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int t = base + 16 * (e >> 2) + 4 * quad + (e & 3);
@@ -539,7 +580,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     for (t0 = u0 * kKv4Unit; t0 < t1; t0 += 32 * kKv4Unit) {
       // the blocks of the wave's tiles: lane 2 i + n holds that of tile n of its i-th pair of these 32
       const int t = t0 + 32 * (wave + 4 * (lane >> 1)) + 16 * (lane & 1);
-      my_id = t < t1 ? b.table[(long long)req * b.max_blocks + (t >> c.block_shift)] : -1;
+      my_id = t < t1 ? table[t >> c.block_shift] : -1;
       if (my_id >= c.n_blocks) my_id = -1;
       const int n_pairs = max((min(t1 - t0, 32 * kKv4Unit) + 127 - 32 * wave) >> 7, 0);
       wait_vmcnt_all();                                         // the compiler's own loads: none may be waited for among the transfers
@@ -559,7 +600,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     if (__ballot(odd)) {
       for (int t = u0 * kKv4Unit; t < t1; ++t) {
         if ((t / 32 - wave) % 4) continue;
-        const int id = b.table[(long long)req * b.max_blocks + (t >> c.block_shift)], o = t & (bs - 1);
+        const int id = table[t >> c.block_shift], o = t & (bs - 1);
         if (id < 0 || id >= c.n_blocks) continue;
         const uint8_t e = c.at(id, head)[Kv4Offsets<HD>::v_exp(bs) + ((o / 4) * (HD / 32) + quad * (HD / 4) / 32) * 4 + o % 4];
 #pragma unroll
@@ -595,7 +636,13 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
           }
         const int i = cn / a.group, h = head * a.group + (cn - i * a.group);
         const long long r = rows.begin + i;
-        if (whole) {
+        if (SHARED && whole) {
+          if constexpr (SHARED) {
+            const long long at_row = ((long long)(req >= b.batch) * b.rows + r) * a.q_heads + h;
+            *reinterpret_cast<f32x4 *>(a.whole + at_row * HD + d) = o;
+            if (d == 0) *reinterpret_cast<float2 *>(a.whole_ml + at_row * 2) = make_float2(top, sum);
+          }
+        } else if (whole) {
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
           float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
           store_vec<T, 4>(out.at(r, h) + d, f);
@@ -611,6 +658,29 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     at += u1 - u0;
   }
 }
+
+// Sums, maximum and sum of probabilities of a column, in the order of its tokens.
+struct Kv4Sums {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, sum = 0.f;
+  template <int K>
+  __device__ __forceinline__ void add(const float2 (&ml)[K], const f32x4 (&x)[K]) {
+    float next = top;
+#pragma unroll
+    for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
+    const float keep = kv4_weight(top, next);
+    sum *= keep;
+    o *= keep;
+    top = next;
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (kv4_saw(ml[i].x, ml[i].y)) {
+        const float by = kv4_weight(ml[i].x, top);
+        sum += ml[i].y * by;
+        o += x[i] * by;
+      }
+  }
+};
 
 // Joins the parts of segments that several workgroups worked on, in the order of their tokens.  A workgroup per segment; 16 bytes of
 // a column per thread.
@@ -635,8 +705,7 @@ __global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRo
     const int head = seg % c.kv_heads, col0 = seg / c.kv_heads * a.cols, n_cols = min(r.rows.count * a.group - col0, a.cols);
     for (int u = threadIdx.x; u < n_cols * (HD / 4); u += 256) {
       const int n = u / (HD / 4), d = u % (HD / 4) * 4;
-      float top = -INFINITY, sum = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      Kv4Sums s;
       constexpr int K = 8;                                                         // parts requested at once
       for (int w = w0; w <= w1; w += K) {
         float2 ml[K];
@@ -649,21 +718,10 @@ __global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRo
           x[i] = *reinterpret_cast<const f32x4 *>(a.part + at * HD + d);
           if (w + i > w1) ml[i] = make_float2(-INFINITY, 0.f);
         }
-        float next = top;
-#pragma unroll
-        for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
-        const float keep = kv4_weight(top, next);
-        sum *= keep;
-        o *= keep;
-        top = next;
-#pragma unroll
-        for (int i = 0; i < K; ++i)
-          if (kv4_saw(ml[i].x, ml[i].y)) {
-            const float by = kv4_weight(ml[i].x, top);
-            sum += ml[i].y * by;
-            o += x[i] * by;
-          }
+        s.add(ml, x);
       }
+      const float top = s.top, sum = s.sum;
+      const f32x4 o = s.o;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       const int i = (col0 + n) / a.group, h = head * a.group + (col0 + n - i * a.group);
       float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};

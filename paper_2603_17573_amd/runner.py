@@ -181,6 +181,13 @@ def _ints(t, shape, what, device):
     return t.data_ptr()
 
 
+def _floats(t, n, what, device):
+    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n or t.device != device or not t.is_cuda:
+        raise ValueError("%s: expected %d contiguous float32 on %s, got %s %s on %s"
+                         % (what, n, device if device.type == "cuda" else "a GPU", t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
 def make_plan_desc(block_size, n_blocks, cached_len, new_len, owned_in, owned_out, block_table, free_ids, free_count_in, free_count_out,
                    seq_len, cu_rows, slot, position, cu_seq=None) -> B.heisd_plan_desc:
     """The tensors of one heisd_paged_plan call, which must stay alive as long as the descriptor is used."""
@@ -222,6 +229,50 @@ def make_paged_batch(block_table, seq_len, cu_rows, rows) -> B.heisd_paged_batch
     (b, most), dev = block_table.shape, block_table.device
     return B.heisd_paged_batch(_ints(block_table, (b, most), "block_table", dev), _ints(seq_len, (b,), "seq_len", dev),
                                _ints(cu_rows, (b + 1,), "cu_rows", dev) if cu_rows is not None else None, b, most, rows)
+
+
+def make_beam_desc(logits, beams, width, score_in, score_out, beam, token, length_in=None, length_out=None, done_in=None, done_out=None,
+                   end_token=-1, length_power=0.0, parent=None, first=0, stride=0) -> B.heisd_beam_desc:
+    """The tensors of heisd_beam_select calls, which must stay alive as long as the descriptor is used.  logits: [groups * beams, vocab] with
+    adjacent tokens; score_out, beam, token, length_out, done_out: [groups, width]; parent: i32, entries first + group * stride + n are written."""
+    if logits.dim() != 2 or logits.dtype not in _DTYPE or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1) or \
+            beams < 1 or logits.shape[0] % beams:
+        raise ValueError("logits: expected [groups * %d, vocab] of bf16, fp16 or fp32 with adjacent tokens on a GPU, got %s %s strides %s on %s"
+                         % (beams, tuple(logits.shape), logits.dtype, logits.stride(), logits.device))
+    rows, dev = logits.shape[0], logits.device
+    groups = rows // beams
+    d = B.heisd_beam_desc(logits.data_ptr(), logits.stride(0), _DTYPE[logits.dtype], groups, beams, width, logits.shape[1], end_token, length_power)
+    d.score_in, d.score_out = _floats(score_in, rows, "score_in", dev), _floats(score_out, groups * width, "score_out", dev)
+    for name, t, n in (("beam", beam, groups * width), ("token", token, groups * width), ("length_in", length_in, rows),
+                       ("length_out", length_out, groups * width), ("done_in", done_in, rows), ("done_out", done_out, groups * width)):
+        if t is not None:
+            if t.numel() != n:
+                raise ValueError("%s: expected %d values, got %s" % (name, n, tuple(t.shape)))
+            setattr(d, name, _ints(t, t.shape, name, dev))
+    if parent is not None:
+        if parent.numel() < first + (groups - 1) * stride + width:
+            raise ValueError("parent: %d entries, groups of %d from %d on, %d apart" % (parent.numel(), width, first, stride))
+        d.parent, d.first, d.stride = _ints(parent, parent.shape, "parent", dev), first, stride
+    return d
+
+
+def make_reorder_desc(block_size, n_blocks, parent, len_in, owned_in, table_in, len_out, owned_out, table_out, copy_from, free_ids, free_count_in,
+                      free_count_out, trim=False) -> B.heisd_reorder_desc:
+    """The tensors of one heisd_paged_reorder call, which must stay alive as long as the descriptor is used."""
+    b, most = table_in.shape
+    d = B.heisd_reorder_desc(b, block_size, most, n_blocks, int(trim))
+    for name, t, shape in (("parent", parent, (b,)), ("len_in", len_in, (b,)), ("owned_in", owned_in, (b,)), ("table_in", table_in, (b, most)),
+                           ("len_out", len_out, (b,)), ("owned_out", owned_out, (b,)), ("table_out", table_out, (b, most)),
+                           ("copy_from", copy_from, (b,)), ("free_ids", free_ids, (n_blocks,)), ("free_count_in", free_count_in, (1,)),
+                           ("free_count_out", free_count_out, (1,))):
+        setattr(d, name, _ints(t, shape, name, parent.device))
+    return d
+
+
+def make_prefix_groups(first, prefix, max_rows, max_prefix) -> B.heisd_prefix_groups:
+    """first i32 [groups + 1], prefix i32 [groups]: group g is requests first[g] .. first[g + 1] - 1, which all see request prefix[g]'s tokens."""
+    n = prefix.shape[0]
+    return B.heisd_prefix_groups(_ints(first, (n + 1,), "first", prefix.device), _ints(prefix, (n,), "prefix", prefix.device), n, max_rows, max_prefix)
 
 
 class PagedCache:
