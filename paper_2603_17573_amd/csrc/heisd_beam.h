@@ -8,23 +8,24 @@ namespace heisd {
 // ---- the next beams ---------------------------------------------------------------------------------------------------
 
 constexpr int kBeamMost = 64;                       // beams and width at most: a lane each
-constexpr int kBeamValues = 32;                     // logits that a thread holds
-constexpr int kBeamChunk = 256 * kBeamValues;       // logits that a workgroup takes
-constexpr int kBeamKeep = 512;                      // candidates of a workgroup that are ranked among each other
+constexpr int kBeamWave = 2048;                     // logits that a wave of beam_scan reads
+constexpr int kBeamWaves = 8;                       // waves of a workgroup of beam_pick
+constexpr int kBeamList = 448;                      // candidates that a wave ranks at once: up to 256 come at a time
+template <typename T>
+constexpr int kBeamSegment = 64 * 16 / sizeof(T);   // logits of one load of a wave
 
 struct BeamArgs {
   const void *logits;
   long long row_stride;
-  int groups, beams, width, vocab, chunks, end_token;
+  int groups, beams, width, vocab, segments, end_token;   // segments: of a row, a multiple of those that a wave reads
   double power;
   const float *score_in;
   const int32_t *length_in, *done_in;
   float *score_out;
   int32_t *beam, *token, *length_out, *done_out, *parent;
   int first, stride;
-  float *ms;                                        // [rows][chunks][2]: maximum and sum of a chunk
-  float *value;                                     // [rows][chunks][width] the largest logits of a chunk, in order
-  int32_t *index;                                   // and their tokens (-1: no more)
+  float2 *ms;                                       // [rows][segments / segments of a wave]: maximum and sum of exponentials
+  float *top;                                       // [rows][segments] maxima
 };
 
 // Is (v, i) in front of (w, j)?  Larger values first, lower tokens among equals.
@@ -37,70 +38,60 @@ __device__ __forceinline__ void beam_wave_best(float &v, int &i) {
   v = top;
 }
 
-// A chunk of one row: its maximum, its sum of exponentials and its `width` largest logits, with one read of it.  Within a beam scores are logits and
-// one constant, so the order of the logits is that of the scores.
+// The lane's part of segment s of a row: logits V * lane on of kBeamSegment.  Loads are aligned whatever the row's address is, so the first and the
+// last may be cut.  Returns the token of f[0].  What is not there is minus infinity.
 template <typename T>
-__global__ __launch_bounds__(256) void beam_rows(BeamArgs a) {
-  constexpr int V = 16 / sizeof(T), NV = kBeamValues / V;
-  __shared__ float s_v[4], s_s[4];
-  __shared__ int s_i[4];
-  const int row = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
-  const long long part = (long long)row * a.chunks + chunk;
-  const float before = a.score_in[row];
-  if ((a.done_in && a.done_in[row]) || !(before > -INFINITY)) return;       // beam_join does not look here
+__device__ __forceinline__ int beam_load(const T *x, int vocab, int s, float *f) {
+  constexpr int V = 16 / sizeof(T);
+  const int t0 = s * kBeamSegment<T> + (threadIdx.x & 63) * V - (int)(((uintptr_t)x & 15) / sizeof(T));
+  if (t0 >= 0 && t0 + V <= vocab) load_vec<T, V>(x + t0, f);
+  else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = t0 + e >= 0 && t0 + e < vocab ? (float)x[t0 + e] : -INFINITY;
+  }
+  return t0;
+}
+
+// Maxima of N segments of a row from s on, and (maximum, sum of exponentials) of all of them, in every lane.
+template <typename T, int N, typename Top>
+__device__ __forceinline__ float2 beam_segments(const T *x, int vocab, int s, Top top) {
+  constexpr int V = 16 / sizeof(T);
+  float f[N * V], m = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) beam_load(x, vocab, s + k, f + k * V);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    float mine = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < V; ++e) mine = fmaxf(mine, f[k * V + e]);       // fmaxf drops NaN
+    mine = wave_max(mine);
+    top(s + k, mine);
+    m = fmaxf(m, mine);
+  }
+  if (m > -INFINITY) {
+#pragma unroll
+    for (int e = 0; e < N * V; ++e) {
+      const float p = __builtin_amdgcn_exp2f((f[e] - m) * 1.4426950408889634f);
+      sum += f[e] == f[e] ? p : 0.f;
+    }
+  }
+  return make_float2(m, wave_sum(sum));
+}
+
+// One read of the logits: the sum of exponentials, a wave's part at a time, and the maximum of every segment.  The `width` largest logits of a row lie
+// in the `width` segments with the largest maxima (the lower ones among equals: each of them holds a logit that comes before whatever lies outside), so
+// nothing else has to be kept.
+template <typename T>
+__global__ __launch_bounds__(256) void beam_scan(BeamArgs a) {
+  constexpr int N = kBeamWave / kBeamSegment<T>;
+  const int row = blockIdx.y, part = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (part * N >= a.segments) return;
+  if ((a.done_in && a.done_in[row]) || !(a.score_in[row] > -INFINITY)) return;      // beam_pick does not look here
   const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
-  // vectors are aligned whatever the row's address is: the first and the last of a row may be cut
-  const int shift = (int)(((uintptr_t)x & 15) / sizeof(T));
-  float f[kBeamValues];
-  auto token_of = [&](int n) { return chunk * kBeamChunk + ((n / V) * 256 + tid) * V + n % V - shift; };
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int t0 = token_of(k * V);
-    if (t0 >= 0 && t0 + V <= a.vocab) load_vec<T, V>(x + t0, f + k * V);
-    else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) f[k * V + e] = t0 + e >= 0 && t0 + e < a.vocab ? (float)x[t0 + e] : -INFINITY;
-    }
-  }
-  float top = -INFINITY;
-#pragma unroll
-  for (int n = 0; n < kBeamValues; ++n) {
-    if (!(f[n] > -INFINITY)) f[n] = -INFINITY;      // NaN
-    top = fmaxf(top, f[n]);
-  }
-  top = wave_max(top);
-  if ((tid & 63) == 0) s_v[wave] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(s_v[0], s_v[1]), fmaxf(s_v[2], s_v[3]));
-  float sum = 0.f;
-  if (top > -INFINITY) {
-#pragma unroll
-    for (int n = 0; n < kBeamValues; ++n) sum += expf(f[n] - top);
-  }
-  sum = wave_sum(sum);
-  if ((tid & 63) == 0) s_s[wave] = sum;
-  __syncthreads();
-  if (tid == 0) *reinterpret_cast<float2 *>(a.ms + part * 2) = make_float2(top, (s_s[0] + s_s[1]) + (s_s[2] + s_s[3]));
-  float last = INFINITY;                            // the one that was taken last
-  int last_i = -1;
-  for (int n = 0; n < a.width; ++n) {
-    float best = -INFINITY;
-    int at = 0x7FFFFFFF;
-#pragma unroll
-    for (int k = 0; k < kBeamValues; ++k) {
-      const int i = token_of(k);
-      if (f[k] > -INFINITY && beam_before(last, last_i, f[k], i) && beam_before(f[k], i, best, at)) best = f[k], at = i;
-    }
-    beam_wave_best(best, at);
-    __syncthreads();
-    if ((tid & 63) == 0) s_v[wave] = best, s_i[wave] = at;
-    __syncthreads();
-    last = -INFINITY, last_i = 0x7FFFFFFF;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-      if (beam_before(s_v[w], s_i[w], last, last_i)) last = s_v[w], last_i = s_i[w];
-    if (tid == 0) a.value[part * a.width + n] = last, a.index[part * a.width + n] = last > -INFINITY ? last_i : -1;
-  }
+  float mine = 0.f;
+  const float2 ms = beam_segments<T, N>(x, a.vocab, part * N, [&](int s, float v) { mine = s - part * N == lane ? v : mine; });
+  if (lane < N) a.top[(long long)row * a.segments + part * N + lane] = mine;
+  if (lane == 0) a.ms[(long long)row * (a.segments / N) + part] = ms;
 }
 
 __device__ __forceinline__ double wave_max64(double v) {
@@ -114,14 +105,42 @@ __device__ __forceinline__ double wave_sum64d(double v) {
   return v;
 }
 
-// A group's next beams.  A wave joins the chunks of one beam (a lane each); then the beams' candidates, which are in order, are merged by one wave
-// (a lane a beam).  Scores are held in 64 bits: what decides between two beams' candidates are differences of sums.
-template <int W>
-__global__ __launch_bounds__(W * 64) void beam_join(BeamArgs a) {
-  __shared__ double s_add[kBeamMost];               // what a beam's logits are added to; its length's power
-  __shared__ double s_norm[kBeamMost];
-  __shared__ float s_value[kBeamMost * kBeamMost];  // a beam's best logits in order
-  __shared__ int s_token[kBeamMost * kBeamMost];
+// The best `most` of `count` candidates of the wave in LDS, in order, to the front of the list; the new count.
+__device__ __forceinline__ int beam_rank(float2 *list, int count, int most) {
+  constexpr int K = kBeamList / 64;
+  const int lane = threadIdx.x & 63;
+  float v[K], last = INFINITY, keep = 0.f;
+  int i[K], last_i = -1, keep_i = 0, n = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const float2 c = lane + 64 * k < count ? list[lane + 64 * k] : make_float2(-INFINITY, 0.f);
+    v[k] = c.x, i[k] = __float_as_int(c.y);
+  }
+  for (; n < min(count, most); ++n) {
+    float best = -INFINITY;
+    int at = 0x7FFFFFFF;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (beam_before(last, last_i, v[k], i[k]) && beam_before(v[k], i[k], best, at)) best = v[k], at = i[k];
+    beam_wave_best(best, at);
+    last = best, last_i = at;
+    if (lane == n) keep = best, keep_i = at;
+  }
+  if (lane < n) list[lane] = make_float2(keep, __int_as_float(keep_i));
+  return n;
+}
+
+// A group's next beams.  A wave takes a beam: its segments with the largest maxima are read again, and what is not below the last of those maxima is ranked
+// (a list that gets full is cut to the best `width`).  Then the beams' candidates, which are in order, are merged by one wave (a lane a
+// beam).  Scores are held in 64 bits: what decides between two beams' candidates are differences of sums.  DIRECT: rows of few segments, which the wave
+// reads here for the first time, so that one launch does.
+template <typename T, bool DIRECT>
+__global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
+  constexpr int V = 16 / sizeof(T), N = kBeamWave / kBeamSegment<T>, W = kBeamWaves;
+  constexpr int K = DIRECT ? 1 : (1 << 19) / kBeamSegment<T> / 64;      // maxima per lane
+  __shared__ float2 s_list[W][kBeamList];
+  __shared__ float2 s_best[kBeamMost * kBeamMost];  // a beam's best logits in order, and their tokens
+  __shared__ double s_add[kBeamMost], s_norm[kBeamMost];    // what a beam's logits are added to; its length's power
   __shared__ int s_len[kBeamMost], s_done[kBeamMost], s_count[kBeamMost];
   const int g = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   for (int b = wave; b < a.beams; b += W) {
@@ -132,30 +151,68 @@ __global__ __launch_bounds__(W * 64) void beam_join(BeamArgs a) {
     int count = 0;
     double add = before;
     if (alive && done) {
-      if (lane == 0) s_value[b * a.width] = 0.f, s_token[b * a.width] = a.end_token;
+      if (lane == 0) s_best[b * a.width] = make_float2(0.f, __int_as_float(a.end_token));
       count = 1;
     } else if (alive) {
-      const long long part = (long long)row * a.chunks + lane;
-      const float2 ms = lane < a.chunks ? *reinterpret_cast<const float2 *>(a.ms + part * 2) : make_float2(-INFINITY, 0.f);
-      const float top = wave_max(ms.x);
-      const double sum = wave_sum64d(ms.x > -INFINITY && top < INFINITY ? (double)ms.y * exp((double)ms.x - (double)top) : 0.0);
-      if (sum > 0) {
-        add -= (double)top + log(sum);
-        int at = 0;                                 // this lane's chunk has given so many
-        for (; count < a.width; ++count) {
-          float v = -INFINITY;
-          int i = 0x7FFFFFFF;
-          if (lane < a.chunks && at < a.width) {
-            i = a.index[part * a.width + at];
-            v = i < 0 ? -INFINITY : a.value[part * a.width + at];
-            if (i < 0) i = 0x7FFFFFFF;
-          }
-          const int mine = i;
-          beam_wave_best(v, i);
-          if (!(v > -INFINITY)) break;
-          at += mine == i;
-          if (lane == 0) s_value[b * a.width + count] = v, s_token[b * a.width + count] = i;
+      const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+      float tops[K], m = -INFINITY;
+      double sum = 0;
+      if constexpr (DIRECT) {
+        tops[0] = -INFINITY;
+        for (int s = 0; s < a.segments; s += N) {
+          const float2 ms = beam_segments<T, N>(x, a.vocab, s, [&](int at, float v) { tops[0] = at == lane ? v : tops[0]; });
+          const float next = fmaxf(m, ms.x);
+          if (ms.x > -INFINITY) sum = sum * exp((double)m - (double)next) + (double)ms.y * exp((double)ms.x - (double)next);
+          m = next;
         }
+      } else {
+        const int parts = a.segments / N;
+        const float2 *ms = a.ms + (long long)row * parts;
+        for (int i = lane; i < parts; i += 64) m = fmaxf(m, ms[i].x);
+        m = wave_max(m);
+        for (int i = lane; i < parts; i += 64) sum += ms[i].x > -INFINITY ? (double)ms[i].y * exp((double)ms[i].x - (double)m) : 0.0;
+        sum = wave_sum64d(sum);
+#pragma unroll
+        for (int k = 0; k < K; ++k) tops[k] = lane + 64 * k < a.segments ? a.top[(long long)row * a.segments + lane + 64 * k] : -INFINITY;
+      }
+      if (m > -INFINITY && m < INFINITY) {
+        add -= (double)m + log(sum);
+        // the segments, and what a candidate has to reach
+        int mine = 0, chosen = 0, last_i = -1;
+        float last = INFINITY;
+        for (; chosen < a.width; ++chosen) {
+          float best = -INFINITY;
+          int at = 0x7FFFFFFF;
+#pragma unroll
+          for (int k = 0; k < K; ++k)
+            if (beam_before(last, last_i, tops[k], lane + 64 * k) && beam_before(tops[k], lane + 64 * k, best, at)) best = tops[k], at = lane + 64 * k;
+          beam_wave_best(best, at);
+          if (!(best > -INFINITY)) break;
+          last = best, last_i = at;
+          if (lane == chosen) mine = at;
+        }
+        float floor = chosen == a.width ? last : -INFINITY;
+        int floor_i = 0x7FFFFFFF;
+        for (int n = 0; n < chosen; ++n) {
+          float f[V];
+          const int t0 = beam_load(x, a.vocab, __builtin_amdgcn_readlane(mine, n), f);
+#pragma unroll
+          for (int e0 = 0; e0 < V; e0 += 4) {
+            if (count > kBeamList - 256) {
+              count = beam_rank(s_list[wave], count, a.width);
+              if (count == a.width) floor = s_list[wave][count - 1].x, floor_i = __float_as_int(s_list[wave][count - 1].y);
+            }
+#pragma unroll
+            for (int e = e0; e < e0 + 4; ++e) {
+              const bool yes = f[e] > -INFINITY && !beam_before(floor, floor_i, f[e], t0 + e);
+              const unsigned long long all = __ballot(yes);
+              if (yes) s_list[wave][count + __popcll(all & ((1ull << lane) - 1))] = make_float2(f[e], __int_as_float(t0 + e));
+              count += __popcll(all);
+            }
+          }
+        }
+        count = beam_rank(s_list[wave], count, a.width);
+        if (lane < count) s_best[b * a.width + lane] = s_list[wave][lane];
       }
     }
     if (lane == 0) {
@@ -173,7 +230,8 @@ __global__ __launch_bounds__(W * 64) void beam_join(BeamArgs a) {
   const double add = in ? s_add[lane] : 0, norm = in ? s_norm[lane] : 0;
   const int count = in ? s_count[lane] : 0;
   for (int n = 0; n < a.width; ++n) {
-    const double score = at < count ? add + (double)s_value[lane * a.width + at] : -INFINITY;
+    const float2 next = at < count ? s_best[lane * a.width + at] : make_float2(0.f, 0.f);
+    const double score = at < count ? add + (double)next.x : -INFINITY;
     const double rank = at < count ? score * norm : -INFINITY;
     const double best = wave_max64(rank);
     const unsigned long long who = __ballot(at < count && rank == best);
@@ -190,7 +248,7 @@ __global__ __launch_bounds__(W * 64) void beam_join(BeamArgs a) {
     }
     const int b = __builtin_ctzll(who);
     if (lane == b) {
-      const int token = s_token[lane * a.width + at];
+      const int token = __float_as_int(next.y);
       a.score_out[to] = (float)score;
       a.beam[to] = b;
       a.token[to] = token;

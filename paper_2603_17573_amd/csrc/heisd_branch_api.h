@@ -3,9 +3,8 @@
 
 // ---- the next beams --------------------------------------------------------------------------------------------------
 
-// A lane of beam_join takes a chunk; a row's address may cut its first vector, so that it needs up to a vector more.
-constexpr int kBeamMostVocab = kBeamMost * kBeamChunk - 8;
-static int beam_chunks(int32_t vocab) { return (vocab + 7 + kBeamChunk - 1) / kBeamChunk; }
+constexpr int kBeamMostVocab = (1 << 19) - 8;       // as many segments as beam_pick's lanes hold; a row's address may cut its first and last
+constexpr int kBeamDirectVocab = 4096;              // up to here one launch does
 
 static int beam_sizes_ok(const char *who, int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
   if (groups < 1 || groups > 65535 || beams < 1 || beams > kBeamMost || width < 1 || width > kBeamMost || vocab < 1 || vocab > kBeamMostVocab)
@@ -15,23 +14,31 @@ static int beam_sizes_ok(const char *who, int32_t groups, int32_t beams, int32_t
   return HEISD_OK;
 }
 struct BeamLayout {
-  size_t value, index, total;
-  BeamLayout(int64_t rows, int chunks, int width) {
-    value = align256((size_t)rows * chunks * 2 * sizeof(float));
-    index = value + align256((size_t)rows * chunks * width * sizeof(float));
-    total = index + align256((size_t)rows * chunks * width * sizeof(int32_t));
+  int segments;
+  size_t top, total;
+  BeamLayout(int64_t rows, int64_t vocab, size_t size) {
+    const int64_t waves = (vocab + 16 / size - 1 + kBeamWave - 1) / kBeamWave;
+    segments = (int)(waves * (kBeamWave * size / 1024));
+    top = align256((size_t)(rows * waves) * sizeof(float2));
+    total = top + align256((size_t)rows * segments * sizeof(float));
   }
 };
 
 extern "C" size_t heisd_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
   if (beam_sizes_ok("beam_select_workspace_bytes", groups, beams, width, vocab) != HEISD_OK) return 0;
-  return BeamLayout((int64_t)groups * beams, beam_chunks(vocab), width).total;
+  return BeamLayout((int64_t)groups * beams, vocab, 4).total;        // fp32 has most
 }
 
 template <typename T>
 static void beam_launch(const BeamArgs &a, hipStream_t st) {
-  beam_rows<T><<<dim3(a.chunks, a.groups * a.beams), dim3(256), 0, st>>>(a);
-  beam_join<4><<<dim3(a.groups), dim3(256), 0, st>>>(a);
+  const dim3 groups(a.groups), block(kBeamWaves * 64);
+  if (a.vocab <= kBeamDirectVocab) {
+    beam_pick<T, true><<<groups, block, 0, st>>>(a);
+    return;
+  }
+  const int per = 4 * kBeamWave / kBeamSegment<T>;
+  beam_scan<T><<<dim3((a.segments + per - 1) / per, a.groups * a.beams), dim3(256), 0, st>>>(a);
+  beam_pick<T, false><<<groups, block, 0, st>>>(a);
 }
 
 extern "C" int heisd_beam_select(const heisd_beam_desc *d, void *workspace, size_t workspace_bytes, void *stream) {
@@ -54,14 +61,13 @@ extern "C" int heisd_beam_select(const heisd_beam_desc *d, void *workspace, size
   const void *in[3] = {d->score_in, d->length_in, d->done_in}, *out[3] = {d->score_out, d->length_out, d->done_out};
   for (int i = 0; i < 3; ++i)
     if (in[i] && in[i] == out[i] && d->width != d->beams) return fail(nullptr, HEISD_EINVAL, "%s: in place with another number of beams", who);
-  const int chunks = beam_chunks(d->vocab);
-  const BeamLayout lay((int64_t)d->groups * d->beams, chunks, d->width);
+  const BeamLayout lay((int64_t)d->groups * d->beams, d->vocab, size);
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(nullptr, HEISD_EINVAL, "%s: NULL or misaligned workspace", who);
   if (workspace_bytes < lay.total) return fail(nullptr, HEISD_ENOMEM, "%s: workspace %zu bytes < %zu needed", who, workspace_bytes, lay.total);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  const BeamArgs a{d->logits, d->row_stride, d->groups, d->beams, d->width, d->vocab, chunks, d->end_token, d->length_power, d->score_in, d->length_in,
+  const BeamArgs a{d->logits, d->row_stride, d->groups, d->beams, d->width, d->vocab, lay.segments, d->end_token, d->length_power, d->score_in, d->length_in,
                    d->done_in, d->score_out, d->beam, d->token, d->length_out, d->done_out, d->parent, d->first, d->stride,
-                   reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + lay.value), reinterpret_cast<int32_t *>(ws + lay.index)};
+                   reinterpret_cast<float2 *>(ws), reinterpret_cast<float *>(ws + lay.top)};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (d->dtype == HEISD_DTYPE_F32) beam_launch<float>(a, st);
@@ -239,6 +245,8 @@ extern "C" int heisd_paged_offset(const heisd_paged_batch *batch, const int32_t 
 
 // ---- attention weights and eviction ----------------------------------------------------------------------------------------
 
+constexpr int64_t kWeighFill = 4096;
+
 extern "C" int heisd_kv4_weigh(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_prefix_groups *groups, const heisd_head_rows *q,
                                const float *lse, float scale, float decay, const float *weight_in, float *weight_out, int32_t max_seq, void *stream) {
   const char *who = "kv4_weigh";
@@ -256,21 +264,31 @@ extern "C" int heisd_kv4_weigh(const heisd_kv4_desc *cache, const heisd_paged_ba
   if ((!lse && b.rows > 0) || !weight_in || !weight_out || !std::isfinite(scale) || !std::isfinite(decay))
     return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer, scale %g or decay %g", who, scale, decay);
   const WeighArgs a{scale * 1.4426950408889634f, decay, q->heads / c.kv_heads, q->heads, max_seq, lse, weight_in, weight_out};
-  const int64_t tiles = ((int64_t)std::max(max_seq, p.max_prefix) + kWeighTokens - 1) / kWeighTokens;
-  const dim3 grid((unsigned)tiles, c.kv_heads, b.batch), block(256);
+  // As many pairs per wave as leave some workgroups per compute unit, counted with the largest lengths.
+  const int64_t units = ((int64_t)std::max(max_seq, p.max_prefix) + kWeighUnit - 1) / kWeighUnit;
+  const int pairs = (int)std::max<int64_t>(1, std::min<int64_t>(kWeighPairs, units * c.kv_heads * b.batch / kWeighFill));
+  const dim3 grid((unsigned)((units + pairs - 1) / pairs), c.kv_heads, b.batch), block(256);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   const HeadRows<__bf16> qb = head_rows<__bf16>(*q);
   const HeadRows<const __bf16> qc{qb.p, qb.rs, qb.hs};
   const HeadRows<const _Float16> qh{reinterpret_cast<const _Float16 *>(qb.p), qb.rs, qb.hs};
   if (q->dtype == HEISD_DTYPE_BF16) {
-    if (cache->head_dim == 128) kv4_weigh<__bf16, 128, 1><<<grid, block, 0, st>>>(c, b, p, qc, a);
-    else kv4_weigh<__bf16, 64, 1><<<grid, block, 0, st>>>(c, b, p, qc, a);
+    if (cache->head_dim == 128) kv4_weigh<__bf16, 128, 1><<<grid, block, 0, st>>>(c, b, p, qc, a, pairs);
+    else kv4_weigh<__bf16, 64, 1><<<grid, block, 0, st>>>(c, b, p, qc, a, pairs);
   } else {
-    if (cache->head_dim == 128) kv4_weigh<_Float16, 128, 2><<<grid, block, 0, st>>>(c, b, p, qh, a);
-    else kv4_weigh<_Float16, 64, 2><<<grid, block, 0, st>>>(c, b, p, qh, a);
+    if (cache->head_dim == 128) kv4_weigh<_Float16, 128, 2><<<grid, block, 0, st>>>(c, b, p, qh, a, pairs);
+    else kv4_weigh<_Float16, 64, 2><<<grid, block, 0, st>>>(c, b, p, qh, a, pairs);
   }
   return launched(who);
+}
+
+template <int HD>
+static void kv4_evict_launch(const Kv4Cache &c, const PagedBatch &b, const EvictArgs &a, dim3 grid, hipStream_t st) {
+  if (a.max_seq <= 2048) kv4_evict_held<HD, 4, 8><<<grid, dim3(256), 0, st>>>(c, b, a);
+  else if (a.max_seq <= 8192) kv4_evict_held<HD, 16, 8><<<grid, dim3(1024), 0, st>>>(c, b, a);
+  else if (a.max_seq <= 16384) kv4_evict_held<HD, 16, 16><<<grid, dim3(1024), 0, st>>>(c, b, a);
+  else kv4_evict<HD><<<grid, dim3(kEvictThreads), 0, st>>>(c, b, a);
 }
 
 extern "C" int heisd_kv4_evict(const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes, const heisd_paged_batch *batch, const int32_t *keep,
@@ -286,10 +304,10 @@ extern "C" int heisd_kv4_evict(const heisd_kv4_desc *cache, int32_t layers, int6
     return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer, recent=%d or max_seq=%d (1..2^24)", who, recent, max_seq);
   if (seq_out == b.seq_len) return fail(nullptr, HEISD_EINVAL, "%s: lengths in place", who);
   const EvictArgs a{keep, recent, max_seq, layer_bytes, kv4_weights(c), weight_in, weight_out, seq_out};
-  const dim3 grid(c.kv_heads, b.batch, layers), block(kEvictThreads);
+  const dim3 grid(c.kv_heads, b.batch, layers);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (cache->head_dim == 128) kv4_evict<128><<<grid, block, 0, st>>>(c, b, a);
-  else kv4_evict<64><<<grid, block, 0, st>>>(c, b, a);
+  if (cache->head_dim == 128) kv4_evict_launch<128>(c, b, a, grid, st);
+  else kv4_evict_launch<64>(c, b, a, grid, st);
   return launched(who);
 }

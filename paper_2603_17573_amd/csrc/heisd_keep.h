@@ -66,97 +66,158 @@ struct WeighArgs {
   const float *lse, *weight_in;
   float *weight_out;
 };
-constexpr int kWeighTokens = 128;                   // per workgroup: 32 per wave
+constexpr int kWeighPairs = 8;                      // pairs of tiles that a wave takes at most
+constexpr int kWeighUnit = 128;                     // tokens of a pair for each of the four waves
+
+// What a lane holds of the keys of two tiles of 16 tokens: a quarter of one token's head in each, and the weight that one of the tokens had.
+template <int HD>
+struct WeighPair {
+  uint32_t kc[2][HD / 32], ke[2];
+  float old;
+};
+template <int HD>
+__device__ __forceinline__ bf16x8 weigh_keys(const WeighPair<HD> &p, int n, int j) {
+  const float ks = __uint_as_float(p.ke[n] << 23);
+  const uint32_t w = p.kc[n][j];
+  const auto x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 1),
+             x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 3);
+  bf16x8 k;
+  k[0] = x0[0], k[1] = x0[1], k[2] = x1[0], k[3] = x1[1], k[4] = x2[0], k[5] = x2[1], k[6] = x3[0], k[7] = x3[1];
+  return k;
+}
 
 // weight[t] = decay * weight[t] + sum over the rows that see token t and the query heads of its key head of exp(scale q . k - lse).  Scores are one
-// matrix product of keys (tokens are rows, held in registers) and the rows' queries (columns, 16 at a time); lane l has column l % 16 and four
-// tokens of a tile, adds up its columns' probabilities and the 16 lanes of a token are added at the end.  Every token's weight is written by one wave, whose order of
+// matrix product of keys (tokens are rows) and the rows' queries (columns, 16 at a time); lane l has column l % 16 and four
+// tokens of a tile, adds up its columns' probabilities, and the 16 lanes of a token are added at the end.  Every token's weight is written by one wave, whose order of
 // additions is fixed.  A token that one of its request's rows brought (the last n) had no weight before.  Queries enter as in the attention.
+// A wave takes `pairs` pairs of tiles, the next one on its way while it works.  Where 16 columns hold all rows (single tokens and few), their queries
+// stay in registers.
 template <typename T, int HD, int TERMS>
-__global__ __launch_bounds__(256) void kv4_weigh(Kv4Cache c, PagedBatch b, PrefixGroups p, HeadRows<const T> q, WeighArgs a) {
+__global__ __launch_bounds__(256) void kv4_weigh(Kv4Cache c, PagedBatch b, PrefixGroups p, HeadRows<const T> q, WeighArgs a, int pairs) {
   constexpr int KJ = HD / 32;
   const int req = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bs = c.block_size;
-  const int seq = b.seq_len[req], base = blockIdx.x * kWeighTokens + wave * 32;
-  if (seq <= base || seq > max(a.max_seq, p.groups ? p.max_prefix : 0) || (long long)seq > (long long)b.max_blocks * bs) return;
-  const Span own = wave_span(b.cu_rows, req, b.rows);
-  // keys of 32 tokens
-  bf16x8 kf[2][KJ];
-  int id[2];
+  const int seq = b.seq_len[req], t0 = blockIdx.x * (kWeighUnit * pairs) + wave * 32;
+  if (seq <= t0 || seq > max(a.max_seq, p.groups ? p.max_prefix : 0) || (long long)seq > (long long)b.max_blocks * bs) return;
+  Span own = wave_span(b.cu_rows, req, b.rows);
+  const int had = seq - own.count;                  // tokens that had a weight before
+  if (seq > a.max_seq) own.count = 0;
+  const int n_pairs = min((seq - t0 + kWeighUnit - 1) / kWeighUnit, pairs);
+  int my_id = -1;                                   // lane 2 i + n: the block of tile n of the i-th pair
+  {
+    const int t = t0 + kWeighUnit * (lane >> 1) + 16 * (lane & 1);
+    if (lane < 2 * n_pairs && t < seq) my_id = b.table[(long long)req * b.max_blocks + (t >> c.block_shift)];
+    if (my_id >= c.n_blocks) my_id = -1;
+  }
+  // tokens this lane writes: 4 quad + e of tile n, with col = 4 n + e below 8
+  auto my_token = [&](int i) { return t0 + kWeighUnit * i + 16 * (col >> 2) + 4 * quad + (col & 3); };
+  auto weight_at = [&](int i) {
+    const int id0 = __builtin_amdgcn_readlane(my_id, 2 * i), id1 = __builtin_amdgcn_readlane(my_id, 2 * i + 1), id = col >> 2 ? id1 : id0;
+    return col >= 8 || id < 0 || my_token(i) >= seq ? -1ll : ((long long)id * c.kv_heads + head) * bs + (my_token(i) & (bs - 1));
+  };
+  auto fetch = [&](int i) {
+    WeighPair<HD> r;
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const int t = base + 16 * n;
-    id[n] = t < seq ? b.table[(long long)req * b.max_blocks + (t >> c.block_shift)] : -1;
-    if (id[n] >= c.n_blocks) id[n] = -1;
-    id[n] = __builtin_amdgcn_readfirstlane(id[n]);
-    if (id[n] < 0) continue;
-    const uint8_t *cell = c.at(id[n], head);
-    const int o = (t & (bs - 1)) + col;
-    const uint8_t *codes = cell + o * (HD / 2) + quad * (HD / 8);
-    const float ks = __uint_as_float((uint32_t)cell[Kv4Offsets<HD>::k_exp(bs) + o * (HD / 32) + quad * (HD / 4) / 32] << 23);
+    for (int n = 0; n < 2; ++n) {
+      const uint8_t *cell = c.at(max(__builtin_amdgcn_readlane(my_id, 2 * i + n), 0), head);      // a missing block: any block, not written
+      const int o = ((t0 + kWeighUnit * i + 16 * n) & (bs - 1)) + col;
+      const uint32_t *codes = reinterpret_cast<const uint32_t *>(cell + o * (HD / 2) + quad * (HD / 8));
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) r.kc[n][j] = codes[j];
+      r.ke[n] = cell[Kv4Offsets<HD>::k_exp(bs) + o * (HD / 32) + quad * (HD / 4) / 32];
+    }
+    const long long at = weight_at(i);
+    r.old = at >= 0 && my_token(i) < had ? a.weight_in[at] : 0.f;
+    return r;
+  };
+  // a column's query: column c0 + col of rows [begin, begin + count)
+  struct Column {
+    bf16x8 q[KJ][TERMS];
+    float lse;                                      // in powers of two
+    int seen;
+  };
+  auto column = [&](Column &x, Span rows, int c0, int seen0, bool causal) {
+    const int n_cols = rows.count * a.group, n = min(c0 + col, n_cols - 1), i = n / a.group, h = head * a.group + (n - i * a.group);
+    const T *from = q.at(rows.begin + i, h) + quad * (HD / 4);
+    const float lse = a.lse[(long long)(rows.begin + i) * a.q_heads + h];
+    x.lse = lse * 1.4426950408889634f;
+    x.seen = c0 + col >= n_cols || lse == -INFINITY ? 0 : causal ? seen0 + i : seq;
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
-      const uint32_t w = reinterpret_cast<const uint32_t *>(codes)[j];
-      const auto x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 1),
-                 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 3);
-      kf[n][j][0] = x0[0], kf[n][j][1] = x0[1], kf[n][j][2] = x1[0], kf[n][j][3] = x1[1];
-      kf[n][j][4] = x2[0], kf[n][j][5] = x2[1], kf[n][j][6] = x3[0], kf[n][j][7] = x3[1];
-    }
-  }
-  float sum[2][4] = {};
-  // all columns of rows [r0, r0 + count), of which row i sees tokens below seen0 + i (causal) or all
-  auto add_rows = [&](Span rows, int seen0, bool causal) {
-    const int n_cols = rows.count * a.group;
-    const int i0 = causal ? max(base - seen0 + 1, 0) : 0;         // rows before see none of these tokens
-    for (int c0 = i0 * a.group & ~15; c0 < n_cols; c0 += 16) {
-      const int n = min(c0 + col, n_cols - 1), i = n / a.group, h = head * a.group + (n - i * a.group);
-      const T *x = q.at(rows.begin + i, h) + quad * (HD / 4);
-      const float lse = a.lse[(long long)(rows.begin + i) * a.q_heads + h] * 1.4426950408889634f;
-      const int seen = c0 + col >= n_cols || lse == -INFINITY ? 0 : causal ? seen0 + i : seq;
-      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      const auto v = *reinterpret_cast<const typename VecOf<T, 8>::type *>(from + j * 8);
 #pragma unroll
-      for (int j = 0; j < KJ; ++j) {
-        const auto v = *reinterpret_cast<const typename VecOf<T, 8>::type *>(x + j * 8);
-        bf16x8 qf[TERMS];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float f = (float)v[e];
-          qf[0][e] = (__bf16)f;
-          if constexpr (TERMS == 2) qf[1][e] = (__bf16)(f - (float)qf[0][e]);
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < TERMS; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][j], qf[e], s[t], 0, 0, 0);
+      for (int e = 0; e < 8; ++e) {
+        const float f = (float)v[e];
+        x.q[j][0][e] = (__bf16)f;
+        if constexpr (TERMS == 2) x.q[j][1][e] = (__bf16)(f - (float)x.q[j][0][e]);
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float pr = exp2f(__builtin_fmaf(s[t][e], a.scale_log2, -lse));
-          sum[t][e] += base + 16 * t + 4 * quad + e < seen ? pr : 0.f;
-        }
     }
   };
-  if (own.count && seq <= a.max_seq) add_rows(own, seq - own.count + 1, true);
-  for (int g0 = 0; g0 < p.groups; g0 += 64) {       // the groups that this request is the prefix of
-    unsigned long long mine = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
-    for (; mine; mine &= mine - 1) {
-      const PrefixSpan s = prefix_span(c, b, p, g0 + __builtin_ctzll(mine));
-      if (s.request == req) add_rows(Span{__builtin_amdgcn_readfirstlane(s.rows.begin), __builtin_amdgcn_readfirstlane(s.rows.count)}, 0, false);
+  auto add = [&](float (&sum)[2][4], const bf16x8 (&kf)[2][KJ], const Column &x, int base) {
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < TERMS; ++e) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][j], x.q[j][e], s[n], 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float pr = exp2_fast(__builtin_fmaf(s[n][e], a.scale_log2, -x.lse));
+        sum[n][e] += base + 16 * n + 4 * quad + e < x.seen ? pr : 0.f;
+      }
+  };
+  unsigned long long any = 0;                       // is it anybody's prefix?
+  for (int g0 = 0; g0 < p.groups && !any; g0 += 64) any = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
+  const int own_cols = own.count * a.group, seen0 = had + 1;
+  const bool few = !any && own_cols <= 16;
+  Column only;
+  if (few && own_cols) column(only, own, 0, seen0, true);
+  WeighPair<HD> next = fetch(0);
+  for (int i = 0; i < n_pairs; ++i) {
+    const WeighPair<HD> now = next;
+    if (i + 1 < n_pairs) next = fetch(i + 1);
+    const int base = t0 + kWeighUnit * i;
+    bf16x8 kf[2][KJ];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) kf[n][j] = weigh_keys<HD>(now, n, j);
+    float sum[2][4] = {};
+    if (few) {
+      if (own_cols) add(sum, kf, only, base);
+    } else {
+      Column x;
+      for (int c0 = max(base - seen0 + 1, 0) * a.group & ~15; c0 < own_cols; c0 += 16) {        // rows before see none of these tokens
+        column(x, own, c0, seen0, true);
+        add(sum, kf, x, base);
+      }
+      for (int g0 = 0; g0 < p.groups; g0 += 64) {   // the groups that this request is the prefix of
+        unsigned long long mine = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
+        for (; mine; mine &= mine - 1) {
+          const PrefixSpan s = prefix_span(c, b, p, g0 + __builtin_ctzll(mine));
+          if (s.request != req) continue;
+          const Span rows{__builtin_amdgcn_readfirstlane(s.rows.begin), __builtin_amdgcn_readfirstlane(s.rows.count)};
+          for (int c0 = 0; c0 < rows.count * a.group; c0 += 16) {
+            column(x, rows, c0, 0, false);
+            add(sum, kf, x, base);
+          }
+        }
+      }
     }
+    const long long at = weight_at(i);
+    float fresh = 0.f;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float all = sum16(sum[n][e]);
+        fresh = col == 4 * n + e ? all : fresh;
+      }
+    if (at >= 0) a.weight_out[at] = __builtin_fmaf(a.decay, now.old, fresh);
   }
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float fresh = sum16(sum[n][e]);
-      const int t = base + 16 * n + 4 * quad + e;
-      if (col != 4 * n + e || t >= seq || id[n] < 0) continue;
-      const long long at = ((long long)id[n] * c.kv_heads + head) * bs + (t & (bs - 1));
-      const float old = t < seq - own.count ? a.weight_in[at] : 0.f;
-      a.weight_out[at] = __builtin_fmaf(a.decay, old, fresh);
-    }
 }
 
 // ---- eviction -----------------------------------------------------------------------------------------------------------
@@ -180,97 +241,239 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictQueue = 4 * kEvictThreads;
 
+// A sixteenth of a token's bytes on their way from one place to another, in one lane of 16: 4 (2) bytes of key codes and of value codes each, an
+// exponent of a key (value) group in one of the first lanes, the weight in the first.
+template <int HD>
+struct EvictPiece {
+  typedef std::conditional_t<HD == 128, uint32_t, uint16_t> Codes;
+  Codes k, v;
+  float w;
+  uint8_t e;
+  static constexpr int G = HD / 32;
+  __device__ __forceinline__ static int value_at(int t, int bs, int lane16) {
+    return Kv4Offsets<HD>::v_codes(bs) + (t / 4) * (2 * HD) + lane16 * (HD / 8) + (t % 4) * G;
+  }
+  __device__ __forceinline__ static int exp_at(int t, int bs, int lane16) {
+    const int g = lane16 % G;
+    return lane16 < G ? Kv4Offsets<HD>::k_exp(bs) + t * G + g : Kv4Offsets<HD>::v_exp(bs) + ((t / 4) * G + g) * 4 + t % 4;
+  }
+  __device__ __forceinline__ void load(const uint8_t *cell, const float *weight, int t, int bs, int lane16) {
+    k = reinterpret_cast<const Codes *>(cell + t * (HD / 2))[lane16];
+    v = *reinterpret_cast<const Codes *>(cell + value_at(t, bs, lane16));
+    if (lane16 < 2 * G) e = cell[exp_at(t, bs, lane16)];
+    if (lane16 == 0) w = *weight;
+  }
+  __device__ __forceinline__ void store(uint8_t *cell, float *weight, int t, int bs, int lane16) const {
+    reinterpret_cast<Codes *>(cell + t * (HD / 2))[lane16] = k;
+    *reinterpret_cast<Codes *>(cell + value_at(t, bs, lane16)) = v;
+    if (lane16 < 2 * G) cell[exp_at(t, bs, lane16)] = e;
+    if (lane16 == 0) *weight = w;
+  }
+};
+
+// What a workgroup of an eviction has to do: one request, head and layer.  Every thread of the workgroup makes it (a barrier is in it).
+struct EvictTask {
+  Kv4Cache c;
+  const int32_t *table;
+  const float *w_in;
+  float *w_out;
+  int head, n, keep, recent, cand, first;           // cand: tokens that may go, of which `first` stay
+  bool whole, cut;
+  __device__ __forceinline__ EvictTask(const Kv4Cache &cache, const PagedBatch &b, const EvictArgs &a) : c(cache) {
+    const int req = blockIdx.y, bs = c.block_size;
+    head = blockIdx.x;
+    table = b.table + (long long)req * b.max_blocks;
+    n = b.seq_len[req];
+    keep = a.keep[req];
+    c.pool += blockIdx.z * a.layer_bytes;
+    w_in = a.weight_in + blockIdx.z * a.layer_weights;
+    w_out = a.weight_out + blockIdx.z * a.layer_weights;
+    whole = n >= 0 && n <= a.max_seq && (long long)n <= (long long)b.max_blocks * bs;
+    bool missing = false;
+    if (whole)
+      for (int j = threadIdx.x; (long long)j * bs < n; j += blockDim.x) missing |= table[j] < 0 || table[j] >= c.n_blocks;
+    whole = !__syncthreads_or(missing) && whole;
+    cut = whole && keep >= 0 && keep < n;
+    recent = min(a.recent, cut ? keep : 0);
+    cand = n - recent;
+    first = keep - recent;
+    if (head == 0 && blockIdx.z == 0 && threadIdx.x == 0) a.seq_out[req] = cut ? keep : n;
+  }
+  __device__ __forceinline__ long long weight_at(int t) const {
+    return ((long long)table[t >> c.block_shift] * c.kv_heads + head) * c.block_size + (t & (c.block_size - 1));
+  }
+  __device__ __forceinline__ uint8_t *cell(int t) const { return c.at(table[t >> c.block_shift], head); }
+  template <int HD>
+  __device__ __forceinline__ void load(EvictPiece<HD> &p, int t, int lane16) const {
+    p.load(cell(t), w_in + weight_at(t), t & (c.block_size - 1), c.block_size, lane16);
+  }
+  template <int HD>
+  __device__ __forceinline__ void store(const EvictPiece<HD> &p, int t, int lane16) const {
+    p.store(cell(t), w_out + weight_at(t), t & (c.block_size - 1), c.block_size, lane16);
+  }
+  // A request that loses nothing: its weights go where they are wanted.
+  __device__ __forceinline__ void pass_weights() const {
+    if (whole && w_in != w_out)
+      for (int t = threadIdx.x; t < n; t += blockDim.x) w_out[weight_at(t)] = w_in[weight_at(t)];
+  }
+};
+
+// The bin, counted from the last, in which the `left`-th lies: {bin, how many of it are wanted}.  Clears the bins.  All of the workgroup's threads.
+template <int W, int BINS>
+__device__ __forceinline__ uint2 evict_bin(uint32_t *hist, uint32_t left, uint32_t *part, uint2 *pick) {
+  constexpr int PER = BINS / (W * 64);
+  static_assert(PER >= 1 && BINS % (W * 64) == 0, "bins per thread");
+  uint32_t h[PER], sum = 0, none = 0;
+  const int top = BINS - 1 - threadIdx.x * PER;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    h[i] = hist[top - i];
+    hist[top - i] = 0;
+    sum += h[i];
+  }
+  uint32_t before = plan_scan<W>(sum, none, part) - sum;
+  if (before < left && left <= before + sum) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (before < left && left <= before + h[i]) *pick = make_uint2(top - i, left - before);
+      before += h[i];
+    }
+  }
+  __syncthreads();
+  return *pick;
+}
+
 // Of the first n - recent tokens of a request the heaviest stay (in each layer and head for itself), and all of the last `recent`.  Tokens that
 // stay and lie behind the first keep - recent places fill the places of those that go, in order; then the last ones move up.  So
 // only what has to move is moved: a context at its budget that loses 64 of 2112 tokens moves 64 + the last ones, not 2048.
-// One workgroup per request, head and layer.  The threshold is found eight bits at a time (a histogram in LDS; counts do not depend on the order
-// of the atomics); holes and fillers are then listed chunk by chunk, both in order, and as many pairs as both lists hold are moved.
-template <int HD>
-__global__ __launch_bounds__(kEvictThreads) void kv4_evict(Kv4Cache c, PagedBatch b, EvictArgs a) {
-  constexpr int N = kEvictThreads, W = N / 64;
-  __shared__ uint32_t hist[256], part[W];
-  __shared__ uint32_t s_pick[3];
-  __shared__ int holes[kEvictQueue + N], fillers[kEvictQueue + N];
-  const int head = blockIdx.x, req = blockIdx.y, tid = threadIdx.x, bs = c.block_size;
-  const int32_t *table = b.table + (long long)req * b.max_blocks;
-  const int n = b.seq_len[req], keep = a.keep[req];
-  c.pool += blockIdx.z * a.layer_bytes;
-  const float *w_in = a.weight_in + blockIdx.z * a.layer_weights;
-  float *w_out = a.weight_out + blockIdx.z * a.layer_weights;
-  bool whole = n >= 0 && n <= a.max_seq && (long long)n <= (long long)b.max_blocks * bs;
-  bool missing = false;
-  if (whole)
-    for (int j = tid; (long long)j * bs < n; j += N) missing |= table[j] < 0 || table[j] >= c.n_blocks;
-  whole = !__syncthreads_or(missing) && whole;
-  const bool cut = whole && keep >= 0 && keep < n;
-  if (head == 0 && blockIdx.z == 0 && tid == 0) a.seq_out[req] = cut ? keep : n;
-  if (!whole) return;
-  auto place = [&](int t) { return ((long long)table[t >> c.block_shift] * c.kv_heads + head) * bs + (t & (bs - 1)); };
-  const int recent = min(a.recent, cut ? keep : 0), cand = n - recent, first = keep - recent;   // candidates, and how many of them stay
-  if (!cut) {
-    if (w_in != w_out)
-      for (int t = tid; t < n; t += N) w_out[place(t)] = w_in[place(t)];
+// One workgroup per request, head and layer.  A thread holds the keys of E tokens that follow each other; the threshold is found 11 bits at a time (a
+// histogram in LDS; counts do not depend on the order of the atomics), then two sums over the workgroup say which of the tokens at the threshold stay (the
+// lowest) and where every hole and every filler stands in its list.  The moves are read in lots, all of a lot before any of it is written: places lie
+// before the tokens of later lots, so what is read is never new.
+constexpr int kEvictLot = 4;                        // moves that a sixteenth of a wave's lanes reads at once
+template <int HD, int W, int E>
+__global__ __launch_bounds__(W * 64) void kv4_evict_held(Kv4Cache cache, PagedBatch b, EvictArgs a) {
+  constexpr int N = W * 64, BINS = 2048;
+  __shared__ uint32_t hist[BINS], part[W];
+  __shared__ uint2 pick;
+  __shared__ uint16_t holes[N * E / 2], fillers[N * E / 2];
+  const int tid = threadIdx.x;
+  for (int i = tid; i < BINS; i += N) hist[i] = 0;
+  const EvictTask k(cache, b, a);
+  if (!k.cut) {
+    k.pass_weights();
     return;
   }
+  const int t0 = tid * E;
+  uint32_t key[E];
+  float w[E];
+  if (t0 < k.n) {                                   // E is a part of 16, so these are in one block
+    const float *from = k.w_in + k.weight_at(t0);
+#pragma unroll
+    for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4 *>(w + i) = *reinterpret_cast<const f32x4 *>(from + i);
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) key[i] = t0 + i < k.cand ? evict_key(w[i]) : 0;
+  uint32_t prefix = 0, left = (uint32_t)k.first;
+  if (k.first) {
+    auto digit = [&](int shift, int above, uint32_t mask) {
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (t0 + i < k.cand && (above > 31 || key[i] >> above == prefix >> above)) atomicAdd(&hist[key[i] >> shift & mask], 1u);
+      __syncthreads();
+      const uint2 d = evict_bin<W, BINS>(hist, left, part, &pick);
+      prefix |= d.x << shift;
+      left = d.y;
+      __syncthreads();
+    };
+    digit(21, 32, 2047);
+    digit(10, 21, 2047);
+    digit(0, 10, 1023);
+  }
+  // tokens at the threshold: the first `left` stay
+  uint32_t equal = 0, none = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) equal += t0 + i < k.cand && key[i] == prefix;
+  uint32_t before = plan_scan<W>(equal, none, part) - equal;
+  uint32_t stays = 0, counts = 0;                   // holes in the low half, fillers in the high
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const bool in = t0 + i < k.cand && k.first, eq = in && key[i] == prefix;
+    const bool yes = in && (key[i] > prefix || (eq && before < left));
+    before += eq;
+    stays |= (uint32_t)yes << i;
+    counts += t0 + i < k.first ? !yes : yes ? 0x10000u : 0u;
+  }
+  none = 0;
+  uint32_t at = plan_scan<W>(counts, none, part) - counts;
+  const int fills = (int)(none & 0xFFFFu);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const bool yes = stays >> i & 1;
+    if (t0 + i < k.first) {
+      if (!yes) holes[at & 0xFFFFu] = (uint16_t)(t0 + i), ++at;
+      else if (k.w_in != k.w_out) k.w_out[k.weight_at(t0 + i)] = w[i];
+    } else if (yes) fillers[at >> 16] = (uint16_t)(t0 + i), at += 0x10000u;
+  }
+  __syncthreads();
+  const int moves = fills + k.recent, lane16 = tid & 15;
+  for (int m0 = 0; m0 < moves; m0 += N / 16 * kEvictLot) {
+    EvictPiece<HD> p[kEvictLot];
+    int to[kEvictLot];
+#pragma unroll
+    for (int i = 0; i < kEvictLot; ++i) {
+      const int m = m0 + i * (N / 16) + tid / 16;
+      to[i] = m >= moves ? -1 : m < fills ? (int)holes[m] : k.first + m - fills;
+      if (to[i] >= 0) k.load(p[i], m < fills ? (int)fillers[m] : k.cand + m - fills, lane16);
+    }
+    wait_vmcnt_all();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEvictLot; ++i)
+      if (to[i] >= 0) k.store(p[i], to[i], lane16);
+  }
+}
+
+// The same for any length: the weights are read again where they are needed, eight bits of the threshold at a time, and holes and fillers are listed chunk by
+// chunk, both in order; as many pairs as both lists hold are moved.
+template <int HD>
+__global__ __launch_bounds__(kEvictThreads) void kv4_evict(Kv4Cache cache, PagedBatch b, EvictArgs a) {
+  constexpr int N = kEvictThreads, W = N / 64, BINS = 1024;
+  __shared__ uint32_t hist[BINS], part[W];
+  __shared__ uint2 pick;
+  __shared__ int holes[kEvictQueue + N], fillers[kEvictQueue + N];
+  const int tid = threadIdx.x;
+  hist[tid] = 0;
+  const EvictTask k(cache, b, a);
+  if (!k.cut) {
+    k.pass_weights();
+    return;
+  }
+  const int cand = k.cand, first = k.first;
+  auto key_of = [&](int t) { return evict_key(k.w_in[k.weight_at(t)]); };
   // the key of the lightest that stays, and how many with that key stay
   uint32_t prefix = 0, left = (uint32_t)first;
   for (int shift = 24; shift >= 0 && first; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
     for (int t = tid; t < cand; t += N) {
-      const uint32_t key = evict_key(w_in[place(t)]);
+      const uint32_t key = key_of(t);
       if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[key >> shift & 255], 1u);
     }
     __syncthreads();
-    if (tid == 0) {
-      uint32_t sum = 0;
-      int d = 255;
-      for (; d > 0 && sum + hist[d] < left; --d) sum += hist[d];
-      s_pick[0] = prefix | (uint32_t)d << shift;
-      s_pick[1] = left - sum;
-    }
-    __syncthreads();
-    prefix = s_pick[0], left = s_pick[1];
+    const uint2 d = evict_bin<W, BINS>(hist, left, part, &pick);
+    prefix |= d.x << shift;
+    left = d.y;
     __syncthreads();
   }
   // which tokens stay, chunk by chunk and in order: equal ones from the lowest on
   uint32_t equal_holes = 0, equal_behind = 0;       // tokens with the threshold's key before the chunk, in either region
-  for (int t0 = 0; t0 < first; t0 += N) {
-    const bool eq = t0 + tid < first && evict_key(w_in[place(t0 + tid)]) == prefix;
-    plan_scan<W>((uint32_t)eq, equal_behind, part);
-  }
+  for (int t0 = 0; t0 < first; t0 += N) plan_scan<W>((uint32_t)(t0 + tid < first && key_of(t0 + tid) == prefix), equal_behind, part);
   auto stays = [&](int t, int end, uint32_t &equal_before) {
-    const uint32_t key = t < end ? evict_key(w_in[place(t)]) : 0;
+    const uint32_t key = t < end ? key_of(t) : 0;
     const bool eq = t < end && key == prefix;
     const uint32_t rank = plan_scan<W>((uint32_t)eq, equal_before, part);
     return t < end && first && (key > prefix || (eq && rank <= left));
   };
-  const uint32_t behind0 = equal_behind;
-  (void)behind0;
   int at_hole = 0, at_filler = first, n_holes = 0, n_fillers = 0;
-  auto move_token = [&](int to, int from, int lane16) {
-    // 16 lanes move a token: 4 (2) bytes of key codes and of value codes each, exponents by the first
-    const int ti = to & (bs - 1), fi = from & (bs - 1);
-    uint8_t *d = c.at(table[to >> c.block_shift], head);
-    const uint8_t *s = c.at(table[from >> c.block_shift], head);
-    const int vd = Kv4Offsets<HD>::v_codes(bs) + (ti / 4) * (2 * HD) + lane16 * (HD / 8) + (ti % 4) * (HD / 32);
-    const int vs = Kv4Offsets<HD>::v_codes(bs) + (fi / 4) * (2 * HD) + lane16 * (HD / 8) + (fi % 4) * (HD / 32);
-    typedef std::conditional_t<HD == 128, uint32_t, uint16_t> Piece;
-    const Piece k = reinterpret_cast<const Piece *>(s + fi * (HD / 2))[lane16], v = *reinterpret_cast<const Piece *>(s + vs);
-    uint8_t e = 0;
-    const bool is_k = lane16 < HD / 32, is_v = lane16 >= HD / 32 && lane16 < HD / 16;
-    const int g = lane16 % (HD / 32);
-    const int ed = is_k ? Kv4Offsets<HD>::k_exp(bs) + ti * (HD / 32) + g : Kv4Offsets<HD>::v_exp(bs) + ((ti / 4) * (HD / 32) + g) * 4 + ti % 4;
-    const int es = is_k ? Kv4Offsets<HD>::k_exp(bs) + fi * (HD / 32) + g : Kv4Offsets<HD>::v_exp(bs) + ((fi / 4) * (HD / 32) + g) * 4 + fi % 4;
-    if (is_k || is_v) e = s[es];
-    const float w = w_in[place(from)];
-    return [=]() {
-      reinterpret_cast<Piece *>(d + ti * (HD / 2))[lane16] = k;
-      *reinterpret_cast<Piece *>(d + vd) = v;
-      if (is_k || is_v) d[ed] = e;
-      if (lane16 == 0) w_out[place(to)] = w;
-    };
-  };
   while (true) {
     while (n_holes < kEvictQueue && at_hole < first) {
       const int t = at_hole + tid;
@@ -278,7 +481,7 @@ __global__ __launch_bounds__(kEvictThreads) void kv4_evict(Kv4Cache c, PagedBatc
       uint32_t count = (uint32_t)n_holes;
       const uint32_t rank = plan_scan<W>((uint32_t)hole, count, part);
       if (hole) holes[rank - 1] = t;
-      if (yes && w_in != w_out) w_out[place(t)] = w_in[place(t)];
+      if (yes && k.w_in != k.w_out) k.w_out[k.weight_at(t)] = k.w_in[k.weight_at(t)];
       n_holes = (int)count;
       at_hole += N;
     }
@@ -294,7 +497,11 @@ __global__ __launch_bounds__(kEvictThreads) void kv4_evict(Kv4Cache c, PagedBatc
     __syncthreads();
     const int moves = min(n_holes, n_fillers);
     if (!moves) break;
-    for (int i = tid / 16; i < moves; i += N / 16) move_token(holes[i], fillers[i], tid & 15)();
+    for (int i = tid / 16; i < moves; i += N / 16) {
+      EvictPiece<HD> p;
+      k.load(p, fillers[i], tid & 15);
+      k.store(p, holes[i], tid & 15);
+    }
     __syncthreads();
     // what is left of either list moves to its front
     const int left_holes = n_holes - moves, left_fillers = n_fillers - moves;
@@ -307,15 +514,16 @@ __global__ __launch_bounds__(kEvictThreads) void kv4_evict(Kv4Cache c, PagedBatc
     }
     n_holes = left_holes, n_fillers = left_fillers;
   }
-  // the last ones move up; a chunk is read before it is written, and its places lie before those of later chunks
+  // the last ones move up; a chunk is read before it is written, and its places lie before the tokens of later chunks
+  wait_vmcnt_all();
   __syncthreads();
-  for (int i0 = 0; i0 < recent; i0 += N / 16) {
+  for (int i0 = 0; i0 < k.recent; i0 += N / 16) {
     const int i = i0 + tid / 16;
-    const bool in = i < recent;
-    const auto write = move_token(first + (in ? i : recent - 1), cand + (in ? i : recent - 1), tid & 15);
+    EvictPiece<HD> p;
+    if (i < k.recent) k.load(p, cand + i, tid & 15);
+    wait_vmcnt_all();
     __syncthreads();
-    if (in) write();
-    __syncthreads();
+    if (i < k.recent) k.store(p, first + i, tid & 15);
   }
 }
 
