@@ -148,22 +148,36 @@ static int groups_desc_ok(const char *who, const heisd_prefix_groups *g, PrefixG
   return HEISD_OK;
 }
 
-// As Kv4Plan, with the groups' work beside the requests'.
+// As Kv4Plan, with the groups' work beside the requests'.  Groups of many columns are kv4_prefix's, and then a request's own tokens are not cut where that
+// leaves enough workgroups.
+constexpr int64_t kWideLeast = 64, kWideMany = 192, kWholeTokens = 1024;
 struct SharedPlan {
-  int col_tiles;
-  int64_t groups;
-  size_t part_ml, whole, whole_ml, total;
+  int col_tiles, unit, wide_waves, own_tiles;
+  int64_t groups, wide;
+  bool joins;
+  size_t part_ml, whole, whole_ml, wide_part, wide_ml, total;
   SharedPlan(int64_t batch, int64_t rows, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, const PrefixGroups &p, int64_t head_dim) {
-    const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::max<int64_t>(own_cols, std::min<int64_t>((int64_t)p.max_rows * group, 1 << 22));
-    col_tiles = cols > 16 ? 2 : 1;
+    const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::min<int64_t>(std::min<int64_t>(p.max_rows, rows) * group, 1 << 22);
+    wide_waves = cols >= kWideMany ? 8 : 4;
+    const int64_t wide_cols = 32 * wide_waves;
+    wide = p.groups && cols >= kWideLeast
+               ? std::min<int64_t>(p.groups * kv_heads * ((cols + wide_cols - 1) / wide_cols) * ((p.max_prefix + 255) / 256), 8 / wide_waves * kKv4Units) : 0;
+    col_tiles = (wide ? own_cols : std::max(own_cols, cols)) > 16 ? 2 : 1;
     const int64_t tile = 16 * col_tiles, most = kv4_per_unit((int)head_dim, col_tiles) * kKv4Units;
-    const int64_t own = batch * std::min<int64_t>(kv_heads * ((own_cols + tile - 1) / tile), 65535) * ((max_seq + kKv4Unit - 1) / kKv4Unit);
-    const int64_t shared = (int64_t)p.groups * std::min<int64_t>(kv_heads * ((cols + tile - 1) / tile), 65535) * ((p.max_prefix + kKv4Unit - 1) / kKv4Unit);
-    groups = std::max<int64_t>(1, std::min<int64_t>((own + shared + 1) / 2, most));
+    const int64_t segments = batch * std::min<int64_t>(kv_heads * ((own_cols + tile - 1) / tile), 65535);
+    unit = wide && max_seq <= kWholeTokens ? kWholeTokens : kKv4Unit;
+    const int64_t own = segments * ((max_seq + unit - 1) / unit);
+    const int64_t shared = wide ? 0 : (int64_t)p.groups * std::min<int64_t>(kv_heads * ((cols + tile - 1) / tile), 65535) * ((p.max_prefix + kKv4Unit - 1) / kKv4Unit);
+    joins = !wide || unit == kKv4Unit || own > kMostGroups || kv_heads * ((own_cols + tile - 1) / tile) > 65535;
+    if (joins) unit = kKv4Unit;
+    own_tiles = joins ? 0 : (int)(segments / batch / kv_heads);
+    groups = joins ? std::max<int64_t>(1, std::min<int64_t>((own + shared + 1) / 2, most)) : own;
     part_ml = align256((size_t)2 * groups * tile * head_dim * sizeof(float));
     whole = part_ml + align256((size_t)2 * groups * tile * 2 * sizeof(float));
     whole_ml = whole + align256((size_t)2 * rows * group * kv_heads * head_dim * sizeof(float));
-    total = whole_ml + align256((size_t)2 * rows * group * kv_heads * 2 * sizeof(float));
+    wide_part = whole_ml + align256((size_t)2 * rows * group * kv_heads * 2 * sizeof(float));
+    wide_ml = wide_part + align256((size_t)2 * wide * wide_cols * head_dim * sizeof(float));
+    total = wide_ml + align256((size_t)2 * wide * wide_cols * 2 * sizeof(float));
   }
 };
 
@@ -177,16 +191,40 @@ extern "C" size_t heisd_kv4_shared_attention_workspace_bytes(const heisd_kv4_des
   return SharedPlan(batch, rows, cache->kv_heads, q_heads / cache->kv_heads, max_q, max_seq, p, cache->head_dim).total;
 }
 
+template <typename T, int HD, int W>
+static hipError_t kv4_prefix_launch(const Kv4Cache &c, const PagedBatch &b, const HeadRows<const T> &q, const Kv4SharedAttend &a, hipStream_t st) {
+  constexpr int lds = wide_lds_bytes<HD>;
+  if constexpr (lds > 65536 - 1024) {                // above the usual limit of a workgroup (which has 1 KB beside it), which is raised once per device
+    static std::atomic<bool> raised[kRetrieveMaxDevices];
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && (dev < 0 || dev >= kRetrieveMaxDevices)) e = hipErrorInvalidDevice;
+    if (e == hipSuccess && !raised[dev].load()) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv4_prefix<T, HD, W>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e == hipSuccess) raised[dev].store(true);
+    }
+    if (e != hipSuccess) return e;
+  }
+  kv4_prefix<T, HD, W><<<dim3((unsigned)a.wide), dim3(64 * W), lds, st>>>(c, b, q, a);
+  return hipSuccess;
+}
+
 template <typename T, int HD, int TERMS>
-static void kv4_shared_launch(const Kv4Cache &c, const PagedBatch &b, const heisd_head_rows *q, const heisd_head_rows *out, const Kv4SharedAttend &a,
+static hipError_t kv4_shared_launch(const Kv4Cache &c, const PagedBatch &b, const heisd_head_rows *q, const heisd_head_rows *out, const Kv4SharedAttend &a,
                               const SharedPlan &plan, int max_q, hipStream_t st) {
   const HeadRows<T> qi = head_rows<T>(*q), o = head_rows<T>(*out);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
   const dim3 block(256), grid((unsigned)plan.groups);
+  if (plan.wide) {
+    const hipError_t e = plan.wide_waves == 8 ? kv4_prefix_launch<T, HD, 8>(c, b, qc, a, st) : kv4_prefix_launch<T, HD, 4>(c, b, qc, a, st);
+    if (e != hipSuccess) return e;
+  }
   if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
   else kv4_attend<T, HD, 1, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
+  if (!plan.joins) return hipSuccess;
   const int64_t per = 256 / (HD / 4), cols = std::min<int64_t>((int64_t)max_q * a.q_heads, (int64_t)b.rows * a.q_heads);
   kv4_shared_join<T, HD><<<dim3((unsigned)std::min<int64_t>((cols + per - 1) / per, 65535), b.batch), block, 0, st>>>(c, b, o, a, (int)plan.groups);
+  return hipSuccess;
 }
 
 extern "C" int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const heisd_paged_batch *batch, const heisd_prefix_groups *groups,
@@ -218,17 +256,25 @@ extern "C" int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const hei
                                           scale < 0, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
                                           reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + plan.part_ml), lse};
   a.prefix = p;
+  a.unit = plan.unit;
+  a.wide = (int)plan.wide;
+  a.wide_cols = 32 * plan.wide_waves;
+  a.own_tiles = plan.own_tiles;
+  a.wide_part = reinterpret_cast<float *>(ws + plan.wide_part);
+  a.wide_ml = reinterpret_cast<float *>(ws + plan.wide_ml);
   a.whole = reinterpret_cast<float *>(ws + plan.whole);
   a.whole_ml = reinterpret_cast<float *>(ws + plan.whole_ml);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  hipError_t e;
   if (q->dtype == HEISD_DTYPE_BF16) {
-    if (cache->head_dim == 128) kv4_shared_launch<__bf16, 128, 1>(c, b, q, out, a, plan, max_q, st);
-    else kv4_shared_launch<__bf16, 64, 1>(c, b, q, out, a, plan, max_q, st);
+    if (cache->head_dim == 128) e = kv4_shared_launch<__bf16, 128, 1>(c, b, q, out, a, plan, max_q, st);
+    else e = kv4_shared_launch<__bf16, 64, 1>(c, b, q, out, a, plan, max_q, st);
   } else {
-    if (cache->head_dim == 128) kv4_shared_launch<_Float16, 128, 2>(c, b, q, out, a, plan, max_q, st);
-    else kv4_shared_launch<_Float16, 64, 2>(c, b, q, out, a, plan, max_q, st);
+    if (cache->head_dim == 128) e = kv4_shared_launch<_Float16, 128, 2>(c, b, q, out, a, plan, max_q, st);
+    else e = kv4_shared_launch<_Float16, 64, 2>(c, b, q, out, a, plan, max_q, st);
   }
+  if (e != hipSuccess) return fail(nullptr, HEISD_EHIP, "%s: %s", who, hipGetErrorString(e));
   return launched(who);
 }
 

@@ -243,13 +243,6 @@ struct Kv4Attend {
   float *part, *part_ml;                            // sums of unfinished segments [2 * workgroups][cols][HD], their maxima and sums [..][cols][2]
   float *lse;
 };
-// With groups that share a prefix: they come behind the requests, as if they were requests whose rows are all of the group's and that see all of
-// their tokens.  A row has two parts then, and what a segment gives is always kept: [own, prefix][rows][q_heads] sums, maxima and sums.
-struct Kv4SharedAttend : Kv4Attend {
-  PrefixGroups prefix;
-  float *whole, *whole_ml;
-};
-
 // Work is counted in units: 128 tokens (a pair of tiles for each wave) of one request, key head and group of columns - a segment is all
 // units of such a three.  Every workgroup takes an equal run of the units of the whole call, whatever the requests' lengths are.
 // A workgroup per chunk of 1024 tokens instead: 71 us with 64 contexts of 256 to 8191 tokens, where runs took 62 (the last chunks left most of
@@ -273,16 +266,6 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const Paged
   if (r.seq < 0 || r.seq > a.max_seq || (long long)r.seq > (long long)b.max_blocks * c.block_size) r.seq = 0;
   r.units = max((r.seq + kKv4Unit - 1) / kKv4Unit, 1);          // one even without tokens: somebody writes the zeros
   r.work = (long long)r.units * ((r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads);
-  return r;
-}
-
-__device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4Attend &) { return b.batch; }
-__device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4SharedAttend &a) { return b.batch + a.prefix.groups; }
-__device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int i) {
-  if (i < b.batch) return kv4_request(c, b, static_cast<const Kv4Attend &>(a), i);
-  const PrefixSpan s = prefix_span(c, b, a.prefix, i - b.batch);
-  Kv4Request r{s.rows, s.tokens, max((s.tokens + kKv4Unit - 1) / kKv4Unit, 1), 0};
-  r.work = (long long)r.units * ((r.rows.count * (long long)a.group + a.cols - 1) / a.cols * c.kv_heads);
   return r;
 }
 
@@ -313,6 +296,141 @@ __device__ __forceinline__ bool kv4_saw(float m, float l) { return m != -INFINIT
 // What such a part's sums are multiplied by where the maximum over all parts is `top`.
 __device__ __forceinline__ float kv4_weight(float m, float top) { return m == -INFINITY ? 1.f : exp2_fast(m - top); }
 
+// ---- parts of a row --------------------------------------------------------------------------------------------------
+
+// Sums, maximum and sum of probabilities of a column, in the order of its tokens.
+struct Kv4Sums {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, sum = 0.f;
+  template <int K>
+  __device__ __forceinline__ void add(const float2 (&ml)[K], const f32x4 (&x)[K]) {
+    float next = top;
+#pragma unroll
+    for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
+    const float keep = kv4_weight(top, next);
+    sum *= keep;
+    o *= keep;
+    top = next;
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (kv4_saw(ml[i].x, ml[i].y)) {
+        const float by = kv4_weight(ml[i].x, top);
+        sum += ml[i].y * by;
+        o += x[i] * by;
+      }
+  }
+};
+
+// With groups that share a prefix.  Narrow: they come behind the requests, as if they were requests whose rows are all of the group's and that see all of their
+// tokens; kv4_shared_join joins a row's own tokens and its prefix.  Wide (groups of many columns): kv4_prefix has done the prefixes before, in runs of
+// `wide` workgroups, and whoever ends a row's own tokens joins them.  What a segment of a prefix (narrow: any segment) gives is kept: whole ones by row,
+// [own, prefix][rows][q_heads], the others by workgroup.
+constexpr int kWideTokens = 64;                     // of a unit of kv4_prefix's work
+struct Kv4SharedAttend : Kv4Attend {
+  PrefixGroups prefix;
+  int unit;                                         // tokens of a unit of own work
+  int wide, wide_cols;                              // workgroups of kv4_prefix, columns that one takes at a time
+  int own_tiles;                                    // not 0: every workgroup has one segment of own tokens, request by request, own_tiles for each key head (and more, one after the other, where max_q does not hold)
+  float *whole, *whole_ml, *wide_part, *wide_ml;
+};
+__device__ __forceinline__ constexpr int kv4_unit(const Kv4Attend &) { return kKv4Unit; }
+__device__ __forceinline__ int kv4_unit(const Kv4SharedAttend &a) { return a.unit; }
+__device__ __forceinline__ constexpr int kv4_own_tiles(const Kv4Attend &) { return 0; }
+__device__ __forceinline__ int kv4_own_tiles(const Kv4SharedAttend &a) { return a.own_tiles; }
+__device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4Attend &) { return b.batch; }
+__device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4SharedAttend &a) { return a.wide ? b.batch : b.batch + a.prefix.groups; }
+__device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int i) {
+  Kv4Request r;
+  if (i < b.batch) {
+    r = kv4_request(c, b, static_cast<const Kv4Attend &>(a), i);
+  } else {
+    const PrefixSpan s = prefix_span(c, b, a.prefix, i - b.batch);
+    r.rows = s.rows, r.seq = s.tokens;
+  }
+  r.units = max((r.seq + a.unit - 1) / a.unit, 1);
+  r.work = (long long)r.units * ((r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads);
+  return r;
+}
+// A group's work for kv4_prefix.
+__device__ __forceinline__ Kv4Request wide_request(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int g) {
+  const PrefixSpan s = prefix_span(c, b, a.prefix, g);
+  Kv4Request r{s.rows, s.tokens, (s.tokens + kWideTokens - 1) / kWideTokens, 0};
+  r.work = (long long)r.units * ((r.rows.count * a.group + a.wide_cols - 1) / a.wide_cols * c.kv_heads);
+  return r;
+}
+
+// Which group request i belongs to (-1: none).  Groups that are described follow each other, so at most one does.
+__device__ __forceinline__ int group_of(const PrefixGroups &p, int i) {
+  const int lane = threadIdx.x & 63;
+  for (int g0 = 0; g0 < p.groups; g0 += 64) {
+    const int g = min(g0 + lane, p.groups - 1);
+    const unsigned long long m = __ballot(p.first[g] <= i && i < p.first[g + 1]);
+    if (m) return g0 + __builtin_ctzll(m);
+  }
+  return -1;
+}
+
+// Where the parts of a request's (a group's) segments are.
+struct Kv4Parts {
+  Kv4Request r;
+  long long before, per;                            // work before it, work of a workgroup
+  int cols;
+  const float *part, *part_ml;
+  // Where a column's parts are: the workgroups from w0 to w1 have them, w0 in first_slot, the others (which begin their runs inside the segment) in
+  // the first of their two slots; n: the column's place in a slot.  w0 = w1: one workgroup has all, which is kept by row.  w1 < w0: none.
+  struct Place {
+    int w0, w1, first_slot, n;
+  };
+  __device__ __forceinline__ Place place(int kv_heads, int head, int col) const {
+    const long long s0 = before + ((long long)(col / cols) * kv_heads + head) * r.units;
+    const int w0 = (int)wave_div(s0, per);
+    return Place{w0, (int)wave_div(s0 + r.units - 1, per), 2 * w0 + (w0 * per != s0), col % cols};
+  }
+  // Adds what it has of 4 channels from d on.  whole: where the column's are if one workgroup has all.
+  template <int HD>
+  __device__ __forceinline__ void add(Kv4Sums &s, const Place &p, int d, const float *whole, const float *whole_ml) const {
+    if (p.w0 == p.w1) {
+      const float2 ml[1] = {*reinterpret_cast<const float2 *>(whole_ml)};
+      const f32x4 x[1] = {*reinterpret_cast<const f32x4 *>(whole + d)};
+      s.add(ml, x);
+      return;
+    }
+    constexpr int K = 4;                                                           // parts requested at once
+    for (int i = p.w0; i <= p.w1; i += K) {
+      float2 ml[K];
+      f32x4 x[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int wi = min(i + k, p.w1);
+        const long long at = (long long)(wi == p.w0 ? p.first_slot : 2 * wi) * cols + p.n;
+        ml[k] = *reinterpret_cast<const float2 *>(part_ml + at * 2);
+        x[k] = *reinterpret_cast<const f32x4 *>(part + at * HD + d);
+        if (i + k > p.w1) ml[k] = make_float2(-INFINITY, 0.f);
+      }
+      s.add(ml, x);
+    }
+  }
+};
+// The parts of a group's prefix that kv4_prefix left.  A wave's.
+__device__ __forceinline__ Kv4Parts wide_parts(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int g) {
+  const int lane = threadIdx.x & 63;
+  Kv4Parts p{wide_request(c, b, a, g), 0, 0, a.wide_cols, a.wide_part, a.wide_ml};
+  long long all = 0;
+  for (int i = lane; i < a.prefix.groups; i += 64) {
+    const long long work = wide_request(c, b, a, i).work;
+    all += work;
+    if (i < g) p.before += work;
+  }
+  p.before = wave_sum64(p.before);
+  p.per = kv4_run(wave_sum64(all), a.wide);
+  return p;
+}
+// Is the request there (or has it been left out)?
+__device__ __forceinline__ bool kv4_live(const Kv4Cache &c, const PagedBatch &b, const Kv4Attend &a, int req) {
+  const int n = b.seq_len[req];
+  return n >= 0 && n <= a.max_seq && (long long)n <= (long long)b.max_blocks * c.block_size;
+}
+
 // softmax(q K^T) V over the tokens of segments.  The query rows of the heads that share the key head are the columns of the matrix products (CT tiles of
 // 16): scores^T = K q^T (tokens are rows), out^T = V^T p^T.  A lane holds the scores of one column and four tokens of each tile, which are
 // its summed indices of the second product, so the probabilities never leave their lane.  Four waves take pairs of tiles in turn,
@@ -332,6 +450,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
   __shared__ float s_m[4][16], s_l[4][16];
   __shared__ long long s_start[4][64];                          // a wave's own: on its way to a later request another may be behind
   __shared__ int4 s_req[4][64];
+  __shared__ Kv4Parts::Place s_place[SHARED ? 16 : 1];          // wide: where the parts of the prefix are, a column each
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int bs = c.block_size;
 
@@ -353,10 +472,13 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     s_start[wave][lane] = start + before - r.work;
     s_req[wave][lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
   };
-  requests(0);
+  bool direct = false;
+  if constexpr (SHARED) direct = a.own_tiles != 0;
+  if (!direct) requests(0);
+  else end = 1ll << 62;
   long long all = end;
-  for (int i = 64; i < n_requests; i += 64) all += wave_sum64(i + lane < n_requests ? kv4_request(c, b, a, i + lane).work : 0);
-  const long long per = kv4_run(all, gridDim.x), run0 = blockIdx.x * per, run1 = min(run0 + per, all);
+  for (int i = 64; i < n_requests && !direct; i += 64) all += wave_sum64(i + lane < n_requests ? kv4_request(c, b, a, i + lane).work : 0);
+  const long long per = kv4_run(all, gridDim.x), run0 = direct ? 0 : blockIdx.x * per, run1 = direct ? all : min(run0 + per, all);
 
   for (long long at = run0; at < run1;) {
     while (at >= end && first + 64 < n_requests) {
@@ -364,12 +486,20 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       requests(end);
     }
     if (at >= end) break;                                       // not reached while the lengths stay as they are
-    const int local = 63 - __clzll(__ballot(s_start[wave][lane] <= at));      // the last of those that begin here has the work
-    const int req = first + local;
-    const int4 rq = s_req[wave][local];
+    int local = 0, req;
+    int4 rq;
+    if (SHARED && direct) {
+      req = blockIdx.x / (c.kv_heads * max(kv4_own_tiles(a), 1));
+      const Kv4Request r = kv4_request(c, b, a, req);
+      rq = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
+    } else {
+      local = 63 - __clzll(__ballot(s_start[wave][lane] <= at));             // the last of those that begin here has the work
+      req = first + local;
+      rq = s_req[wave][local];
+    }
     const Span rows{__builtin_amdgcn_readfirstlane(rq.x), __builtin_amdgcn_readfirstlane(rq.y)};
     const int seq = __builtin_amdgcn_readfirstlane(rq.z), units = __builtin_amdgcn_readfirstlane(rq.w);
-    const long long in_req = at - lane_value64(s_start[wave][lane], local);
+    const long long in_req = direct ? blockIdx.x + (at - req) * c.kv_heads * kv4_own_tiles(a) : at - lane_value64(s_start[wave][lane], local);
     const int segment = __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
     const int u0 = __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
     const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
@@ -377,7 +507,8 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     const bool whole = u0 == 0 && u1 == units;
     const long long slot = 2 * (long long)blockIdx.x + (at != run0);
     const int n_cols = rows.count * a.group;
-    const int t1 = min(seq, u1 * kKv4Unit);
+    if (SHARED && direct && col0 >= n_cols) break;
+    const int unit = kv4_unit(a), t1 = (int)min((long long)seq, (long long)u1 * unit);
     int owner = req, few = seq - rows.count + 1;                  // whose blocks; tokens that every row sees
     if constexpr (SHARED)
       if (req >= b.batch) owner = __builtin_amdgcn_readfirstlane(a.prefix.prefix[req - b.batch]), few = seq;
@@ -577,7 +708,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       }
       __builtin_amdgcn_sched_barrier(0);
     };
-    for (t0 = u0 * kKv4Unit; t0 < t1; t0 += 32 * kKv4Unit) {
+    for (t0 = u0 * unit; t0 < t1; t0 += 32 * kKv4Unit) {
       // the blocks of the wave's tiles: lane 2 i + n holds that of tile n of its i-th pair of these 32
       const int t = t0 + 32 * (wave + 4 * (lane >> 1)) + 16 * (lane & 1);
       my_id = t < t1 ? table[t >> c.block_shift] : -1;
@@ -598,7 +729,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     // what is not finite makes NaN of the columns that do see it (rare: the exponents of all of the wave's tokens are read again)
     uint32_t nan_out = 0;                                       // bit ct: the lane's column of tile ct, in the lane's channels
     if (__ballot(odd)) {
-      for (int t = u0 * kKv4Unit; t < t1; ++t) {
+      for (int t = u0 * unit; t < t1; ++t) {
         if ((t / 32 - wave) % 4) continue;
         const int id = table[t >> c.block_shift], o = t & (bs - 1);
         if (id < 0 || id >= c.n_blocks) continue;
@@ -607,6 +738,12 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
         for (int ct = 0; ct < CT; ++ct) nan_out |= (uint32_t)(e >= kKv4NotFinite && t < seen[ct]) << ct;
       }
     }
+    [[maybe_unused]] Kv4Parts prefix{};                         // wide: of this request's prefix
+    if constexpr (SHARED)
+      if (a.wide && whole && kv4_live(c, b, a, req)) {
+        const int g = group_of(a.prefix, req);
+        if (g >= 0) prefix = wide_parts(c, b, a, g);
+      }
     // join the waves, a tile of columns at a time
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -620,6 +757,13 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int d = 0; d < ND; ++d) to[(4 * quad + e) * ND + d] = nan_out >> ct & 1 ? __uint_as_float(0x7FC00000u) : acc[ct][d][e];
+      if constexpr (SHARED)
+        if (a.wide && whole && threadIdx.x < 16) {
+          const int cn = min(col0 + ct * 16 + col, n_cols - 1), i = cn / a.group;
+          const long long in_group = (long long)rows.begin + i - prefix.r.rows.begin;
+          s_place[col] = prefix.r.work > 0 && in_group >= 0 && in_group < prefix.r.rows.count
+                             ? prefix.place(c.kv_heads, head, (int)in_group * a.group + cn - i * a.group) : Kv4Parts::Place{0, -1, 0, 0};
+        }
       __syncthreads();
       for (int u = threadIdx.x; u < 16 * (HD / 4); u += 256) {
         const int n = u / (HD / 4), d = u % (HD / 4) * 4, cn = col0 + ct * 16 + n;
@@ -638,9 +782,18 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
         const long long r = rows.begin + i;
         if (SHARED && whole) {
           if constexpr (SHARED) {
-            const long long at_row = ((long long)(req >= b.batch) * b.rows + r) * a.q_heads + h;
-            *reinterpret_cast<f32x4 *>(a.whole + at_row * HD + d) = o;
-            if (d == 0) *reinterpret_cast<float2 *>(a.whole_ml + at_row * 2) = make_float2(top, sum);
+            const long long at_row = ((long long)(a.wide || req >= b.batch) * b.rows + r) * a.q_heads + h;      // own tokens first, then prefixes
+            if (!a.wide) {
+              *reinterpret_cast<f32x4 *>(a.whole + at_row * HD + d) = o;
+              if (d == 0) *reinterpret_cast<float2 *>(a.whole_ml + at_row * 2) = make_float2(top, sum);
+            } else {
+              Kv4Sums s{o, top, sum};
+              prefix.add<HD>(s, s_place[n], d, a.whole + at_row * HD, a.whole_ml + at_row * 2);
+              const float inv = s.sum == 0.f ? 0.f : 1.f / s.sum;
+              float f[4] = {s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv};
+              store_vec<T, 4>(out.at(r, h) + d, f);
+              if (a.lse && d == 0) a.lse[r * a.q_heads + h] = s.sum == 0.f ? -INFINITY : (s.top + log2f(s.sum)) * 0.6931471805599453f;
+            }
           }
         } else if (whole) {
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -658,29 +811,6 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     at += u1 - u0;
   }
 }
-
-// Sums, maximum and sum of probabilities of a column, in the order of its tokens.
-struct Kv4Sums {
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float top = -INFINITY, sum = 0.f;
-  template <int K>
-  __device__ __forceinline__ void add(const float2 (&ml)[K], const f32x4 (&x)[K]) {
-    float next = top;
-#pragma unroll
-    for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
-    const float keep = kv4_weight(top, next);
-    sum *= keep;
-    o *= keep;
-    top = next;
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-      if (kv4_saw(ml[i].x, ml[i].y)) {
-        const float by = kv4_weight(ml[i].x, top);
-        sum += ml[i].y * by;
-        o += x[i] * by;
-      }
-  }
-};
 
 // Joins the parts of segments that several workgroups worked on, in the order of their tokens.  A workgroup per segment; 16 bytes of
 // a column per thread.

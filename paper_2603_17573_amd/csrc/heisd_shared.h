@@ -3,81 +3,424 @@
 #include "heisd_common.h"
 #include "heisd_kv4.h"
 #include "heisd_paged.h"
+#include "heisd_prompt.h"
 
 namespace heisd {
 
-// Which group request i belongs to (-1: none).  Groups that are described follow each other, so at most one does.
-__device__ __forceinline__ int group_of(const PrefixGroups &p, int i) {
-  const int lane = threadIdx.x & 63;
-  for (int g0 = 0; g0 < p.groups; g0 += 64) {
-    const int g = min(g0 + lane, p.groups - 1);
-    const unsigned long long m = __ballot(p.first[g] <= i && i < p.first[g + 1]);
-    if (m) return g0 + __builtin_ctzll(m);
+// ---- a prefix, for many rows ----------------------------------------------------------------------------------------------
+
+// Values enter the second product as fp16 (and keys the first, where the queries are fp16) where those of a run allow it: times 2^13 over the largest exponent of their
+// group of 32 channels (of all keys).  The sixteen codes times 2^-36 of that are still fp16 numbers, so nothing is rounded.  Where exponents lie further apart, or something
+// is not finite, all of it is bf16, with probabilities (and fp16 queries) as a bf16 and a remainder.  (Groups of e = 1, 6 2^-126 at most, may become zero beside others.)
+constexpr int kWideShift = 13, kWideSpread = 36;
+template <int HD>
+constexpr int wide_lds_bytes = 2 * 2 * kWideTokens * HD * 2 + 2 * kWideTokens;
+
+// softmax(q K^T) V over a run of a prefix's tokens.  A workgroup has 32 * W columns (rows of the group times the query heads of one key head), a wave
+// 32 of them; the products are those of prompt_attend.  64 tokens at a time become bf16 once for all columns, on their way into LDS: a lane brings 32
+// keys' values of a token, or four tokens' values of eight channels, 16 bytes of codes either way, requested a step ahead and its block's number two.  Which
+// bytes of LDS a row's pieces take is as in prompt_attend; K goes by tokens across the lanes and V by channels, so that no two lanes of a write
+// meet in a bank.  All columns see the same tokens: what nobody sees (behind the end, in missing blocks) has scores of minus infinity and values of zero.
+// Every workgroup takes an equal run of the work of all groups, as in kv4_attend; a unit is a step for 32 * W columns of a key head.
+template <typename T, int HD, int W>
+__global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b, HeadRows<const T> q, Kv4SharedAttend a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr int RB = HD * 2, CH = RB / 16, TILE = kWideTokens * RB, G = HD / 32;
+  constexpr int NS = HD / 16, ND = HD / 32, NT = kWideTokens / 32, NK = kWideTokens / 16;
+  constexpr int NU = (2 * G + W - 1) / W;           // of a wave's 2 * G lots of 64 lanes' loads
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  __shared__ int2 s_e[W][G + 1];
+  const int bs = c.block_size;
+  int first = 0;                                    // 64 groups are at hand, a lane each
+  Kv4Request mine;
+  long long start, end;
+  auto groups = [&](long long before) {
+    mine = wide_request(c, b, a, min(first + lane, a.prefix.groups - 1));
+    if (first + lane >= a.prefix.groups) mine.work = 0;
+    start = mine.work;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long t = __shfl_up(start, o);
+      if (lane >= o) start += t;
+    }
+    end = before + lane_value64(start, 63);
+    start += before - mine.work;
+  };
+  groups(0);
+  long long all = end;
+  for (int i = 64; i < a.prefix.groups; i += 64) all += wave_sum64(i + lane < a.prefix.groups ? wide_request(c, b, a, i + lane).work : 0);
+  const long long per = kv4_run(all, gridDim.x), run0 = blockIdx.x * per, run1 = min(run0 + per, all);
+  int head = 0, t_begin = 0, t_end = 0;
+  const int32_t *table = b.table;
+
+  // what this lane brings of a step: lots 0 .. G - 1 are keys' groups, the others a G-th of the values each
+  struct Lot {
+    u32x4 code;
+    uint32_t e;
+    int id;
+  };
+  Lot lot[NU];
+  auto lot_of = [&](int n) { return wave + n * W; };
+  auto token_of = [&](int n) {                      // within a step
+    if (lot_of(n) < G) return lane;
+    const int v = (lot_of(n) - G) * 64 + lane;
+    return v / (HD / 8) * 4;
+  };
+  auto ask_block = [&](int step, int n) {
+    const int t = t_begin + step * kWideTokens + token_of(n);
+    int id = t < t_end ? table[t >> c.block_shift] : -1;
+    return id >= c.n_blocks ? -1 : id;
+  };
+  auto ask_codes = [&](int step, int n) {
+    if (lot_of(n) >= 2 * G) return;
+    const int o = (t_begin + step * kWideTokens + token_of(n)) & (bs - 1);
+    const uint8_t *cell = c.at(max(lot[n].id, 0), head);
+    if (lot_of(n) < G) {
+      lot[n].code = *reinterpret_cast<const u32x4 *>(cell + o * (HD / 2) + lot_of(n) * 16);
+      lot[n].e = cell[Kv4Offsets<HD>::k_exp(bs) + o * G + lot_of(n)];
+    } else {
+      const int piece = lane % (HD / 8);
+      lot[n].code = *reinterpret_cast<const u32x4 *>(cell + Kv4Offsets<HD>::v_codes(bs) + o / 4 * (2 * HD) + piece * 16);
+      lot[n].e = *reinterpret_cast<const uint32_t *>(cell + Kv4Offsets<HD>::v_exp(bs) + (o / 4 * G + piece / 4) * 4);
+    }
+  };
+  auto widen = [&](uint32_t w, uint32_t e) {
+    const float s = __uint_as_float(e << 23);
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    return r;
+  };
+  int top_e[G], top_k = 0;                          // largest exponent of each group of channels in the run, and of the keys
+  auto widen_half = [&](uint32_t w, int e, int top) {
+    const float s = __uint_as_float((uint32_t)max(e - top + (127 + kWideShift), 0) << 23);
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
+    return r;
+  };
+  auto put = [&](int step, int n, int buf, auto fast) {
+    unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE, *seen = smem + 4 * TILE + buf * kWideTokens;
+    if (lot_of(n) >= 2 * G) return;
+    if (lot_of(n) < G) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        u32x4 x;
+        if constexpr (decltype(fast)::value && std::is_same_v<T, _Float16>) x = widen_half(lot[n].code[d], (int)lot[n].e, top_k);
+        else x = widen(lot[n].code[d], lot[n].e);
+        *reinterpret_cast<u32x4 *>(kt + lane * RB + (((lot_of(n) * 4 + d) ^ prompt_swizzle<CH>(lane)) << 4)) = x;
+      }
+      if (lot_of(n) == 0) seen[lane] = lot[n].id >= 0;
+    } else {
+      const int t4 = token_of(n), piece = lane % (HD / 8), left = t_end - (t_begin + step * kWideTokens + t4);
+      const bool cut = __ballot(lot[n].id < 0 || left < 4) != 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t w;
+        if constexpr (HD == 128) w = lot[n].code[j];
+        else w = __builtin_amdgcn_perm(lot[n].code[2 + j / 2], lot[n].code[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+        u32x4 x;
+        if constexpr (decltype(fast)::value) {
+          int of = top_e[0];
+#pragma unroll
+          for (int k = 1; k < G; ++k) of = piece / 4 == k ? top_e[k] : of;
+          x = widen_half(w, (int)(lot[n].e >> (8 * j) & 255), of);
+        } else x = widen(w, lot[n].e >> (8 * j));   // of a scale the conversion reads the exponent only
+        if (cut) {
+          asm volatile("" ::: "memory");            // a branch
+          if (lot[n].id < 0 || j >= left) x = u32x4{0, 0, 0, 0};
+        }
+        *reinterpret_cast<u32x4 *>(vt + (t4 + j) * RB + ((piece ^ prompt_swizzle<CH>(t4 + j)) << 4)) = x;
+      }
+    }
+  };
+  // byte offsets of the lane's reads; rows further on are constants away
+  uint32_t k_at[NS], v_at[ND][2];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) k_at[s] = col * RB + (((2 * s + half) ^ prompt_swizzle<CH>(col)) << 4);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = 8 * e + 4 * half + ((lane & 15) >> 2), chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      v_at[d][e] = row * RB + ((chunk ^ prompt_swizzle<CH>(row)) << 4) + (lane & 1) * 8;
+    }
+
+  for (long long at = run0; at < run1;) {
+    while (at >= end && first + 64 < a.prefix.groups) {
+      first += 64;
+      groups(end);
+    }
+    if (at >= end) break;                           // not reached while the lengths stay as they are
+    const int local = 63 - __clzll(__ballot(start <= at)), g = first + local;      // the last of those that begin here has the work
+    const int row0 = __builtin_amdgcn_readlane(mine.rows.begin, local), n_cols = __builtin_amdgcn_readlane(mine.rows.count, local) * a.group;
+    const int tokens = __builtin_amdgcn_readlane(mine.seq, local), units = __builtin_amdgcn_readlane(mine.units, local);
+    const long long in_group = at - lane_value64(start, local);
+    const int segment = __builtin_amdgcn_readfirstlane((int)wave_div(in_group, units));
+    const int u0 = __builtin_amdgcn_readfirstlane((int)(in_group - (long long)segment * units));
+    const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at))), steps = u1 - u0;
+    const bool whole = steps == units;
+    const long long slot = 2 * (long long)blockIdx.x + (at != run0);
+    at += steps;
+    head = segment % c.kv_heads;
+    t_begin = u0 * kWideTokens;
+    t_end = min(tokens, u1 * kWideTokens);
+    table = b.table + (long long)__builtin_amdgcn_readfirstlane(a.prefix.prefix[g]) * b.max_blocks;
+    const int col0 = (segment / c.kv_heads * W + wave) * 32;
+    const int my_col = min(col0 + col, n_cols - 1), my_row = row0 + my_col / a.group, my_head = head * a.group + my_col % a.group;
+
+    typename MatrixOf<T>::x8 qf[NS];
+    {
+      const T *p = q.at(my_row, my_head) + half * 8;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        u32x4 w = *reinterpret_cast<const u32x4 *>(p + s * 16);
+        w ^= a.flip ? 0x80008000u : 0u;             // a negative scale: the queries' signs, so that larger products are larger scores
+        qf[s] = __builtin_bit_cast(typename MatrixOf<T>::x8, w);
+      }
+    }
+    f32x16 acc[ND];
+  #pragma unroll
+    for (int d = 0; d < ND; ++d)
+  #pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+    float m = -INFINITY, l[4] = {};
+
+    // the run's exponents
+    int e_max = 0, e_min = 255;
+    for (int i = threadIdx.x; i < (t_end - t_begin + 3) / 4 * G; i += 64 * W) {         // of channels 32 (lane % G) on
+      const int t = t_begin + i / G * 4, id = table[t >> c.block_shift];
+      if (id < 0 || id >= c.n_blocks) continue;
+      const uint32_t e = *reinterpret_cast<const uint32_t *>(c.at(id, head) + Kv4Offsets<HD>::v_exp(bs) + ((t & (bs - 1)) / 4 * G + i % G) * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int x = t + j < t_end ? (int)(e >> (8 * j) & 255) : 0;
+        e_max = max(e_max, x);
+        if (x > 1) e_min = min(e_min, x);
+      }
+    }
+#pragma unroll
+    for (int o = G; o < 64; o <<= 1) {
+      e_max = max(e_max, __shfl_xor(e_max, o));
+      e_min = min(e_min, __shfl_xor(e_min, o));
+    }
+    if (lane < G) s_e[wave][lane] = make_int2(e_max, e_min);
+    if constexpr (std::is_same_v<T, _Float16>) {
+      e_max = 0, e_min = 255;
+      for (int t = t_begin + threadIdx.x; t < t_end; t += 64 * W) {
+        const int id = table[t >> c.block_shift];
+        if (id < 0 || id >= c.n_blocks) continue;
+        const uint8_t *from = c.at(id, head) + Kv4Offsets<HD>::k_exp(bs) + (t & (bs - 1)) * G;
+        const uint32_t e = G == 4 ? *reinterpret_cast<const uint32_t *>(from) : *reinterpret_cast<const uint16_t *>(from);
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          const int x = (int)(e >> (8 * j) & 255);
+          e_max = max(e_max, x);
+          if (x > 1) e_min = min(e_min, x);
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        e_max = max(e_max, __shfl_xor(e_max, o));
+        e_min = min(e_min, __shfl_xor(e_min, o));
+      }
+      if (lane == 0) s_e[wave][G] = make_int2(e_max, e_min);
+    }
+    __syncthreads();                                // LDS is free, too
+    bool narrow = true;
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      int2 e = s_e[0][k];
+#pragma unroll
+      for (int w = 1; w < W; ++w) e.x = max(e.x, s_e[w][k].x), e.y = min(e.y, s_e[w][k].y);
+      top_e[k] = __builtin_amdgcn_readfirstlane(e.x);
+      narrow = narrow && e.x < (int)kKv4NotFinite && e.x - e.y <= kWideSpread;
+    }
+    if constexpr (std::is_same_v<T, _Float16>) {
+      int2 e = s_e[0][G];
+#pragma unroll
+      for (int w = 1; w < W; ++w) e.x = max(e.x, s_e[w][G].x), e.y = min(e.y, s_e[w][G].y);
+      top_k = __builtin_amdgcn_readfirstlane(e.x);
+      narrow = narrow && e.x < (int)kKv4NotFinite && e.x - e.y <= kWideSpread;
+    }
+    narrow = __builtin_amdgcn_readfirstlane(narrow);
+    auto walk = [&](auto fast) {
+      constexpr bool FAST = decltype(fast)::value;
+      constexpr int PT = FAST ? 1 : 2;
+      constexpr float kLazy = FAST ? MatrixOf<_Float16>::kLazy : kKv4Lazy, kLift = FAST ? MatrixOf<_Float16>::kLift : 0.f;
+      const float scale_log2 = FAST && std::is_same_v<T, _Float16> ? ldexpf(a.scale_log2, top_k - (127 + kWideShift)) : a.scale_log2;
+      typedef std::conditional_t<FAST, _Float16, __bf16> PE;
+      typedef typename MatrixOf<PE>::x8 P8;
+      int next_id[NU];
+    #pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        lot[n].id = ask_block(0, n);
+        next_id[n] = ask_block(1, n);
+        ask_codes(0, n);
+      }
+    #pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        put(0, n, 0, fast);
+        lot[n].id = next_id[n];
+        next_id[n] = ask_block(2, n);
+        ask_codes(1, n);
+      }
+      for (int step = 0; step < steps; ++step) {
+        const int buf = step & 1;
+        __syncthreads();                                // this step's tokens are in LDS, the step's before have been used
+        if (step + 1 < steps) {
+    #pragma unroll
+          for (int n = 0; n < NU; ++n) {
+            put(step + 1, n, buf ^ 1, fast);
+            lot[n].id = next_id[n];
+            next_id[n] = ask_block(step + 3, n);
+            ask_codes(step + 2, n);
+          }
+        }
+        if (col0 >= n_cols) continue;                   // a wave without columns only brings tokens
+        const unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE, *seen = smem + 4 * TILE + buf * kWideTokens;
+        const unsigned long long live = __ballot(seen[lane] != 0);
+        f32x16 s[NT];
+    #pragma unroll
+        for (int t = 0; t < NT; ++t)
+    #pragma unroll
+          for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+    #pragma unroll
+        for (int n = 0; n < NS; ++n)
+    #pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            if constexpr (FAST || std::is_same_v<T, __bf16>)
+              s[t] = MatrixOf<T>::mul(*reinterpret_cast<const typename MatrixOf<T>::x8 *>(kt + k_at[n] + t * 32 * RB), qf[n], s[t]);
+            else {                                  // fp16 queries as a bf16 and a remainder
+              const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + k_at[n] + t * 32 * RB);
+              bf16x8 hi, lo;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                hi[e] = (__bf16)(float)qf[n][e];
+                lo[e] = (__bf16)((float)qf[n][e] - (float)hi[e]);
+              }
+              s[t] = MatrixOf<__bf16>::mul(kf, hi, s[t]);
+              s[t] = MatrixOf<__bf16>::mul(kf, lo, s[t]);
+            }
+          }
+        if (live != ~0ull) {
+        asm volatile("" ::: "memory");              // a branch: selects would cost every step a hundred instructions
+          const unsigned long long my = live >> (4 * half);
+    #pragma unroll
+          for (int t = 0; t < NT; ++t)
+    #pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (!(my >> (32 * t + 8 * (e >> 2) + (e & 3)) & 1)) s[t][e] = -INFINITY;
+        }
+        float top = s[0][0];
+    #pragma unroll
+        for (int t = 0; t < NT; ++t)
+    #pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+        top = max_xor32(top) * scale_log2;
+        if (__ballot(top > m + kLazy)) {
+          const float next = fmaxf(m, top);
+          const float by = next == -INFINITY ? 1.f : exp2_fast(m - next);
+          m = next;
+    #pragma unroll
+          for (int i = 0; i < 4; ++i) l[i] *= by;
+    #pragma unroll
+          for (int d = 0; d < ND; ++d) acc[d] *= by;
+        }
+        const float use = m == -INFINITY ? 0.f : m - kLift;
+        P8 pf[NK][PT];
+    #pragma unroll
+        for (int t = 0; t < NT; ++t)
+    #pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float p = exp2_fast(__builtin_fmaf(s[t][e], scale_log2, -use));
+            l[e & 3] += p;
+            pf[2 * t + (e >> 3)][0][e & 7] = (PE)p;
+            if constexpr (PT == 2) pf[2 * t + (e >> 3)][1][e & 7] = (PE)(p - (float)(PE)p);
+          }
+    #pragma unroll
+        for (int n = 0; n < NK; ++n)
+    #pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][0] + n * 16 * RB));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][1] + n * 16 * RB));
+            struct Both { s16x4 a, b; } both = {lo, hi};
+            const P8 vf = __builtin_bit_cast(P8, both);
+    #pragma unroll
+            for (int e = 0; e < PT; ++e) acc[d] = MatrixOf<PE>::mul(vf, pf[n][e], acc[d]);
+          }
+      }
+      m -= kLift;
+      if constexpr (FAST) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[d][e] = ldexpf(acc[d][e], top_e[d] - (127 + kWideShift));
+      }
+    };
+    if (narrow) walk(std::true_type{});
+    else walk(std::false_type{});
+    const float sum = sum_xor32((l[0] + l[1]) + (l[2] + l[3]));
+    if (col0 + col >= n_cols) continue;
+    const long long to = whole ? ((long long)b.rows + my_row) * a.q_heads + my_head : slot * (32 * W) + wave * 32 + col;
+    float *o = (whole ? a.whole : a.wide_part) + to * HD;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4 *>(o + d * 32 + e * 8 + half * 4) = f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+    if (half == 0) *reinterpret_cast<float2 *>((whole ? a.whole_ml : a.wide_ml) + to * 2) = make_float2(m, sum);
   }
-  return -1;
 }
 
-// Joins what kv4_attend left of a row: its own tokens' part and its group's prefix', each whole or in parts of several workgroups.  A workgroup takes some
-// columns (rows times query heads) of a request, 16 bytes of a column per thread.
+// ---- joining ---------------------------------------------------------------------------------------------------------------
+
+// Joins what kv4_attend left of a row: its own tokens' part and its group's prefix', each whole or in parts of several workgroups (wide: only rows whose own
+// tokens are in parts).  A workgroup takes some columns (rows times query heads) of a request, 16 bytes of a column per thread.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4SharedAttend a, int grid) {
   const int req = blockIdx.y, lane = threadIdx.x & 63;
-  const Kv4Request own = kv4_request(c, b, a, req);
-  const int n_cols = own.rows.count * a.q_heads;
+  Kv4Parts own{kv4_request(c, b, a, req), 0, 0, a.cols, a.part, a.part_ml}, shared = own;
+  const int n_cols = own.r.rows.count * a.q_heads;
   constexpr int PER = 256 / (HD / 4);
   if ((long long)blockIdx.x * PER >= n_cols) return;
-  const int g = group_of(a.prefix, req), seq = b.seq_len[req];
-  const bool live = seq >= 0 && seq <= a.max_seq && (long long)seq <= (long long)b.max_blocks * c.block_size;
-  long long before[2] = {0, 0}, all = 0;
-  for (int i = lane; i < b.batch + a.prefix.groups; i += 64) {
+  const int g = group_of(a.prefix, req);
+  long long all = 0;
+  shared.r.work = 0;
+  for (int i = lane; i < kv4_requests(b, a); i += 64) {
     const long long work = kv4_request(c, b, a, i).work;
     all += work;
-    if (i < req) before[0] += work;
-    if (i < b.batch + g) before[1] += work;
+    if (i < req) own.before += work;
+    if (i < b.batch + g) shared.before += work;
   }
-  before[0] = wave_sum64(before[0]);
-  before[1] = wave_sum64(before[1]);
-  const long long per = kv4_run(wave_sum64(all), grid);
-  Kv4Request shared{};
-  if (g >= 0) shared = kv4_request(c, b, a, b.batch + g);
-  for (int u = blockIdx.x * PER + threadIdx.x / (HD / 4); u < n_cols; u += gridDim.x * PER) {
-    const int d = threadIdx.x % (HD / 4) * 4, i = u / a.q_heads, h = u - i * a.q_heads, head = h / a.group;
-    const long long r = own.rows.begin + i;
-    Kv4Sums s;
-#pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      const Kv4Request &q = part ? shared : own;
-      if (!live || !q.work || r < q.rows.begin || r >= q.rows.begin + q.rows.count) continue;
-      const int col = (int)(r - q.rows.begin) * a.group + h - head * a.group, tile = col / a.cols, n = col - tile * a.cols;
-      const long long s0 = before[part] + ((long long)tile * c.kv_heads + head) * q.units;
-      const int w0 = (int)wave_div(s0, per), w1 = (int)wave_div(s0 + q.units - 1, per);
-      if (w0 == w1) {
-        const long long at = ((long long)part * b.rows + r) * a.q_heads + h;
-        const float2 ml[1] = {*reinterpret_cast<const float2 *>(a.whole_ml + at * 2)};
-        const f32x4 x[1] = {*reinterpret_cast<const f32x4 *>(a.whole + at * HD + d)};
-        s.add(ml, x);
-        continue;
-      }
-      const int first_slot = 2 * w0 + (w0 * per != s0);
-      constexpr int K = 8;
-      for (int w = w0; w <= w1; w += K) {
-        float2 ml[K];
-        f32x4 x[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const int wi = min(w + k, w1);
-          const long long at = (long long)(wi == w0 ? first_slot : 2 * wi) * a.cols + n;
-          ml[k] = *reinterpret_cast<const float2 *>(a.part_ml + at * 2);
-          x[k] = *reinterpret_cast<const f32x4 *>(a.part + at * HD + d);
-          if (w + k > w1) ml[k] = make_float2(-INFINITY, 0.f);
-        }
-        s.add(ml, x);
-      }
+  own.before = wave_sum64(own.before);
+  own.per = shared.per = kv4_run(wave_sum64(all), grid);
+  if (kv4_live(c, b, a, req) && g >= 0) {
+    if (a.wide) shared = wide_parts(c, b, a, g);
+    else {
+      shared.r = kv4_request(c, b, a, b.batch + g);
+      shared.before = wave_sum64(shared.before);
     }
+  }
+  for (int u = blockIdx.x * PER + threadIdx.x / (HD / 4); u < n_cols; u += gridDim.x * PER) {
+    const int d = threadIdx.x % (HD / 4) * 4, i = u / a.q_heads, h = u - i * a.q_heads, head = h / a.group, in_head = h - head * a.group;
+    const long long r = own.r.rows.begin + i, at = r * a.q_heads + h, at_prefix = ((long long)b.rows + r) * a.q_heads + h;
+    const Kv4Parts::Place mine = own.place(c.kv_heads, head, i * a.group + in_head);
+    if (a.wide && mine.w0 == mine.w1) continue;     // done
+    Kv4Sums s;
+    own.add<HD>(s, mine, d, a.whole + at * HD, a.whole_ml + at * 2);
+    const long long in_group = r - shared.r.rows.begin;
+    if (shared.r.work && in_group >= 0 && in_group < shared.r.rows.count)
+      shared.add<HD>(s, shared.place(c.kv_heads, head, (int)in_group * a.group + in_head), d, a.whole + at_prefix * HD, a.whole_ml + at_prefix * 2);
     const float inv = s.sum == 0.f ? 0.f : 1.f / s.sum;
     float f[4] = {s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv};
     store_vec<T, 4>(out.at(r, h) + d, f);
-    if (a.lse && d == 0) a.lse[r * a.q_heads + h] = s.sum == 0.f ? -INFINITY : (s.top + log2f(s.sum)) * 0.6931471805599453f;
+    if (a.lse && d == 0) a.lse[at] = s.sum == 0.f ? -INFINITY : (s.top + log2f(s.sum)) * 0.6931471805599453f;
   }
 }
 
