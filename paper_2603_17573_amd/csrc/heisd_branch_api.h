@@ -155,14 +155,14 @@ struct SharedPlan {
   int col_tiles, unit, wide_waves, own_tiles;
   int64_t groups, wide;
   bool joins;
-  size_t part_ml, whole, whole_ml, wide_part, wide_ml, total;
+  size_t part_ml, whole, whole_ml, wide_part, wide_ml, book, group_of, total;
   SharedPlan(int64_t batch, int64_t rows, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, const PrefixGroups &p, int64_t head_dim) {
     const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::min<int64_t>(std::min<int64_t>(p.max_rows, rows) * group, 1 << 22);
     wide_waves = cols >= kWideMany ? 8 : 4;
     const int64_t wide_cols = 32 * wide_waves;
     wide = p.groups && cols >= kWideLeast
                ? std::min<int64_t>(p.groups * kv_heads * ((cols + wide_cols - 1) / wide_cols) * ((p.max_prefix + 255) / 256), 8 / wide_waves * kKv4Units) : 0;
-    col_tiles = (wide ? own_cols : std::max(own_cols, cols)) > 16 ? 2 : 1;
+    col_tiles = !wide && std::max(own_cols, cols) > 16 ? 2 : 1;
     const int64_t tile = 16 * col_tiles, most = kv4_per_unit((int)head_dim, col_tiles) * kKv4Units;
     const int64_t segments = batch * std::min<int64_t>(kv_heads * ((own_cols + tile - 1) / tile), 65535);
     unit = wide && max_seq <= kWholeTokens ? kWholeTokens : kKv4Unit;
@@ -177,7 +177,9 @@ struct SharedPlan {
     whole_ml = whole + align256((size_t)2 * rows * group * kv_heads * head_dim * sizeof(float));
     wide_part = whole_ml + align256((size_t)2 * rows * group * kv_heads * 2 * sizeof(float));
     wide_ml = wide_part + align256((size_t)2 * wide * wide_cols * head_dim * sizeof(float));
-    total = wide_ml + align256((size_t)2 * wide * wide_cols * 2 * sizeof(float));
+    book = wide_ml + align256((size_t)2 * wide * wide_cols * 2 * sizeof(float));
+    group_of = book + align256(wide ? p.groups * sizeof(WideBook) : 0);
+    total = group_of + align256(wide ? batch * sizeof(int32_t) : 0);
   }
 };
 
@@ -214,7 +216,7 @@ static hipError_t kv4_shared_launch(const Kv4Cache &c, const PagedBatch &b, cons
                               const SharedPlan &plan, int max_q, hipStream_t st) {
   const HeadRows<T> qi = head_rows<T>(*q), o = head_rows<T>(*out);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
-  const dim3 block(256), grid((unsigned)plan.groups);
+  const dim3 block(256), grid = plan.own_tiles ? dim3(c.kv_heads, plan.own_tiles, b.batch) : dim3((unsigned)plan.groups);
   if (plan.wide) {
     const hipError_t e = plan.wide_waves == 8 ? kv4_prefix_launch<T, HD, 8>(c, b, qc, a, st) : kv4_prefix_launch<T, HD, 4>(c, b, qc, a, st);
     if (e != hipSuccess) return e;
@@ -256,12 +258,16 @@ extern "C" int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const hei
                                           scale < 0, q->heads / c.kv_heads, q->heads, max_seq, 16 * plan.col_tiles,
                                           reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + plan.part_ml), lse};
   a.prefix = p;
-  a.unit = plan.unit;
+  a.unit_shift = __builtin_ctz(plan.unit);
+  a.cols_shift = __builtin_ctz(a.cols);
+  a.group_shift = (a.group & (a.group - 1)) ? -1 : __builtin_ctz(a.group);
   a.wide = (int)plan.wide;
-  a.wide_cols = 32 * plan.wide_waves;
+  a.wide_shift = __builtin_ctz(32 * plan.wide_waves);
   a.own_tiles = plan.own_tiles;
   a.wide_part = reinterpret_cast<float *>(ws + plan.wide_part);
   a.wide_ml = reinterpret_cast<float *>(ws + plan.wide_ml);
+  a.book = reinterpret_cast<WideBook *>(ws + plan.book);
+  a.group_at = reinterpret_cast<int32_t *>(ws + plan.group_of);
   a.whole = reinterpret_cast<float *>(ws + plan.whole);
   a.whole_ml = reinterpret_cast<float *>(ws + plan.whole_ml);
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -299,25 +299,39 @@ __device__ __forceinline__ float kv4_weight(float m, float top) { return m == -I
 // ---- parts of a row --------------------------------------------------------------------------------------------------
 
 // Sums, maximum and sum of probabilities of a column, in the order of its tokens.
+template <int V>
 struct Kv4Sums {
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  f32x4 o[V] = {};
   float top = -INFINITY, sum = 0.f;
   template <int K>
-  __device__ __forceinline__ void add(const float2 (&ml)[K], const f32x4 (&x)[K]) {
+  __device__ __forceinline__ void add(const float2 (&ml)[K], const f32x4 (&x)[K][V]) {
     float next = top;
 #pragma unroll
     for (int i = 0; i < K; ++i) next = fmaxf(next, ml[i].x);
     const float keep = kv4_weight(top, next);
     sum *= keep;
-    o *= keep;
+#pragma unroll
+    for (int v = 0; v < V; ++v) o[v] *= keep;
     top = next;
 #pragma unroll
     for (int i = 0; i < K; ++i)
       if (kv4_saw(ml[i].x, ml[i].y)) {
         const float by = kv4_weight(ml[i].x, top);
         sum += ml[i].y * by;
-        o += x[i] * by;
+#pragma unroll
+        for (int v = 0; v < V; ++v) o[v] += x[i][v] * by;
       }
+  }
+  // The row's values from p on, and its log-sum.
+  template <typename T>
+  __device__ __forceinline__ void store(T *p, float *lse) const {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    float f[4 * V];
+#pragma unroll
+    for (int i = 0; i < 4 * V; ++i) f[i] = o[i / 4][i % 4] * inv;
+#pragma unroll
+    for (int v = 0; v < V; ++v) store_vec<T, 4>(p + 4 * v, f + 4 * v);
+    if (lse) *lse = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
   }
 };
 
@@ -326,15 +340,24 @@ struct Kv4Sums {
 // `wide` workgroups, and whoever ends a row's own tokens joins them.  What a segment of a prefix (narrow: any segment) gives is kept: whole ones by row,
 // [own, prefix][rows][q_heads], the others by workgroup.
 constexpr int kWideTokens = 64;                     // of a unit of kv4_prefix's work
+// Where kv4_prefix's work for a group lies: its rows, units of one of its segments, work before it, work per workgroup.
+struct WideBook {
+  int begin, count, units, pad;
+  long long before, per;
+};
 struct Kv4SharedAttend : Kv4Attend {
   PrefixGroups prefix;
-  int unit;                                         // tokens of a unit of own work
-  int wide, wide_cols;                              // workgroups of kv4_prefix, columns that one takes at a time
-  int own_tiles;                                    // not 0: every workgroup has one segment of own tokens, request by request, own_tiles for each key head (and more, one after the other, where max_q does not hold)
+  int unit_shift, cols_shift, group_shift;          // powers of two: tokens of a unit of own work, columns; the group, where it is one (else -1)
+  int wide, wide_shift;                             // workgroups of kv4_prefix, columns that one takes at a time (a power of two)
+  int own_tiles;                                    // not 0: the grid is key heads, so many tiles of columns (where max_q does not hold, more of them one after the other), requests
   float *whole, *whole_ml, *wide_part, *wide_ml;
+  WideBook *book;                                   // [groups], written by kv4_prefix
+  int32_t *group_at;                                // [batch], so is this: a request's group (-1: none with a prefix)
 };
 __device__ __forceinline__ constexpr int kv4_unit(const Kv4Attend &) { return kKv4Unit; }
-__device__ __forceinline__ int kv4_unit(const Kv4SharedAttend &a) { return a.unit; }
+__device__ __forceinline__ int kv4_unit(const Kv4SharedAttend &a) { return 1 << a.unit_shift; }
+__device__ __forceinline__ int kv4_row(const Kv4Attend &a, int column) { return column / a.group; }
+__device__ __forceinline__ int kv4_row(const Kv4SharedAttend &a, int column) { return a.group_shift >= 0 ? column >> a.group_shift : column / a.group; }
 __device__ __forceinline__ constexpr int kv4_own_tiles(const Kv4Attend &) { return 0; }
 __device__ __forceinline__ int kv4_own_tiles(const Kv4SharedAttend &a) { return a.own_tiles; }
 __device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4Attend &) { return b.batch; }
@@ -347,15 +370,15 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const Paged
     const PrefixSpan s = prefix_span(c, b, a.prefix, i - b.batch);
     r.rows = s.rows, r.seq = s.tokens;
   }
-  r.units = max((r.seq + a.unit - 1) / a.unit, 1);
-  r.work = (long long)r.units * ((r.rows.count * a.group + a.cols - 1) / a.cols * c.kv_heads);
+  r.units = max((r.seq + (1 << a.unit_shift) - 1) >> a.unit_shift, 1);
+  r.work = (long long)r.units * (((r.rows.count * a.group + a.cols - 1) >> a.cols_shift) * c.kv_heads);
   return r;
 }
 // A group's work for kv4_prefix.
 __device__ __forceinline__ Kv4Request wide_request(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int g) {
   const PrefixSpan s = prefix_span(c, b, a.prefix, g);
   Kv4Request r{s.rows, s.tokens, (s.tokens + kWideTokens - 1) / kWideTokens, 0};
-  r.work = (long long)r.units * ((r.rows.count * a.group + a.wide_cols - 1) / a.wide_cols * c.kv_heads);
+  r.work = (long long)r.units * (((r.rows.count * a.group + (1 << a.wide_shift) - 1) >> a.wide_shift) * c.kv_heads);
   return r;
 }
 
@@ -374,7 +397,7 @@ __device__ __forceinline__ int group_of(const PrefixGroups &p, int i) {
 struct Kv4Parts {
   Kv4Request r;
   long long before, per;                            // work before it, work of a workgroup
-  int cols;
+  int cols_shift;
   const float *part, *part_ml;
   // Where a column's parts are: the workgroups from w0 to w1 have them, w0 in first_slot, the others (which begin their runs inside the segment) in
   // the first of their two slots; n: the column's place in a slot.  w0 = w1: one workgroup has all, which is kept by row.  w1 < w0: none.
@@ -382,47 +405,46 @@ struct Kv4Parts {
     int w0, w1, first_slot, n;
   };
   __device__ __forceinline__ Place place(int kv_heads, int head, int col) const {
-    const long long s0 = before + ((long long)(col / cols) * kv_heads + head) * r.units;
+    const long long s0 = before + ((long long)(col >> cols_shift) * kv_heads + head) * r.units;
     const int w0 = (int)wave_div(s0, per);
-    return Place{w0, (int)wave_div(s0 + r.units - 1, per), 2 * w0 + (w0 * per != s0), col % cols};
+    return Place{w0, (int)wave_div(s0 + r.units - 1, per), 2 * w0 + (w0 * per != s0), col & ((1 << cols_shift) - 1)};
   }
-  // Adds what it has of 4 channels from d on.  whole: where the column's are if one workgroup has all.
-  template <int HD>
-  __device__ __forceinline__ void add(Kv4Sums &s, const Place &p, int d, const float *whole, const float *whole_ml) const {
+  // Adds what it has of 4 * V channels from d on.  whole: where the column's are if one workgroup has all.
+  template <int HD, int V>
+  __device__ __forceinline__ void add(Kv4Sums<V> &s, const Place &p, int d, const float *whole, const float *whole_ml) const {
     if (p.w0 == p.w1) {
       const float2 ml[1] = {*reinterpret_cast<const float2 *>(whole_ml)};
-      const f32x4 x[1] = {*reinterpret_cast<const f32x4 *>(whole + d)};
+      f32x4 x[1][V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[0][v] = *reinterpret_cast<const f32x4 *>(whole + d + 4 * v);
       s.add(ml, x);
       return;
     }
     constexpr int K = 4;                                                           // parts requested at once
     for (int i = p.w0; i <= p.w1; i += K) {
       float2 ml[K];
-      f32x4 x[K];
+      f32x4 x[K][V];
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int wi = min(i + k, p.w1);
-        const long long at = (long long)(wi == p.w0 ? p.first_slot : 2 * wi) * cols + p.n;
+        const long long at = ((long long)(wi == p.w0 ? p.first_slot : 2 * wi) << cols_shift) + p.n;
         ml[k] = *reinterpret_cast<const float2 *>(part_ml + at * 2);
-        x[k] = *reinterpret_cast<const f32x4 *>(part + at * HD + d);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[k][v] = *reinterpret_cast<const f32x4 *>(part + at * HD + d + 4 * v);
         if (i + k > p.w1) ml[k] = make_float2(-INFINITY, 0.f);
       }
       s.add(ml, x);
     }
   }
 };
-// The parts of a group's prefix that kv4_prefix left.  A wave's.
-__device__ __forceinline__ Kv4Parts wide_parts(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int g) {
-  const int lane = threadIdx.x & 63;
-  Kv4Parts p{wide_request(c, b, a, g), 0, 0, a.wide_cols, a.wide_part, a.wide_ml};
-  long long all = 0;
-  for (int i = lane; i < a.prefix.groups; i += 64) {
-    const long long work = wide_request(c, b, a, i).work;
-    all += work;
-    if (i < g) p.before += work;
-  }
-  p.before = wave_sum64(p.before);
-  p.per = kv4_run(wave_sum64(all), a.wide);
+// The parts of the prefix of request i's group that kv4_prefix left (r.work 0: none).
+__device__ __forceinline__ Kv4Parts wide_parts(const Kv4SharedAttend &a, int i) {
+  Kv4Parts p{{{0, 0}, 0, 0, 0}, 0, 1, a.wide_shift, a.wide_part, a.wide_ml};
+  const int g = a.group_at[i];
+  if (g < 0) return p;
+  const WideBook k = a.book[g];
+  p.r = Kv4Request{{k.begin, k.count}, 0, k.units, 1};
+  p.before = k.before, p.per = k.per;
   return p;
 }
 // Is the request there (or has it been left out)?
@@ -450,7 +472,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
   __shared__ float s_m[4][16], s_l[4][16];
   __shared__ long long s_start[4][64];                          // a wave's own: on its way to a later request another may be behind
   __shared__ int4 s_req[4][64];
-  __shared__ Kv4Parts::Place s_place[SHARED ? 16 : 1];          // wide: where the parts of the prefix are, a column each
+  __shared__ Kv4Parts::Place s_place[SHARED ? 16 * CT : 1];     // wide: where the parts of the prefix are, a column each
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int bs = c.block_size;
 
@@ -489,7 +511,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     int local = 0, req;
     int4 rq;
     if (SHARED && direct) {
-      req = blockIdx.x / (c.kv_heads * max(kv4_own_tiles(a), 1));
+      req = blockIdx.z;
       const Kv4Request r = kv4_request(c, b, a, req);
       rq = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
     } else {
@@ -499,11 +521,12 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     }
     const Span rows{__builtin_amdgcn_readfirstlane(rq.x), __builtin_amdgcn_readfirstlane(rq.y)};
     const int seq = __builtin_amdgcn_readfirstlane(rq.z), units = __builtin_amdgcn_readfirstlane(rq.w);
-    const long long in_req = direct ? blockIdx.x + (at - req) * c.kv_heads * kv4_own_tiles(a) : at - lane_value64(s_start[wave][lane], local);
-    const int segment = __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
-    const int u0 = __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
-    const int u1 = __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
-    const int head = segment % c.kv_heads, col0 = segment / c.kv_heads * (16 * CT);
+    const long long in_req = direct ? 0 : at - lane_value64(s_start[wave][lane], local);
+    const int segment = direct ? 0 : __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
+    const int u0 = direct ? 0 : __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
+    const int u1 = direct ? 1 : __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
+    const int tile = __builtin_amdgcn_readfirstlane(direct ? (int)blockIdx.y + (int)at * kv4_own_tiles(a) : segment / c.kv_heads);
+    const int head = __builtin_amdgcn_readfirstlane(direct ? (int)blockIdx.x : segment - tile * c.kv_heads), col0 = tile * (16 * CT);
     const bool whole = u0 == 0 && u1 == units;
     const long long slot = 2 * (long long)blockIdx.x + (at != run0);
     const int n_cols = rows.count * a.group;
@@ -514,12 +537,22 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       if (req >= b.batch) owner = __builtin_amdgcn_readfirstlane(a.prefix.prefix[req - b.batch]), few = seq;
     const int32_t *table = b.table + (long long)owner * b.max_blocks;
 
+    [[maybe_unused]] Kv4Parts prefix{};                         // wide: of this request's prefix
+    if constexpr (SHARED)
+      if (a.wide && whole && kv4_live(c, b, a, req)) prefix = wide_parts(a, req);
+    if constexpr (SHARED)
+      if (a.wide && whole && threadIdx.x < 16 * CT) {
+        const int cn = min(col0 + (int)threadIdx.x, n_cols - 1), i = kv4_row(a, cn);
+        const long long in_group = (long long)rows.begin + i - prefix.r.rows.begin;
+        s_place[threadIdx.x] = prefix.r.work > 0 && in_group >= 0 && in_group < prefix.r.rows.count
+                                   ? prefix.place(c.kv_heads, head, (int)in_group * a.group + cn - i * a.group) : Kv4Parts::Place{0, -1, 0, 0};
+      }
     // the columns' queries and how many tokens each may see
     typename VecOf<T, 8>::type qr[CT][KJ];
     int seen[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      const int n = min(col0 + ct * 16 + col, n_cols - 1), i = n / a.group;       // columns past the end: the last again, not stored
+      const int n = min(col0 + ct * 16 + col, n_cols - 1), i = kv4_row(a, n);       // columns past the end: the last again, not stored
       seen[ct] = min(few + i, seq);
       const T *p = q.at(rows.begin + i, head * a.group + (n - i * a.group)) + quad * (HD / 4);
 #pragma unroll
@@ -535,6 +568,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[ct][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    bool busy = false;                                          // this wave has had tokens
     int t0 = 0, my_id = -1;                                     // tokens t0 .. t0 + 4095 are at hand
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)s_mine[wave];
     // Requests pair i: codes 16 bytes a lane, all exponents in one transfer of 4 bytes a lane.
@@ -714,6 +748,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       my_id = t < t1 ? table[t >> c.block_shift] : -1;
       if (my_id >= c.n_blocks) my_id = -1;
       const int n_pairs = max((min(t1 - t0, 32 * kKv4Unit) + 127 - 32 * wave) >> 7, 0);
+      busy = busy || n_pairs;
       wait_vmcnt_all();                                         // the compiler's own loads: none may be waited for among the transfers
       for (int i = 0; i < min(n_pairs, kKv4Ring); ++i) fetch(i);
       for (int i = 0; i < n_pairs; ++i) {
@@ -738,12 +773,6 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
         for (int ct = 0; ct < CT; ++ct) nan_out |= (uint32_t)(e >= kKv4NotFinite && t < seen[ct]) << ct;
       }
     }
-    [[maybe_unused]] Kv4Parts prefix{};                         // wide: of this request's prefix
-    if constexpr (SHARED)
-      if (a.wide && whole && kv4_live(c, b, a, req)) {
-        const int g = group_of(a.prefix, req);
-        if (g >= 0) prefix = wide_parts(c, b, a, g);
-      }
     // join the waves, a tile of columns at a time
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -752,58 +781,52 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
         s_m[wave][col] = m[ct];
         s_l[wave][col] = l[ct];
       }
+      if (SHARED && !busy) {                                    // a wave that had no tokens has nothing to add
+        __syncthreads();
+      } else {
       float *to = reinterpret_cast<float *>(s_mine[wave]) + col * LD;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int d = 0; d < ND; ++d) to[(4 * quad + e) * ND + d] = nan_out >> ct & 1 ? __uint_as_float(0x7FC00000u) : acc[ct][d][e];
-      if constexpr (SHARED)
-        if (a.wide && whole && threadIdx.x < 16) {
-          const int cn = min(col0 + ct * 16 + col, n_cols - 1), i = cn / a.group;
-          const long long in_group = (long long)rows.begin + i - prefix.r.rows.begin;
-          s_place[col] = prefix.r.work > 0 && in_group >= 0 && in_group < prefix.r.rows.count
-                             ? prefix.place(c.kv_heads, head, (int)in_group * a.group + cn - i * a.group) : Kv4Parts::Place{0, -1, 0, 0};
-        }
       __syncthreads();
-      for (int u = threadIdx.x; u < 16 * (HD / 4); u += 256) {
-        const int n = u / (HD / 4), d = u % (HD / 4) * 4, cn = col0 + ct * 16 + n;
+      }
+      constexpr int V = SHARED && HD == 128 ? 2 : 1, PER = HD / (4 * V);      // 16 bytes that a thread has of a column, threads per column
+      for (int u = threadIdx.x; u < 16 * PER; u += 256) {
+        const int n = u / PER, d = u % PER * (4 * V), cn = col0 + ct * 16 + n;
         if (cn >= n_cols) continue;
         const float top = fmaxf(fmaxf(s_m[0][n], s_m[1][n]), fmaxf(s_m[2][n], s_m[3][n]));
-        float sum = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        Kv4Sums<V> s;
+        s.top = top;
 #pragma unroll
         for (int w = 0; w < 4; ++w)
           if (kv4_saw(s_m[w][n], s_l[w][n])) {
             const float by = kv4_weight(s_m[w][n], top);
-            sum += s_l[w][n] * by;
-            o += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_mine[w]) + n * LD + d) * by;
+            s.sum += s_l[w][n] * by;
+#pragma unroll
+            for (int v = 0; v < V; ++v) s.o[v] += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_mine[w]) + n * LD + d + 4 * v) * by;
           }
-        const int i = cn / a.group, h = head * a.group + (cn - i * a.group);
+        const int i = kv4_row(a, cn), h = head * a.group + (cn - i * a.group);
         const long long r = rows.begin + i;
-        if (SHARED && whole) {
-          if constexpr (SHARED) {
-            const long long at_row = ((long long)(a.wide || req >= b.batch) * b.rows + r) * a.q_heads + h;      // own tokens first, then prefixes
-            if (!a.wide) {
-              *reinterpret_cast<f32x4 *>(a.whole + at_row * HD + d) = o;
-              if (d == 0) *reinterpret_cast<float2 *>(a.whole_ml + at_row * 2) = make_float2(top, sum);
-            } else {
-              Kv4Sums s{o, top, sum};
-              prefix.add<HD>(s, s_place[n], d, a.whole + at_row * HD, a.whole_ml + at_row * 2);
-              const float inv = s.sum == 0.f ? 0.f : 1.f / s.sum;
-              float f[4] = {s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv};
-              store_vec<T, 4>(out.at(r, h) + d, f);
-              if (a.lse && d == 0) a.lse[r * a.q_heads + h] = s.sum == 0.f ? -INFINITY : (s.top + log2f(s.sum)) * 0.6931471805599453f;
-            }
+        float *lse = a.lse && d == 0 ? a.lse + r * a.q_heads + h : nullptr;
+        if constexpr (SHARED) {
+          const long long at_row = ((long long)(a.wide || req >= b.batch) * b.rows + r) * a.q_heads + h;      // own tokens first, then prefixes
+          if (whole && a.wide) {
+            prefix.add<HD, V>(s, s_place[ct * 16 + n], d, a.whole + at_row * HD, a.whole_ml + at_row * 2);
+            s.store(out.at(r, h) + d, lse);
+            continue;
           }
+          const long long at_col = slot * a.cols + ct * 16 + n;
+          float *to = (whole ? a.whole + at_row * HD : a.part + at_col * HD) + d;
+#pragma unroll
+          for (int v = 0; v < V; ++v) *reinterpret_cast<f32x4 *>(to + 4 * v) = s.o[v];
+          if (d == 0) *reinterpret_cast<float2 *>(whole ? a.whole_ml + at_row * 2 : a.part_ml + at_col * 2) = make_float2(s.top, s.sum);
         } else if (whole) {
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-          store_vec<T, 4>(out.at(r, h) + d, f);
-          if (a.lse && d == 0) a.lse[r * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+          s.store(out.at(r, h) + d, lse);
         } else {
           const long long at_col = slot * a.cols + ct * 16 + n;
-          *reinterpret_cast<f32x4 *>(a.part + at_col * HD + d) = o;
-          if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + at_col * 2) = make_float2(top, sum);
+          *reinterpret_cast<f32x4 *>(a.part + at_col * HD + d) = s.o[0];
+          if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + at_col * 2) = make_float2(s.top, s.sum);
         }
       }
       __syncthreads();
@@ -835,28 +858,23 @@ __global__ __launch_bounds__(256) void kv4_join(Kv4Cache c, PagedBatch b, HeadRo
     const int head = seg % c.kv_heads, col0 = seg / c.kv_heads * a.cols, n_cols = min(r.rows.count * a.group - col0, a.cols);
     for (int u = threadIdx.x; u < n_cols * (HD / 4); u += 256) {
       const int n = u / (HD / 4), d = u % (HD / 4) * 4;
-      Kv4Sums s;
+      Kv4Sums<1> s;
       constexpr int K = 8;                                                         // parts requested at once
       for (int w = w0; w <= w1; w += K) {
         float2 ml[K];
-        f32x4 x[K];
+        f32x4 x[K][1];
 #pragma unroll
         for (int i = 0; i < K; ++i) {
           const int wi = min(w + i, w1);
           const long long at = (long long)(wi == w0 ? first_slot : 2 * wi) * a.cols + n;
           ml[i] = *reinterpret_cast<const float2 *>(a.part_ml + at * 2);
-          x[i] = *reinterpret_cast<const f32x4 *>(a.part + at * HD + d);
+          x[i][0] = *reinterpret_cast<const f32x4 *>(a.part + at * HD + d);
           if (w + i > w1) ml[i] = make_float2(-INFINITY, 0.f);
         }
         s.add(ml, x);
       }
-      const float top = s.top, sum = s.sum;
-      const f32x4 o = s.o;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
       const int i = (col0 + n) / a.group, h = head * a.group + (col0 + n - i * a.group);
-      float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-      store_vec<T, 4>(out.at(r.rows.begin + i, h) + d, f);
-      if (a.lse && d == 0) a.lse[(long long)(r.rows.begin + i) * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      s.store(out.at(r.rows.begin + i, h) + d, a.lse && d == 0 ? a.lse + (long long)(r.rows.begin + i) * a.q_heads + h : nullptr);
     }
   }
 }

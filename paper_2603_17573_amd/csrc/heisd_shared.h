@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
   long long start, end;
   auto groups = [&](long long before) {
     mine = wide_request(c, b, a, min(first + lane, a.prefix.groups - 1));
-    if (first + lane >= a.prefix.groups) mine.work = 0;
+    if (first + lane >= a.prefix.groups) mine.work = 0, mine.units = 0;
     start = mine.work;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -50,6 +50,25 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
   long long all = end;
   for (int i = 64; i < a.prefix.groups; i += 64) all += wave_sum64(i + lane < a.prefix.groups ? wide_request(c, b, a, i + lane).work : 0);
   const long long per = kv4_run(all, gridDim.x), run0 = blockIdx.x * per, run1 = min(run0 + per, all);
+  if (blockIdx.x == gridDim.x - 1) {                // the books for whoever joins the parts
+    for (int i = threadIdx.x; i < b.batch; i += 64 * W) a.group_at[i] = -1;
+    __syncthreads();
+    long long before = 0;
+    for (int g0 = 0; g0 < a.prefix.groups; g0 += 64) {
+      if (g0) groups(before);
+      before = end;
+      const int n = min(64, a.prefix.groups - g0);
+      if (wave == 0 && lane < n) a.book[g0 + lane] = WideBook{mine.rows.begin, mine.rows.count, mine.units, 0, start, per};
+      for (int i = wave; i < n; i += W) {
+        if (__builtin_amdgcn_readlane(mine.units, i) == 0) continue;
+        const int r0 = a.prefix.first[g0 + i], r1 = a.prefix.first[g0 + i + 1];
+        for (int r = r0 + lane; r < r1; r += 64) a.group_at[r] = g0 + i;
+      }
+      first = g0 + 64;
+    }
+    if (a.prefix.groups > 64) first = 0, groups(0);
+    else first = 0;
+  }
   int head = 0, t_begin = 0, t_end = 0;
   const int32_t *table = b.table;
 
@@ -256,13 +275,13 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
       typedef std::conditional_t<FAST, _Float16, __bf16> PE;
       typedef typename MatrixOf<PE>::x8 P8;
       int next_id[NU];
-    #pragma unroll
+#pragma unroll
       for (int n = 0; n < NU; ++n) {
         lot[n].id = ask_block(0, n);
         next_id[n] = ask_block(1, n);
         ask_codes(0, n);
       }
-    #pragma unroll
+#pragma unroll
       for (int n = 0; n < NU; ++n) {
         put(0, n, 0, fast);
         lot[n].id = next_id[n];
@@ -273,7 +292,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
         const int buf = step & 1;
         __syncthreads();                                // this step's tokens are in LDS, the step's before have been used
         if (step + 1 < steps) {
-    #pragma unroll
+#pragma unroll
           for (int n = 0; n < NU; ++n) {
             put(step + 1, n, buf ^ 1, fast);
             lot[n].id = next_id[n];
@@ -285,13 +304,13 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
         const unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE, *seen = smem + 4 * TILE + buf * kWideTokens;
         const unsigned long long live = __ballot(seen[lane] != 0);
         f32x16 s[NT];
-    #pragma unroll
+#pragma unroll
         for (int t = 0; t < NT; ++t)
-    #pragma unroll
+#pragma unroll
           for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-    #pragma unroll
+#pragma unroll
         for (int n = 0; n < NS; ++n)
-    #pragma unroll
+#pragma unroll
           for (int t = 0; t < NT; ++t) {
             if constexpr (FAST || std::is_same_v<T, __bf16>)
               s[t] = MatrixOf<T>::mul(*reinterpret_cast<const typename MatrixOf<T>::x8 *>(kt + k_at[n] + t * 32 * RB), qf[n], s[t]);
@@ -310,48 +329,48 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
         if (live != ~0ull) {
         asm volatile("" ::: "memory");              // a branch: selects would cost every step a hundred instructions
           const unsigned long long my = live >> (4 * half);
-    #pragma unroll
+#pragma unroll
           for (int t = 0; t < NT; ++t)
-    #pragma unroll
+#pragma unroll
             for (int e = 0; e < 16; ++e)
               if (!(my >> (32 * t + 8 * (e >> 2) + (e & 3)) & 1)) s[t][e] = -INFINITY;
         }
         float top = s[0][0];
-    #pragma unroll
+#pragma unroll
         for (int t = 0; t < NT; ++t)
-    #pragma unroll
+#pragma unroll
           for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
         top = max_xor32(top) * scale_log2;
         if (__ballot(top > m + kLazy)) {
           const float next = fmaxf(m, top);
           const float by = next == -INFINITY ? 1.f : exp2_fast(m - next);
           m = next;
-    #pragma unroll
+#pragma unroll
           for (int i = 0; i < 4; ++i) l[i] *= by;
-    #pragma unroll
+#pragma unroll
           for (int d = 0; d < ND; ++d) acc[d] *= by;
         }
         const float use = m == -INFINITY ? 0.f : m - kLift;
         P8 pf[NK][PT];
-    #pragma unroll
+#pragma unroll
         for (int t = 0; t < NT; ++t)
-    #pragma unroll
+#pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float p = exp2_fast(__builtin_fmaf(s[t][e], scale_log2, -use));
             l[e & 3] += p;
             pf[2 * t + (e >> 3)][0][e & 7] = (PE)p;
             if constexpr (PT == 2) pf[2 * t + (e >> 3)][1][e & 7] = (PE)(p - (float)(PE)p);
           }
-    #pragma unroll
+#pragma unroll
         for (int n = 0; n < NK; ++n)
-    #pragma unroll
+#pragma unroll
           for (int d = 0; d < ND; ++d) {
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][0] + n * 16 * RB));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + v_at[d][1] + n * 16 * RB));
             struct Both { s16x4 a, b; } both = {lo, hi};
             const P8 vf = __builtin_bit_cast(P8, both);
-    #pragma unroll
+#pragma unroll
             for (int e = 0; e < PT; ++e) acc[d] = MatrixOf<PE>::mul(vf, pf[n][e], acc[d]);
           }
       }
@@ -385,11 +404,11 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4SharedAttend a, int grid) {
   const int req = blockIdx.y, lane = threadIdx.x & 63;
-  Kv4Parts own{kv4_request(c, b, a, req), 0, 0, a.cols, a.part, a.part_ml}, shared = own;
+  Kv4Parts own{kv4_request(c, b, a, req), 0, 0, a.cols_shift, a.part, a.part_ml}, shared = own;
   const int n_cols = own.r.rows.count * a.q_heads;
   constexpr int PER = 256 / (HD / 4);
   if ((long long)blockIdx.x * PER >= n_cols) return;
-  const int g = group_of(a.prefix, req);
+  const int g = a.wide ? -1 : group_of(a.prefix, req);
   long long all = 0;
   shared.r.work = 0;
   for (int i = lane; i < kv4_requests(b, a); i += 64) {
@@ -400,9 +419,9 @@ __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b,
   }
   own.before = wave_sum64(own.before);
   own.per = shared.per = kv4_run(wave_sum64(all), grid);
-  if (kv4_live(c, b, a, req) && g >= 0) {
-    if (a.wide) shared = wide_parts(c, b, a, g);
-    else {
+  if (kv4_live(c, b, a, req)) {
+    if (a.wide) shared = wide_parts(a, req);
+    else if (g >= 0) {
       shared.r = kv4_request(c, b, a, b.batch + g);
       shared.before = wave_sum64(shared.before);
     }
@@ -412,15 +431,12 @@ __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b,
     const long long r = own.r.rows.begin + i, at = r * a.q_heads + h, at_prefix = ((long long)b.rows + r) * a.q_heads + h;
     const Kv4Parts::Place mine = own.place(c.kv_heads, head, i * a.group + in_head);
     if (a.wide && mine.w0 == mine.w1) continue;     // done
-    Kv4Sums s;
-    own.add<HD>(s, mine, d, a.whole + at * HD, a.whole_ml + at * 2);
+    Kv4Sums<1> s;
+    own.add<HD, 1>(s, mine, d, a.whole + at * HD, a.whole_ml + at * 2);
     const long long in_group = r - shared.r.rows.begin;
     if (shared.r.work && in_group >= 0 && in_group < shared.r.rows.count)
-      shared.add<HD>(s, shared.place(c.kv_heads, head, (int)in_group * a.group + in_head), d, a.whole + at_prefix * HD, a.whole_ml + at_prefix * 2);
-    const float inv = s.sum == 0.f ? 0.f : 1.f / s.sum;
-    float f[4] = {s.o[0] * inv, s.o[1] * inv, s.o[2] * inv, s.o[3] * inv};
-    store_vec<T, 4>(out.at(r, h) + d, f);
-    if (a.lse && d == 0) a.lse[at] = s.sum == 0.f ? -INFINITY : (s.top + log2f(s.sum)) * 0.6931471805599453f;
+      shared.add<HD, 1>(s, shared.place(c.kv_heads, head, (int)in_group * a.group + in_head), d, a.whole + at_prefix * HD, a.whole_ml + at_prefix * 2);
+    s.store(out.at(r, h) + d, a.lse && d == 0 ? a.lse + at : nullptr);
   }
 }
 
