@@ -94,9 +94,26 @@ __global__ __launch_bounds__(256) void beam_scan(BeamArgs a) {
   if (lane == 0) a.ms[(long long)row * (a.segments / N) + part] = ms;
 }
 
-__device__ __forceinline__ double wave_max64(double v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = fmax(v, __shfl_xor(v, o));
+template <int CTRL>
+__device__ __forceinline__ double dpp_move64(double v) {
+  const unsigned long long u = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double((unsigned long long)hi << 32 | lo);
+}
+// Maximum over the lanes of a row of 16 (rows != 0: over the wave), in every lane.
+__device__ __forceinline__ double wave_max64(double v, int rows) {
+  v = fmax(v, dpp_move64<kDppXor1>(v));
+  v = fmax(v, dpp_move64<kDppXor2>(v));
+  v = fmax(v, dpp_move64<kDppHalfMirror>(v));
+  v = fmax(v, dpp_move64<kDppMirror>(v));
+  if (rows) {
+    unsigned long long u = __double_as_longlong(v);
+    auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = fmax(__longlong_as_double((unsigned long long)hi[0] << 32 | lo[0]), __longlong_as_double((unsigned long long)hi[1] << 32 | lo[1]));
+    u = __double_as_longlong(v);
+    lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = fmax(__longlong_as_double((unsigned long long)hi[0] << 32 | lo[0]), __longlong_as_double((unsigned long long)hi[1] << 32 | lo[1]));
+  }
   return v;
 }
 __device__ __forceinline__ double wave_sum64d(double v) {
@@ -120,8 +137,10 @@ __device__ __forceinline__ int beam_rank(float2 *list, int count, int most) {
     float best = -INFINITY;
     int at = 0x7FFFFFFF;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+      if (64 * k >= count) break;
       if (beam_before(last, last_i, v[k], i[k]) && beam_before(v[k], i[k], best, at)) best = v[k], at = i[k];
+    }
     beam_wave_best(best, at);
     last = best, last_i = at;
     if (lane == n) keep = best, keep_i = at;
@@ -146,8 +165,18 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
   for (int b = wave; b < a.beams; b += W) {
     const int row = g * a.beams + b;
     const float before = a.score_in[row];
-    const bool done = a.done_in && a.done_in[row] != 0, alive = before > -INFINITY;
-    const int length = (a.length_in ? a.length_in[row] : 0) + !done;
+    const int ended = a.done_in ? a.done_in[row] : 0, had = a.length_in ? a.length_in[row] : 0;
+    float tops[K], m = -INFINITY;
+    constexpr int P = DIRECT ? 1 : (1 << 19) / kBeamWave / 64;          // parts per lane
+    float2 ms[P];
+    if constexpr (!DIRECT) {                        // requested before it is known whether they are wanted
+#pragma unroll
+      for (int k = 0; k < P; ++k) ms[k] = lane + 64 * k < a.segments / N ? a.ms[(long long)row * (a.segments / N) + lane + 64 * k] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < K; ++k) tops[k] = lane + 64 * k < a.segments ? a.top[(long long)row * a.segments + lane + 64 * k] : -INFINITY;
+    }
+    const bool done = ended != 0, alive = before > -INFINITY;
+    const int length = had + !done;
     int count = 0;
     double add = before;
     if (alive && done) {
@@ -155,7 +184,6 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
       count = 1;
     } else if (alive) {
       const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
-      float tops[K], m = -INFINITY;
       double sum = 0;
       if constexpr (DIRECT) {
         tops[0] = -INFINITY;
@@ -166,14 +194,15 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
           m = next;
         }
       } else {
-        const int parts = a.segments / N;
-        const float2 *ms = a.ms + (long long)row * parts;
-        for (int i = lane; i < parts; i += 64) m = fmaxf(m, ms[i].x);
-        m = wave_max(m);
-        for (int i = lane; i < parts; i += 64) sum += ms[i].x > -INFINITY ? (double)ms[i].y * exp((double)ms[i].x - (double)m) : 0.0;
-        sum = wave_sum64d(sum);
 #pragma unroll
-        for (int k = 0; k < K; ++k) tops[k] = lane + 64 * k < a.segments ? a.top[(long long)row * a.segments + lane + 64 * k] : -INFINITY;
+        for (int k = 0; k < P; ++k) m = fmaxf(m, ms[k].x);
+        m = wave_max(m);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          if (64 * k >= a.segments / N) break;
+          sum += ms[k].x > -INFINITY ? (double)ms[k].y * exp((double)ms[k].x - (double)m) : 0.0;
+        }
+        sum = wave_sum64d(sum);
       }
       if (m > -INFINITY && m < INFINITY) {
         add -= (double)m + log(sum);
@@ -184,8 +213,10 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
           float best = -INFINITY;
           int at = 0x7FFFFFFF;
 #pragma unroll
-          for (int k = 0; k < K; ++k)
+          for (int k = 0; k < K; ++k) {
+            if (64 * k >= a.segments) break;
             if (beam_before(last, last_i, tops[k], lane + 64 * k) && beam_before(tops[k], lane + 64 * k, best, at)) best = tops[k], at = lane + 64 * k;
+          }
           beam_wave_best(best, at);
           if (!(best > -INFINITY)) break;
           last = best, last_i = at;
@@ -193,21 +224,30 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
         }
         float floor = chosen == a.width ? last : -INFINITY;
         int floor_i = 0x7FFFFFFF;
-        for (int n = 0; n < chosen; ++n) {
-          float f[V];
-          const int t0 = beam_load(x, a.vocab, __builtin_amdgcn_readlane(mine, n), f);
+        constexpr int B = 8;                        // segments requested at once
+        for (int n0 = 0; n0 < chosen; n0 += B) {
+          float f[B][V];
+          int t0[B];
 #pragma unroll
-          for (int e0 = 0; e0 < V; e0 += 4) {
-            if (count > kBeamList - 256) {
-              count = beam_rank(s_list[wave], count, a.width);
-              if (count == a.width) floor = s_list[wave][count - 1].x, floor_i = __float_as_int(s_list[wave][count - 1].y);
-            }
+          for (int n = 0; n < B; ++n)
+            if (n0 + n < chosen) t0[n] = beam_load(x, a.vocab, __builtin_amdgcn_readlane(mine, n0 + n), f[n]);
 #pragma unroll
-            for (int e = e0; e < e0 + 4; ++e) {
-              const bool yes = f[e] > -INFINITY && !beam_before(floor, floor_i, f[e], t0 + e);
-              const unsigned long long all = __ballot(yes);
-              if (yes) s_list[wave][count + __popcll(all & ((1ull << lane) - 1))] = make_float2(f[e], __int_as_float(t0 + e));
-              count += __popcll(all);
+          for (int n = 0; n < B; ++n) {
+            if (n0 + n >= chosen) break;
+#pragma unroll
+            for (int e0 = 0; e0 < V; e0 += 4) {
+              if (count > kBeamList - 256) {
+                count = beam_rank(s_list[wave], count, a.width);
+                if (count == a.width) floor = s_list[wave][count - 1].x, floor_i = __float_as_int(s_list[wave][count - 1].y);
+              }
+#pragma unroll
+              for (int e = e0; e < e0 + 4; ++e) {
+                const bool yes = f[n][e] > -INFINITY && !beam_before(floor, floor_i, f[n][e], t0[n] + e);
+                const unsigned long long all = __ballot(yes);
+                if (!all) continue;
+                if (yes) s_list[wave][count + __popcll(all & ((1ull << lane) - 1))] = make_float2(f[n][e], __int_as_float(t0[n] + e));
+                count += __popcll(all);
+              }
             }
           }
         }
@@ -217,7 +257,7 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
     }
     if (lane == 0) {
       s_add[b] = add;
-      s_norm[b] = a.power == 0 ? 1.0 : pow((double)max(length, 1), -a.power);
+      s_norm[b] = a.power == 0 ? 1.0 : exp(-a.power * log((double)max(length, 1)));
       s_len[b] = length;
       s_done[b] = done;
       s_count[b] = count;
@@ -233,8 +273,8 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
     const float2 next = at < count ? s_best[lane * a.width + at] : make_float2(0.f, 0.f);
     const double score = at < count ? add + (double)next.x : -INFINITY;
     const double rank = at < count ? score * norm : -INFINITY;
-    const double best = wave_max64(rank);
-    const unsigned long long who = __ballot(at < count && rank == best);
+    const double best = wave_max64(rank, a.beams > 16);
+    const unsigned long long who = __ballot(at < count && rank == best) & (a.beams > 16 ? ~0ull : 0xFFFFull);      // (of one row: the others hold their own maxima)
     const long long to = (long long)g * a.width + n;
     if (!who) {                                     // no more candidates
       if (lane == 0) {

@@ -318,12 +318,35 @@ struct EvictTask {
   }
 };
 
+// Inclusive sum over the lanes of a wave, in the vector ALU: within rows of 16, then from row to row.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);      // row_shr 1, 2, 4, 8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
+  const uint32_t r0 = __builtin_amdgcn_readlane((int)v, 15), r1 = __builtin_amdgcn_readlane((int)v, 31), r2 = __builtin_amdgcn_readlane((int)v, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return v + (row > 0 ? r0 : 0) + (row > 1 ? r1 : 0) + (row > 2 ? r2 : 0);
+}
+// Sum over the workgroup's threads before this one; total: over all.  part: W values of LDS that nothing else uses before the next barrier but one.
+template <int W>
+__device__ __forceinline__ uint32_t evict_scan(uint32_t v, uint32_t &total, uint32_t *part) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t upto = wave_scan(v);
+  if (lane == 63) part[wave] = upto;
+  __syncthreads();
+  const uint32_t parts = wave_scan(lane < W ? part[lane] : 0);
+  total = __builtin_amdgcn_readlane((int)parts, W - 1);
+  const uint32_t before = __builtin_amdgcn_ds_bpermute(max(wave - 1, 0) * 4, (int)parts);
+  return upto - v + (wave ? before : 0);
+}
+
 // The bin, counted from the last, in which the `left`-th lies: {bin, how many of it are wanted}.  Clears the bins.  All of the workgroup's threads.
 template <int W, int BINS>
 __device__ __forceinline__ uint2 evict_bin(uint32_t *hist, uint32_t left, uint32_t *part, uint2 *pick) {
   constexpr int PER = BINS / (W * 64);
   static_assert(PER >= 1 && BINS % (W * 64) == 0, "bins per thread");
-  uint32_t h[PER], sum = 0, none = 0;
+  uint32_t h[PER], sum = 0, all;
   const int top = BINS - 1 - threadIdx.x * PER;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -331,7 +354,7 @@ __device__ __forceinline__ uint2 evict_bin(uint32_t *hist, uint32_t left, uint32
     hist[top - i] = 0;
     sum += h[i];
   }
-  uint32_t before = plan_scan<W>(sum, none, part) - sum;
+  uint32_t before = evict_scan<W>(sum, all, part);
   if (before < left && left <= before + sum) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -354,8 +377,8 @@ constexpr int kEvictLot = 4;                        // moves that a sixteenth of
 template <int HD, int W, int E>
 __global__ __launch_bounds__(W * 64) void kv4_evict_held(Kv4Cache cache, PagedBatch b, EvictArgs a) {
   constexpr int N = W * 64, BINS = 2048;
-  __shared__ uint32_t hist[BINS], part[W];
-  __shared__ uint2 pick;
+  __shared__ uint32_t hist[BINS], part[5][W];
+  __shared__ uint2 pick[3];
   __shared__ uint16_t holes[N * E / 2], fillers[N * E / 2];
   const int tid = threadIdx.x;
   for (int i = tid; i < BINS; i += N) hist[i] = 0;
@@ -376,25 +399,24 @@ __global__ __launch_bounds__(W * 64) void kv4_evict_held(Kv4Cache cache, PagedBa
   for (int i = 0; i < E; ++i) key[i] = t0 + i < k.cand ? evict_key(w[i]) : 0;
   uint32_t prefix = 0, left = (uint32_t)k.first;
   if (k.first) {
-    auto digit = [&](int shift, int above, uint32_t mask) {
+    auto digit = [&](int n, int shift, int above, uint32_t mask) {
 #pragma unroll
       for (int i = 0; i < E; ++i)
         if (t0 + i < k.cand && (above > 31 || key[i] >> above == prefix >> above)) atomicAdd(&hist[key[i] >> shift & mask], 1u);
       __syncthreads();
-      const uint2 d = evict_bin<W, BINS>(hist, left, part, &pick);
+      const uint2 d = evict_bin<W, BINS>(hist, left, part[n], &pick[n]);
       prefix |= d.x << shift;
       left = d.y;
-      __syncthreads();
     };
-    digit(21, 32, 2047);
-    digit(10, 21, 2047);
-    digit(0, 10, 1023);
+    digit(0, 21, 32, 2047);
+    digit(1, 10, 21, 2047);
+    digit(2, 0, 10, 1023);
   }
   // tokens at the threshold: the first `left` stay
-  uint32_t equal = 0, none = 0;
+  uint32_t equal = 0, none;
 #pragma unroll
   for (int i = 0; i < E; ++i) equal += t0 + i < k.cand && key[i] == prefix;
-  uint32_t before = plan_scan<W>(equal, none, part) - equal;
+  uint32_t before = evict_scan<W>(equal, none, part[3]);
   uint32_t stays = 0, counts = 0;                   // holes in the low half, fillers in the high
 #pragma unroll
   for (int i = 0; i < E; ++i) {
@@ -404,8 +426,7 @@ __global__ __launch_bounds__(W * 64) void kv4_evict_held(Kv4Cache cache, PagedBa
     stays |= (uint32_t)yes << i;
     counts += t0 + i < k.first ? !yes : yes ? 0x10000u : 0u;
   }
-  none = 0;
-  uint32_t at = plan_scan<W>(counts, none, part) - counts;
+  uint32_t at = evict_scan<W>(counts, none, part[4]);
   const int fills = (int)(none & 0xFFFFu);
 #pragma unroll
   for (int i = 0; i < E; ++i) {

@@ -3,7 +3,9 @@
 Tolerances.  Whole numbers, copies and evictions are exact.  Beams: a score is a logit, a sum in 64 bits and the logarithm of a sum of exponentials; an
 exponential is off by 2^-22, its sum over a thread's 32 values and a wave by 40 additions of 2^-24, the sums of chunks are joined in 64 bits: at most 2^-18
 absolutely, and the result is rounded once.  Continuations whose ranks are nearer than that may be in either order, exactly equal ones may not.
-Shared attention: that of heisd_kv4_attention over the prefix's and the request's own tokens (test_gpu_paged.py).  Weights: a score is off by S = (head_dim + 8)
+Shared attention: that of heisd_kv4_attention over the prefix's and the request's own tokens (test_gpu_paged.py); over a prefix a probability p
+may enter the product as one fp16 number, off by 2^-11 p or, below 2^-25 of the largest, by 2^-36 of it, which moves sum(p v) / sum(p) by at most
+2^-11 of the weighted mean of |v| and 2^-36 of the sum of |v| over the largest weight's sum.  Weights: a score is off by S = (head_dim + 8)
 2^-24 * scale * sum |q_i k_i|, the exponent's argument by 2^-22 of its parts and an exponential by 2^-22; sums of n of them add (n + 32) 2^-24."""
 import math
 
@@ -300,7 +302,7 @@ def prefix_of(groups, batch, seq, max_prefix):
     return out
 
 
-def check_shared(c, groups, q, out, lse, cu_rows, k, v, scale, dtype, max_prefix, seq=None, gone=None, heads=None, p_rounding=2.0 ** -16):
+def check_shared(c, groups, q, out, lse, cu_rows, k, v, scale, dtype, max_prefix, seq=None, gone=None, heads=None):
     seq = list(c.total) if seq is None else seq
     q64, out, lse = host(q), host(out), host(lse)
     parents = prefix_of(groups, len(seq), seq, max_prefix)
@@ -320,7 +322,7 @@ def check_shared(c, groups, q, out, lse, cu_rows, k, v, scale, dtype, max_prefix
             want, wl, mean, flat, size = ref.attention(q64[r:r + 1], kk, vv, [len(kk)], scale)
             nan = np.isnan(want)
             assert np.array_equal(np.isnan(out[r:r + 1]), nan), (i, r)
-            tol = tolerance(dtype, p_rounding, 0.0, q.shape[2], len(kk), want, mean, flat, size)
+            tol = tolerance(dtype, 2.0 ** -11, 2.0 ** -36, q.shape[2], len(kk), want, mean, flat, size)
             assert np.all((np.abs(out[r:r + 1] - want) <= tol)[~nan]), (i, r, np.nanmax(np.abs(out[r] - want)))
             fine = np.isfinite(wl)
             assert np.array_equal(lse[r:r + 1][~fine], wl[~fine], equal_nan=True)
