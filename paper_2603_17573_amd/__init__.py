@@ -24,6 +24,6 @@ from .binding import (heisd_model_desc, heisd_kv_desc, heisd_accept_desc, heisd_
                       make_accept_desc, make_model_desc, HEISD_OK, HEISD_EINVAL, HEISD_EUNSUPPORTED,
                       HEISD_ENOMEM, HEISD_EHIP)
 from .runner import (DeviceModel, Verifier, PagedCache, build_sequence_tree, head_rows, make_plan_desc, make_rope_desc, rope_table,
-                     make_kv4_desc, make_paged_batch, make_beam_desc, make_reorder_desc, make_prefix_groups)
+                     make_kv4_desc, make_paged_batch, make_beam_desc, make_reorder_desc, make_prefix_groups, beam_select)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -69,21 +69,117 @@ struct WeighArgs {
 constexpr int kWeighPairs = 8;                      // pairs of tiles that a wave takes at most
 constexpr int kWeighUnit = 128;                     // tokens of a pair for each of the four waves
 
+// The same for four tiles: a quarter of a token's head in each of them, and the weight that the lane's token of the 64 had.
+template <int HD>
+struct WeighFour {
+  uint32_t kc[4][HD / 32], ke[4];
+  float old;
+};
 // What a lane holds of the keys of two tiles of 16 tokens: a quarter of one token's head in each, and the weight that one of the tokens had.
 template <int HD>
 struct WeighPair {
   uint32_t kc[2][HD / 32], ke[2];
   float old;
 };
-template <int HD>
-__device__ __forceinline__ bf16x8 weigh_keys(const WeighPair<HD> &p, int n, int j) {
-  const float ks = __uint_as_float(p.ke[n] << 23);
-  const uint32_t w = p.kc[n][j];
+__device__ __forceinline__ bf16x8 weigh_keys(uint32_t w, uint32_t e) {
+  const float ks = __uint_as_float(e << 23);
   const auto x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 1),
              x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ks, 3);
   bf16x8 k;
   k[0] = x0[0], k[1] = x0[1], k[2] = x1[0], k[3] = x1[1], k[4] = x2[0], k[5] = x2[1], k[6] = x3[0], k[7] = x3[1];
   return k;
+}
+
+// The weights of tokens [t0, t1) of a request with at most four columns (a single token and up to four query heads per key head, four single heads' tokens).  Of a product
+// for sixteen columns these would be a quarter, so tokens are its columns here and the queries its rows, four times over: of tile k's scores the lanes 16 k on keep
+// theirs, and four tiles give every lane one token with all of its scores.  Nothing is exchanged between lanes, and there are a quarter of the exponents
+// (64 contexts of 256 to 8191 tokens: 44 us with columns as columns).
+template <typename T, int HD, int TERMS>
+__device__ __forceinline__ void weigh_four(const Kv4Cache &c, const PagedBatch &b, const HeadRows<const T> &q, const WeighArgs &a, int req, int head, Span own, int had,
+                                           int t0, int t1) {
+  constexpr int KJ = HD / 32;
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, bs = c.block_size;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = t0 + wave * 64;
+  const int units = max((t1 - first + 255) / 256, 0);
+  if (!units) return;
+  int my_id = -1;                                   // lane 4 i + k: the block of tile k of the i-th 64 tokens
+  {
+    const int t = first + 256 * (lane >> 2) + 16 * (lane & 3);
+    if (lane < 4 * units && t < t1) my_id = b.table[(long long)req * b.max_blocks + (t >> c.block_shift)];
+    if (my_id >= c.n_blocks) my_id = -1;
+  }
+  const int n_cols = own.count * a.group;
+  bf16x8 qf[KJ][TERMS];
+  float lse[4];
+  int seen[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int n = min(e, n_cols - 1), i = n / a.group;
+    const float x = n_cols ? a.lse[(long long)(own.begin + i) * a.q_heads + head * a.group + (n - i * a.group)] : 0.f;
+    lse[e] = x * 1.4426950408889634f;
+    seen[e] = e >= n_cols || x == -INFINITY ? 0 : had + 1 + i;
+  }
+  {
+    const int n = min(col & 3, n_cols - 1), i = n_cols ? n / a.group : 0;
+    const T *from = n_cols ? q.at(own.begin + i, head * a.group + (n - i * a.group)) + quad * (HD / 4) : nullptr;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j) {
+      typename VecOf<T, 8>::type v{};
+      if (n_cols) v = *reinterpret_cast<const typename VecOf<T, 8>::type *>(from + j * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = (float)v[e];
+        qf[j][0][e] = (__bf16)f;
+        if constexpr (TERMS == 2) qf[j][1][e] = (__bf16)(f - (float)qf[j][0][e]);
+      }
+    }
+  }
+  auto weight_at = [&](int u) {
+    const int id = __builtin_amdgcn_ds_bpermute((4 * u + quad) * 4, my_id), t = first + 256 * u + lane;
+    return id < 0 || t >= t1 ? -1ll : ((long long)id * c.kv_heads + head) * bs + (t & (bs - 1));
+  };
+  auto fetch = [&](int u) {
+    WeighFour<HD> r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint8_t *cell = c.at(max(__builtin_amdgcn_readlane(my_id, 4 * u + k), 0), head);      // a missing block: any block, not written
+      const int o = ((first + 256 * u + 16 * k) & (bs - 1)) + col;
+      const uint32_t *codes = reinterpret_cast<const uint32_t *>(cell + o * (HD / 2) + quad * (HD / 8));
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) r.kc[k][j] = codes[j];
+      r.ke[k] = cell[Kv4Offsets<HD>::k_exp(bs) + o * (HD / 32) + quad * (HD / 4) / 32];
+    }
+    const long long at = weight_at(u);
+    r.old = at >= 0 && first + 256 * u + lane < had ? a.weight_in[at] : 0.f;
+    return r;
+  };
+  WeighFour<HD> next = fetch(0);
+  for (int u = 0; u < units; ++u) {
+    const WeighFour<HD> now = next;
+    if (u + 1 < units) next = fetch(u + 1);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) {
+        const bf16x8 kf = weigh_keys(now.kc[k][j], now.ke[k]);
+#pragma unroll
+        for (int e = 0; e < TERMS; ++e) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j][e], kf, x, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = quad == k ? x[e] : s[e];
+    }
+    const int t = first + 256 * u + lane;
+    float fresh = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float pr = exp2_fast(__builtin_fmaf(s[e], a.scale_log2, -lse[e]));
+      fresh += t < seen[e] ? pr : 0.f;
+    }
+    const long long at = weight_at(u);
+    if (at >= 0) a.weight_out[at] = __builtin_fmaf(a.decay, now.old, fresh);
+  }
 }
 
 // weight[t] = decay * weight[t] + sum over the rows that see token t and the query heads of its key head of exp(scale q . k - lse).  Scores are one
@@ -93,15 +189,22 @@ __device__ __forceinline__ bf16x8 weigh_keys(const WeighPair<HD> &p, int n, int 
 // A wave takes `pairs` pairs of tiles, the next one on its way while it works.  Where 16 columns hold all rows (single tokens and few), their queries
 // stay in registers.
 template <typename T, int HD, int TERMS>
-__global__ __launch_bounds__(256) void kv4_weigh(Kv4Cache c, PagedBatch b, PrefixGroups p, HeadRows<const T> q, WeighArgs a, int pairs) {
+__global__ __launch_bounds__(256, 4) void kv4_weigh(Kv4Cache c, PagedBatch b, PrefixGroups p, HeadRows<const T> q, WeighArgs a, int pairs) {
   constexpr int KJ = HD / 32;
   const int req = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bs = c.block_size;
   const int seq = b.seq_len[req], t0 = blockIdx.x * (kWeighUnit * pairs) + wave * 32;
-  if (seq <= t0 || seq > max(a.max_seq, p.groups ? p.max_prefix : 0) || (long long)seq > (long long)b.max_blocks * bs) return;
+  if (seq <= (int)blockIdx.x * (kWeighUnit * pairs) || seq > max(a.max_seq, p.groups ? p.max_prefix : 0) || (long long)seq > (long long)b.max_blocks * bs) return;
   Span own = wave_span(b.cu_rows, req, b.rows);
   const int had = seq - own.count;                  // tokens that had a weight before
   if (seq > a.max_seq) own.count = 0;
+  unsigned long long any = 0;                       // is it anybody's prefix?
+  for (int g0 = 0; g0 < p.groups && !any; g0 += 64) any = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
+  if (!any && own.count * a.group <= 4) {
+    weigh_four<T, HD, TERMS>(c, b, q, a, req, head, own, had, blockIdx.x * (kWeighUnit * pairs), min(seq, (int)(blockIdx.x + 1) * (kWeighUnit * pairs)));
+    return;
+  }
+  if (seq <= t0) return;
   const int n_pairs = min((seq - t0 + kWeighUnit - 1) / kWeighUnit, pairs);
   int my_id = -1;                                   // lane 2 i + n: the block of tile n of the i-th pair
   {
@@ -153,14 +256,7 @@ __global__ __launch_bounds__(256) void kv4_weigh(Kv4Cache c, PagedBatch b, Prefi
       }
     }
   };
-  auto add = [&](float (&sum)[2][4], const bf16x8 (&kf)[2][KJ], const Column &x, int base) {
-    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-    for (int j = 0; j < KJ; ++j)
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < TERMS; ++e) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][j], x.q[j][e], s[n], 0, 0, 0);
+  auto collect = [&](float (&sum)[2][4], const f32x4 (&s)[2], const Column &x, int base) {
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -169,44 +265,22 @@ __global__ __launch_bounds__(256) void kv4_weigh(Kv4Cache c, PagedBatch b, Prefi
         sum[n][e] += base + 16 * n + 4 * quad + e < x.seen ? pr : 0.f;
       }
   };
-  unsigned long long any = 0;                       // is it anybody's prefix?
-  for (int g0 = 0; g0 < p.groups && !any; g0 += 64) any = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
+  auto add = [&](float (&sum)[2][4], const bf16x8 (&kf)[2][KJ], const Column &x, int base) {
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < TERMS; ++e) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][j], x.q[j][e], s[n], 0, 0, 0);
+    collect(sum, s, x, base);
+  };
   const int own_cols = own.count * a.group, seen0 = had + 1;
   const bool few = !any && own_cols <= 16;
   Column only;
   if (few && own_cols) column(only, own, 0, seen0, true);
-  WeighPair<HD> next = fetch(0);
-  for (int i = 0; i < n_pairs; ++i) {
-    const WeighPair<HD> now = next;
-    if (i + 1 < n_pairs) next = fetch(i + 1);
-    const int base = t0 + kWeighUnit * i;
-    bf16x8 kf[2][KJ];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int j = 0; j < KJ; ++j) kf[n][j] = weigh_keys<HD>(now, n, j);
-    float sum[2][4] = {};
-    if (few) {
-      if (own_cols) add(sum, kf, only, base);
-    } else {
-      Column x;
-      for (int c0 = max(base - seen0 + 1, 0) * a.group & ~15; c0 < own_cols; c0 += 16) {        // rows before see none of these tokens
-        column(x, own, c0, seen0, true);
-        add(sum, kf, x, base);
-      }
-      for (int g0 = 0; g0 < p.groups; g0 += 64) {   // the groups that this request is the prefix of
-        unsigned long long mine = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
-        for (; mine; mine &= mine - 1) {
-          const PrefixSpan s = prefix_span(c, b, p, g0 + __builtin_ctzll(mine));
-          if (s.request != req) continue;
-          const Span rows{__builtin_amdgcn_readfirstlane(s.rows.begin), __builtin_amdgcn_readfirstlane(s.rows.count)};
-          for (int c0 = 0; c0 < rows.count * a.group; c0 += 16) {
-            column(x, rows, c0, 0, false);
-            add(sum, kf, x, base);
-          }
-        }
-      }
-    }
+  // the weights of pair i: the columns' sums, added up by the 16 lanes of a token
+  auto finish = [&](int i, const float (&sum)[2][4], float old) {
     const long long at = weight_at(i);
     float fresh = 0.f;
 #pragma unroll
@@ -216,7 +290,59 @@ __global__ __launch_bounds__(256) void kv4_weigh(Kv4Cache c, PagedBatch b, Prefi
         const float all = sum16(sum[n][e]);
         fresh = col == 4 * n + e ? all : fresh;
       }
-    if (at >= 0) a.weight_out[at] = __builtin_fmaf(a.decay, now.old, fresh);
+    if (at >= 0) a.weight_out[at] = __builtin_fmaf(a.decay, old, fresh);
+  };
+  if (few) {
+    WeighPair<HD> next = fetch(0);
+    for (int i = 0; i < n_pairs; ++i) {
+      const WeighPair<HD> now = next;
+      if (i + 1 < n_pairs) next = fetch(i + 1);
+      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      float sum[2][4] = {};
+      if (own_cols) {
+#pragma unroll
+        for (int j = 0; j < KJ; ++j)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const bf16x8 kf = weigh_keys(now.kc[n][j], now.ke[n]);
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, only.q[j][e], s[n], 0, 0, 0);
+          }
+        collect(sum, s, only, t0 + kWeighUnit * i);
+      }
+      finish(i, sum, now.old);
+    }
+    return;
+  }
+  WeighPair<HD> next = fetch(0);
+  for (int i = 0; i < n_pairs; ++i) {
+    const WeighPair<HD> now = next;
+    if (i + 1 < n_pairs) next = fetch(i + 1);
+    const int base = t0 + kWeighUnit * i;
+    bf16x8 kf[2][KJ];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) kf[n][j] = weigh_keys(now.kc[n][j], now.ke[n]);
+    float sum[2][4] = {};
+    Column x;
+    for (int c0 = max(base - seen0 + 1, 0) * a.group & ~15; c0 < own_cols; c0 += 16) {        // rows before see none of these tokens
+      column(x, own, c0, seen0, true);
+      add(sum, kf, x, base);
+    }
+    for (int g0 = 0; g0 < p.groups; g0 += 64) {     // the groups that this request is the prefix of
+      unsigned long long mine = __ballot(g0 + lane < p.groups && p.prefix[min(g0 + lane, p.groups - 1)] == req);
+      for (; mine; mine &= mine - 1) {
+        const PrefixSpan s = prefix_span(c, b, p, g0 + __builtin_ctzll(mine));
+        if (s.request != req) continue;
+        const Span rows{__builtin_amdgcn_readfirstlane(s.rows.begin), __builtin_amdgcn_readfirstlane(s.rows.count)};
+        for (int c0 = 0; c0 < rows.count * a.group; c0 += 16) {
+          column(x, rows, c0, 0, false);
+          add(sum, kf, x, base);
+        }
+      }
+    }
+    finish(i, sum, now.old);
   }
 }
 

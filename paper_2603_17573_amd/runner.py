@@ -280,11 +280,15 @@ class PagedCache:
     the order a decoder makes them: begin() once, then for every layer rotate(), append() and one of attend() (single
     tokens and drafts), prompt() (whole prompts into empty caches) or chunk() (chunks behind cached rows).
 
+    Requests that continue others: share() says which ones see another request's tokens in front of their own, attend_shared() then takes the place of attend();
+    fork() lets requests go on as continuations of others; weigh() adds up what attention the tokens receive (weights=True), evict() keeps those that received
+    most.  offset() gives rows the positions that they have behind a prefix or after an eviction.
+
     max_batch requests of at most max_len tokens (rounded up to whole blocks); a step has at most max_rows packed rows.  Everything the calls need is allocated
-    here, so a step can be captured into a HIP graph (chunk() too, once its buffers have been made by a first call)."""
+    here (and by share()), so a step can be captured into a HIP graph (chunk() too, once its buffers have been made by a first call)."""
 
     def __init__(self, n_layers, q_heads, kv_heads, head_dim, max_batch, max_len, max_rows, n_blocks, block_size=64, rope=None,
-                 layout="half", max_new=1, device="cuda:0"):
+                 layout="half", max_new=1, device="cuda:0", weights=False):
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
@@ -309,10 +313,13 @@ class PagedCache:
             if n == 0:
                 raise ValueError("invalid attention: %d query heads, %d rows, max_new %d, max_len %d" % (q_heads, max_rows, max_new, self.max_len))
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+            self.weights = torch.empty((n_layers, n_blocks, kv_heads, block_size), device=self.device) if weights else None
+            self.lengths, self.copy_from = torch.empty(max_batch, **i32), torch.empty(max_batch, **i32)
+            self._table, self._owned = torch.empty_like(self.table), torch.empty_like(self.owned)
             desc = rope if rope is not None else make_rope_desc(head_dim)
             self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]
             self.turns, self.magnitude = rope_table(desc, self.device)
-        self.rows, self._kv, self._captured = 0, {}, []
+        self.rows, self._kv, self._captured, self._shared = 0, {}, [], None
         self.batch = make_paged_batch(self.table, self.seq_len, self.cu_rows, 0)
 
     def _call(self, fn, *args):
@@ -364,6 +371,74 @@ class PagedCache:
                    self.workspace.numel())
         return out
 
+    def offset(self, offset):
+        """Adds offset i32[max_batch] to the positions of this step's rows, request by request: the length of the prefix that a request's tokens lie behind, the
+        number of its tokens that were evicted.  Once per step, before rotate()."""
+        self._call(B.heisd_paged_offset, self.batch, _ints(offset, self.seq_len.shape, "offset", self.device), self.position.data_ptr())
+
+    def share(self, first, prefix, max_rows, max_prefix=None, max_own=None):
+        """first i32[groups + 1], prefix i32[groups]: the requests first[g] .. first[g + 1] - 1 see the tokens of request prefix[g] in front of their own, from
+        now on (both may change between steps).  max_rows: at least the rows of a group in a step; max_prefix, max_own (max_len if not given): at least the longest prefix, and the
+        longest request that has rows."""
+        groups = make_prefix_groups(first, prefix, max_rows, self.max_len if max_prefix is None else max_prefix)
+        if first.device != self.device:
+            raise ValueError("first, prefix: expected on %s, got on %s" % (self.device, first.device))
+        own = self.max_len if max_own is None else max_own
+        n = B.heisd_kv4_shared_attention_workspace_bytes(self.descs[0], self.table.shape[0], self.slot.shape[0], self.q_heads, self.max_new, own, groups)
+        if n == 0:
+            raise ValueError("invalid groups: max_rows %d, max_prefix %d, max_own %d" % (max_rows, groups.max_prefix, own))
+        with torch.cuda.device(self.device):
+            self._shared = (groups, own, torch.empty(n, dtype=torch.uint8, device=self.device), first, prefix)
+
+    def attend_shared(self, layer, q, scale=None, out=None, lse=None):
+        """Attention of this step's rows over their group's prefix and everything their requests have cached."""
+        if self._shared is None:
+            raise ValueError("attend_shared without share")
+        out = torch.empty_like(q) if out is None else out
+        hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
+        groups, own, workspace = self._shared[:3]
+        self._call(B.heisd_kv4_shared_attention, self.descs[layer], self.batch, groups, hq, ho, self._lse(lse),
+                   self.head_dim ** -0.5 if scale is None else scale, self.max_new, own, workspace.data_ptr(), workspace.numel())
+        return out
+
+    def weigh(self, layer, q, lse, scale=None, decay=1.0):
+        """Adds to the weight of every cached token (times decay) the attention that it receives from this step's rows; lse: what attend() or attend_shared() of
+        the same rows gave."""
+        if self.weights is None:
+            raise ValueError("weigh: made without weights")
+        groups, own = self._shared[:2] if self._shared is not None else (None, self.max_len)
+        w = self.weights[layer].data_ptr()
+        self._call(B.heisd_kv4_weigh, self.descs[layer], self.batch, groups, self._of_step(q, self.q_heads, "q"), self._lse(lse),
+                   self.head_dim ** -0.5 if scale is None else scale, decay, w, w, own)
+
+    def evict(self, keep, recent):
+        """Cuts every request of more than keep[b] tokens (i32[max_batch], negative: it stays as it is) to keep[b], in every layer and head for itself: the last `recent`
+        stay, and of the others those with the largest weights.  Returns the lengths, i32[max_batch], which the next begin() takes as cached_len (the buffer is
+        written again by the next evict() or fork())."""
+        if self.weights is None:
+            raise ValueError("evict: made without weights")
+        w = self.weights.data_ptr()
+        self._call(B.heisd_kv4_evict, self.descs[0], len(self.descs), self.pools.shape[1], self.batch,
+                   _ints(keep, self.seq_len.shape, "keep", self.device), recent, w, w, self.lengths.data_ptr(), self.max_len)
+        self.seq_len.copy_(self.lengths)
+        return self.lengths
+
+    def fork(self, parent, length, trim=False):
+        """Request b goes on as a continuation of what was request parent[b] with its first length[parent[b]] tokens (i32[max_batch]; a parent outside
+        0 .. max_batch - 1: it ends); trim: blocks behind those tokens are given back.  Between two steps.  Returns the lengths as evict() does; a request that got no blocks has -1."""
+        shape, dev = self.seq_len.shape, self.device
+        _ints(parent, shape, "parent", dev), _ints(length, shape, "length", dev)
+        if length.data_ptr() == self.lengths.data_ptr():
+            length = length.clone()
+        self._call(B.heisd_paged_reorder, make_reorder_desc(self.block_size, self.n_blocks, parent, length, self.owned, self.table, self.lengths, self._owned,
+                                                            self._table, self.copy_from, self.free_ids, self.free_count, self.free_count, trim))
+        self._call(B.heisd_kv4_copy, self.descs[0], len(self.descs), self.pools.shape[1], make_paged_batch(self._table, self.lengths, None, 0),
+                   self.copy_from.data_ptr(), None if self.weights is None else self.weights.data_ptr(), self.max_len)
+        self.table.copy_(self._table)
+        self.owned.copy_(self._owned)
+        self.seq_len.fill_(-1)
+        return self.lengths
+
     def prompt(self, q, k, v, scale=None, out=None, lse=None):
         """Causal attention of whole prompts over their own rows (nothing cached before them), as they are and not as they are held."""
         out = torch.empty_like(q) if out is None else out
@@ -399,3 +474,24 @@ class PagedCache:
                    self.cu_seq.data_ptr(), self.table.shape[0], self.rows, total, self.head_dim,
                    self.head_dim ** -0.5 if scale is None else scale, 1)
         return out
+
+
+def beam_select(logits, beams, width, score, length=None, done=None, end_token=-1, length_power=0.0, parent=None, first=0, stride=0):
+    """The `width` best continuations of every group of `beams` beams (heisd_beam_select): a dict of score, beam, token and, where they are given,
+    length and done, [groups, width].  logits [groups * beams, vocab]; score f32, length and done i32 [groups * beams]; parent i32 takes, from entry
+    first + group * stride on, which request every new beam continues, as PagedCache.fork() wants it."""
+    if not logits.is_cuda or logits.dim() != 2 or beams < 1:
+        raise ValueError("logits: expected [groups * beams, vocab] on a GPU, got %s on %s" % (tuple(logits.shape), logits.device))
+    groups, dev = logits.shape[0] // beams, logits.device
+    with torch.cuda.device(dev):
+        out = {k: torch.empty((groups, width), dtype=torch.int32, device=dev)
+               for k, given in (("beam", True), ("token", True), ("length", length is not None), ("done", done is not None)) if given}
+        out["score"] = torch.empty((groups, width), device=dev)
+        d = make_beam_desc(logits, beams, width, score, out["score"], out["beam"], out["token"], length, out.get("length"), done, out.get("done"),
+                           end_token, length_power, parent, first, stride)
+        n = B.heisd_beam_select_workspace_bytes(groups, beams, width, logits.shape[1])
+        workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
+        rc = B.heisd_beam_select(d, workspace.data_ptr(), n, torch.cuda.current_stream(dev).cuda_stream)
+    if rc != 0:
+        raise RuntimeError("heisd_beam_select failed (%d): %s" % (rc, B.heisd_last_error(None)))
+    return out

@@ -323,6 +323,9 @@ def check_shared(c, groups, q, out, lse, cu_rows, k, v, scale, dtype, max_prefix
             nan = np.isnan(want)
             assert np.array_equal(np.isnan(out[r:r + 1]), nan), (i, r)
             tol = tolerance(dtype, 2.0 ** -11, 2.0 ** -36, q.shape[2], len(kk), want, mean, flat, size)
+            large = ~nan & (np.abs(want) > (65520 if dtype == "f16" else 2.0 ** 128))       # what the rows' type rounds to infinity (fp16 from 65520 on)
+            assert np.array_equal(out[r:r + 1][large], np.copysign(np.inf, want[large]))
+            nan |= large
             assert np.all((np.abs(out[r:r + 1] - want) <= tol)[~nan]), (i, r, np.nanmax(np.abs(out[r] - want)))
             fine = np.isfinite(wl)
             assert np.array_equal(lse[r:r + 1][~fine], wl[~fine], equal_nan=True)
@@ -427,8 +430,137 @@ def test_shared_attention_like_the_whole_contexts(P):
     q = randn(rng, (len(own), heads[0], hd), "bf16")
     g = ([members * i for i in range(groups + 1)], [len(own) + i for i in range(groups)])
     for scale in (0.125, -0.125, 0.0):
-        out, lse = shared(P, c, g, q, cu, 1, 30, 3, 90, scale)
-        check_shared(c, g, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), scale, "bf16", 90)
+        for max_seq, max_rows in ((30, 3), (30, 64), (4000, 64)):      # narrow; wide; wide with own tokens that may be cut
+            out, lse = shared(P, c, g, q, cu, 1, max_seq, max_rows, 90, scale)
+            check_shared(c, g, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), scale, "bf16", 90)
+
+
+WIDE = 1024      # a bound on the rows of a group that makes many columns of it
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("rows", [2, WIDE])
+def test_shared_attention_of_values_far_apart(P, dtype, head_dim, rows):
+    """Groups of values whose powers of two lie far apart, small ones beside zero, infinities and NaN, in prefixes of many rows: whatever the form is in which they
+    enter the products."""
+    rng = np.random.default_rng(head_dim)
+    total = [9, 5, 40, 40, 40, 40]
+    c = Cache(P, rng, total, 1, head_dim, 16)
+    at = np.concatenate([[0], np.cumsum(total)])
+    for case in range(6):
+        k, v = (randn(rng, (sum(total), 1, head_dim), "f32") for _ in range(2))
+        if case == 1:
+            v[at[2] + 3, 0, :32] *= 2.0 ** 35
+            v[at[3] + 20, 0, -20:] *= 2.0 ** -33
+        if case == 2:
+            v[at[2] + 3, 0, :32] *= 2.0 ** 90
+            v[at[2] + 8, 0, :32] *= 2.0 ** -90
+            k[at[3] + 7] *= 2.0 ** -50
+        if case == 3:
+            v[at[2]:at[3], 0, :32] = 0
+            v[at[3]:at[4]] *= 2.0 ** -110
+            k[at[2]:at[3], 0, 32:] = 0
+        if case == 4:
+            v[at[2] + 39, 0, 5] = math.inf
+            k[at[3] + 39, 0, 5] = math.nan
+        if case == 5:
+            k[at[2]:at[3]] = math.nan
+        c.pool.fill_(255)
+        c.write(P, k, v)
+        for groups in (([0, 1, 2], [2, 3]), ([0, 2], [4]), ([0, 2], [2])):
+            for cu in ([0, 2, 4, 4, 4, 4, 4], [0, 9, 14, 14, 14, 14, 14]):
+                q = randn(rng, (cu[-1], 5, head_dim), dtype)
+                out, lse = shared(P, c, groups, q, cu, 9, 40, rows, 40, 0.1)
+                check_shared(c, groups, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.1, dtype, 40)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("max_seq", [100, 3000])
+def test_shared_attention_with_other_bounds(P, dtype, max_seq):
+    """More rows than max_q and max_rows say, long tokens of their own, blocks that are missing, padded rows, requests left out; more columns than a workgroup has."""
+    rng = np.random.default_rng(max_seq)
+    total = [70, 100, 9, 0, 30, 2500 if max_seq > 100 else 60, 700, 90, 333]
+    new = [40, 3, 9, 0, 30, 2, 0, 20, 0]
+    c = Cache(P, rng, total, 2, 64, 16)
+    k, v = (randn(rng, (sum(total), 2, 64), "f32") for _ in range(2))
+    c.write(P, k, v)
+    gone = [np.zeros(2500, bool) for _ in total]
+    c.table[6, 3], c.table[6, 40], c.table[1, 0] = -1, c.n_blocks, -5
+    gone[6][48:64], gone[6][640:656], gone[1][:16] = True, True, True
+    seq = list(total)
+    seq[2] = -1
+    c.t_table, c.t_seq = i32(c.table), i32(seq)
+    cu = np.concatenate([[0], np.cumsum(new)]).tolist()
+    q = randn(rng, (cu[-1] + 3, 8, 64), dtype)
+    for groups in (([0, 6], [6]), ([0, 2, 5, 8], [6, 8, 6]), ([4, 6, 6], [0, 8])):
+        for max_q, max_rows in ((40, 200), (1, 16), (4, 1000)):
+            out, lse = shared(P, c, groups, q, cu, max_q, max_seq, max_rows, 700, -0.125)
+            check_shared(c, groups, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), -0.125, dtype, 700, seq=seq, gone=gone)
+            assert torch.all(out[cu[-1]:] == 7) and torch.all(lse[cu[-1]:] == 7)
+            again, _ = shared(P, c, groups, q, cu, max_q, max_seq, max_rows, 700, -0.125)
+            assert torch.equal(out, again)
+    for spans in ([0, -5, 90, 4, 2, 2 ** 31 - 1, 3, 9, 8, 7], [0, 50, 10, 20, 30, 31, 32, 33, 34, 35]):      # nothing read or written out of range
+        out, lse = shared(P, c, ([0, 6], [6]), q, spans, 40, max_seq, 200, 700, 0.125)
+        assert torch.all(out[50 if spans[1] == 50 else 9:] == 7)       # (request 0 has the rows 0 .. 49 in the second, 7 and 8 have none in either)
+
+
+def test_layouts(P):
+    """Queries and outputs in any order of rows and heads."""
+    rng = np.random.default_rng(21)
+    total = [9, 5, 40, 7, 130]
+    c = Cache(P, rng, total, 2, 128, 16)
+    k, v = (randn(rng, (sum(total), 2, 128), "bf16") for _ in range(2))
+    c.write(P, k, v)
+    cu, groups = [0, 2, 4, 10, 12, 12], ([0, 4], [4])
+    q = randn(rng, (12, 8, 128), "bf16")
+    for rows in (12, 100):
+        want, want_lse = shared(P, c, groups, q, cu, 6, 40, rows, 130, 0.1)
+        for make in (lambda t: t.transpose(0, 1).contiguous().transpose(0, 1), lambda t: torch.cat([t, t], 2)[..., :128], lambda t: torch.cat([t, t], 1)[:, 8:]):
+            x, o = make(q), make(torch.full_like(q, 7.0))
+            out, lse = shared(P, c, groups, x, cu, 6, 40, rows, 130, 0.1, out=o)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+            check_weigh(P, c, groups, x, lse, cu, 0.1, 0.5, ref.held(host(k)), 40, 130)
+
+
+def test_a_pool_past_32_bits(P):
+    """Blocks more than 4 GiB behind the pool's begin: attention, weights, eviction and copies."""
+    rng = np.random.default_rng(8)
+    total = [70, 60, 500]
+    c = Cache(P, rng, total, 8, 128, 64, spare=66000)
+    c.table[:, :9] = np.where(c.table[:, :9] >= 0, c.n_blocks - 1 - np.arange(27).reshape(3, 9), -1)
+    c.t_table = i32(c.table)
+    assert (c.n_blocks - 30) * 8 * 64 * 136 > 1 << 32
+    k, v = (randn(rng, (sum(total), 8, 128), "bf16") for _ in range(2))
+    c.write(P, k, v)
+    cu, groups = [0, 5, 9, 9], ([0, 2], [2])
+    q = randn(rng, (9, 16, 128), "bf16")
+    for rows in (9, 100):
+        out, lse = shared(P, c, groups, q, cu, 5, 70, rows, 500, 0.1)
+        check_shared(c, groups, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.1, "bf16", 500)
+    weight = torch.rand((c.n_blocks, 8, 64), device=DEV)
+    first, prefix = i32(groups[0]), i32(groups[1])
+    ok(P, P.heisd_kv4_weigh(c.desc, c.batch(P, cu, 9), P.make_prefix_groups(first, prefix, 9, 500), P.head_rows(q), lse.data_ptr(), 0.1, 0.0, weight.data_ptr(),
+                            weight.data_ptr(), 70, stream()))
+    slots = c.slots()[130:]
+    w = host(weight[i32(slots // 64).long(), :, i32(slots % 64).long()])
+    want, _ = branch.weights(host(q), ref.held(host(k))[130:], 0.1, host(lse), [500] * 9)
+    assert np.allclose(w, want, rtol=1e-4, atol=1e-30)
+    out_len = i32([-7] * 3)
+    t_keep = i32([-1, -1, 200])
+    ok(P, P.heisd_kv4_evict(c.desc, 1, 0, P.make_paged_batch(c.t_table, c.t_seq, None, 0), t_keep.data_ptr(), 50, weight.data_ptr(), weight.data_ptr(), out_len.data_ptr(),
+                            500, stream()))
+    c.t_seq, c.cu_seq = out_len, np.array([0, 70, 130, 330])
+    got = host(c.read(P)[0])
+    for h in range(8):
+        assert np.array_equal(got[130:, h], ref.held(host(k))[130 + np.array(branch.cut(w[:, h], 200, 50)), h])
+    t_from = i32([2, -1, -1])
+    c.table[0, :4] = np.arange(4)
+    c.t_table, c.t_seq = i32(c.table), i32([200, 60, 200])
+    ok(P, P.heisd_kv4_copy(c.desc, 1, 0, P.make_paged_batch(c.t_table, c.t_seq, None, 0), t_from.data_ptr(), weight.data_ptr(), 200, stream()))
+    c.cu_seq = np.array([0, 200, 260, 460])
+    k2, v2 = c.read(P)
+    assert torch.equal(k2[:200], k2[260:]) and torch.equal(v2[:200], v2[260:])
 
 
 # ---- weights of cached tokens -----------------------------------------------------------------------------------------------
@@ -600,12 +732,13 @@ def check_evict(P, rng, total, keep, recent, kv_heads, head_dim, block, layers, 
 
 @pytest.mark.parametrize("head_dim,block,kv_heads,layers", [(64, 16, 1, 1), (128, 64, 2, 2), (128, 16, 3, 1), (64, 128, 2, 2)])
 @pytest.mark.parametrize("in_place", [False, True])
-def test_evict(P, head_dim, block, kv_heads, layers, in_place):
+@pytest.mark.parametrize("max_seq", [1100, 8192, 16384, 1 << 20])           # keys held by 256 threads, by 1024, by twice as many each, read again
+def test_evict(P, head_dim, block, kv_heads, layers, in_place, max_seq):
     rng = np.random.default_rng(head_dim + block)
     total = [1, 5, 40, 200, 1100, 64, 0, 333, 90]
     for keep, recent in (([0, 2, 40, 100, 1000, 65, 0, 1, 0], 0), ([1, 4, 39, 199, 40, 63, -1, 300, 17], 16), ([0, 5, 20, 30, 600, 64, 3, 10, 89], 1000),
                          ([-1, 3, -1, 130, 1099, 32, 0, 332, 45], 33)):
-        check_evict(P, rng, total, keep, recent, kv_heads, head_dim, block, layers, in_place=in_place)
+        check_evict(P, rng, total, keep, recent, kv_heads, head_dim, block, layers, in_place=in_place, max_seq=max_seq)
 
 
 def test_evict_many(P):
@@ -614,6 +747,11 @@ def test_evict_many(P):
     total = [20000, 9001, 16384, 8192]
     for keep, recent in (([10000, 100, 16000, 8000], 64), ([1, 9000, 8192, 2049], 0), ([19999, 4500, 300, 8191], 5000)):
         check_evict(P, rng, total, keep, recent, 1, 64, 64, 1)
+    total = [16384, 8193, 8192, 15000]
+    for keep, recent in (([8192, 100, 8000, 14999], 64), ([1, 8192, 4096, 7500], 0), ([16383, 4500, 300, 2], 5000)):
+        check_evict(P, rng, total, keep, recent, 1, 64, 64, 1, max_seq=16384)
+    for keep, recent in (([4096, 100, 8000, 8191], 64), ([1, 8000, 4097, 7500], 0), ([8191, 4500, 300, 2], 5000)):
+        check_evict(P, rng, [8192, 8001, 8192, 8192], keep, recent, 2, 128, 32, 1, max_seq=8192, in_place=True)
 
 
 def test_evict_of_weights_that_are_equal_or_not_numbers(P):
@@ -624,7 +762,8 @@ def test_evict_of_weights_that_are_equal_or_not_numbers(P):
         return lambda shape: np.asarray(values)[rng.integers(0, len(values), shape)]
     for values in ([0.0], [0.0, -0.0], [1.0, 2.0], [math.nan], [math.nan, 0.0, 1.0], [-math.inf, math.inf, 3.0, -2.0], [1e-45, 0.0, -1e-45]):
         for in_place in (False, True):
-            check_evict(P, rng, total, keep, 7, 2, 64, 16, 1, make=some(values), in_place=in_place)
+            for max_seq in (2500, 1 << 20):
+                check_evict(P, rng, total, keep, 7, 2, 64, 16, 1, make=some(values), in_place=in_place, max_seq=max_seq)
 
 
 def test_evict_leaves_others_as_they_are(P):
