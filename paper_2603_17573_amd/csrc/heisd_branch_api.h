@@ -148,13 +148,12 @@ static int groups_desc_ok(const char *who, const heisd_prefix_groups *g, PrefixG
   return HEISD_OK;
 }
 
-// As Kv4Plan, with the groups' work beside the requests'.  Groups of many columns are kv4_prefix's, and then a request's own tokens are not cut where that
-// leaves enough workgroups.
-constexpr int64_t kWideLeast = 64, kWideMany = 192, kWholeTokens = 1024;
+// As Kv4Plan, with the groups' work beside the requests'.  Groups of many columns are kv4_prefix's.  Where the requests' own tokens are few, nothing of them is cut, and a
+// workgroup knows by its number what it has to do (`direct`): prefixes are cut into a power of two of runs then, so that there are kSplitGroups workgroups for them.
+constexpr int64_t kWideLeast = 64, kWideMany = 192, kWholeTokens = 1024, kSplitGroups = 512, kSplitTokens = 4096;
 struct SharedPlan {
-  int col_tiles, unit, wide_waves, own_tiles;
-  int64_t groups, wide;
-  bool joins;
+  int col_tiles, unit, wide_waves, direct, split_shift;
+  int64_t groups, wide, tiles, depth;
   size_t part_ml, whole, whole_ml, wide_part, wide_ml, book, group_of, total;
   SharedPlan(int64_t batch, int64_t rows, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, const PrefixGroups &p, int64_t head_dim) {
     const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::min<int64_t>(std::min<int64_t>(p.max_rows, rows) * group, 1 << 22);
@@ -164,18 +163,21 @@ struct SharedPlan {
                ? std::min<int64_t>(p.groups * kv_heads * ((cols + wide_cols - 1) / wide_cols) * ((p.max_prefix + 255) / 256), 8 / wide_waves * kKv4Units) : 0;
     col_tiles = !wide && std::max(own_cols, cols) > 16 ? 2 : 1;
     const int64_t tile = 16 * col_tiles, most = kv4_per_unit((int)head_dim, col_tiles) * kKv4Units;
-    const int64_t segments = batch * std::min<int64_t>(kv_heads * ((own_cols + tile - 1) / tile), 65535);
-    unit = wide && max_seq <= kWholeTokens ? kWholeTokens : kKv4Unit;
-    const int64_t own = segments * ((max_seq + unit - 1) / unit);
-    const int64_t shared = wide ? 0 : (int64_t)p.groups * std::min<int64_t>(kv_heads * ((cols + tile - 1) / tile), 65535) * ((p.max_prefix + kKv4Unit - 1) / kKv4Unit);
-    joins = !wide || unit == kKv4Unit || own > kMostGroups || kv_heads * ((own_cols + tile - 1) / tile) > 65535;
-    if (joins) unit = kKv4Unit;
-    own_tiles = joins ? 0 : (int)(segments / batch / kv_heads);
-    groups = joins ? std::max<int64_t>(1, std::min<int64_t>((own + shared + 1) / 2, most)) : own;
+    const int64_t own_tiles = (own_cols + tile - 1) / tile, group_tiles = wide ? 0 : (cols + tile - 1) / tile;
+    tiles = std::max<int64_t>(own_tiles, group_tiles);
+    for (split_shift = 0; !wide && p.groups && (1 << split_shift) < kSplitsMost && ((int64_t)p.groups * kv_heads * group_tiles << split_shift) < kSplitGroups &&
+                          (kKv4Unit << split_shift) < p.max_prefix;) ++split_shift;
+    depth = batch + (wide ? 0 : (int64_t)p.groups << split_shift);
+    direct = max_seq <= kWholeTokens && (wide || p.max_prefix <= kSplitTokens << split_shift) && tiles <= 65535 && depth <= 65535;
+    unit = direct ? kWholeTokens : kKv4Unit;
+    const int64_t own = batch * std::min<int64_t>(kv_heads * own_tiles, 65535) * ((max_seq + unit - 1) / unit);
+    const int64_t shared = wide ? 0 : (int64_t)p.groups * std::min<int64_t>(kv_heads * group_tiles, 65535) * ((p.max_prefix + kKv4Unit - 1) / kKv4Unit);
+    groups = direct ? 0 : std::max<int64_t>(1, std::min<int64_t>((own + shared + 1) / 2, most));
     part_ml = align256((size_t)2 * groups * tile * head_dim * sizeof(float));
     whole = part_ml + align256((size_t)2 * groups * tile * 2 * sizeof(float));
-    whole_ml = whole + align256((size_t)2 * rows * group * kv_heads * head_dim * sizeof(float));
-    wide_part = whole_ml + align256((size_t)2 * rows * group * kv_heads * 2 * sizeof(float));
+    const size_t parts = 1 + (direct && !wide ? (size_t)1 << split_shift : 1);      // by row: own tokens, the prefix or its runs
+    whole_ml = whole + align256(parts * rows * group * kv_heads * head_dim * sizeof(float));
+    wide_part = whole_ml + align256(parts * rows * group * kv_heads * 2 * sizeof(float));
     wide_ml = wide_part + align256((size_t)2 * wide * wide_cols * head_dim * sizeof(float));
     book = wide_ml + align256((size_t)2 * wide * wide_cols * 2 * sizeof(float));
     group_of = book + align256(wide ? p.groups * sizeof(WideBook) : 0);
@@ -216,16 +218,18 @@ static hipError_t kv4_shared_launch(const Kv4Cache &c, const PagedBatch &b, cons
                               const SharedPlan &plan, int max_q, hipStream_t st) {
   const HeadRows<T> qi = head_rows<T>(*q), o = head_rows<T>(*out);
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
-  const dim3 block(256), grid = plan.own_tiles ? dim3(c.kv_heads, plan.own_tiles, b.batch) : dim3((unsigned)plan.groups);
+  const dim3 block(256), grid = plan.direct ? dim3(c.kv_heads, (unsigned)plan.tiles, (unsigned)plan.depth) : dim3((unsigned)plan.groups);
   if (plan.wide) {
     const hipError_t e = plan.wide_waves == 8 ? kv4_prefix_launch<T, HD, 8>(c, b, qc, a, st) : kv4_prefix_launch<T, HD, 4>(c, b, qc, a, st);
     if (e != hipSuccess) return e;
   }
   if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
   else kv4_attend<T, HD, 1, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
-  if (!plan.joins) return hipSuccess;
+  if (plan.direct && plan.wide) return hipSuccess;
   const int64_t per = 256 / (HD / 4), cols = std::min<int64_t>((int64_t)max_q * a.q_heads, (int64_t)b.rows * a.q_heads);
-  kv4_shared_join<T, HD><<<dim3((unsigned)std::min<int64_t>((cols + per - 1) / per, 65535), b.batch), block, 0, st>>>(c, b, o, a, (int)plan.groups);
+  const dim3 joins((unsigned)std::min<int64_t>((cols + per - 1) / per, 65535), b.batch);
+  if (plan.direct) kv4_direct_join<T, HD><<<joins, block, 0, st>>>(c, b, o, a);
+  else kv4_shared_join<T, HD><<<joins, block, 0, st>>>(c, b, o, a, (int)plan.groups);
   return hipSuccess;
 }
 
@@ -263,7 +267,8 @@ extern "C" int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const hei
   a.group_shift = (a.group & (a.group - 1)) ? -1 : __builtin_ctz(a.group);
   a.wide = (int)plan.wide;
   a.wide_shift = __builtin_ctz(32 * plan.wide_waves);
-  a.own_tiles = plan.own_tiles;
+  a.direct = plan.direct;
+  a.split_shift = plan.split_shift;
   a.wide_part = reinterpret_cast<float *>(ws + plan.wide_part);
   a.wide_ml = reinterpret_cast<float *>(ws + plan.wide_ml);
   a.book = reinterpret_cast<WideBook *>(ws + plan.book);

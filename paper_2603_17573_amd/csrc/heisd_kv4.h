@@ -349,7 +349,8 @@ struct Kv4SharedAttend : Kv4Attend {
   PrefixGroups prefix;
   int unit_shift, cols_shift, group_shift;          // powers of two: tokens of a unit of own work, columns; the group, where it is one (else -1)
   int wide, wide_shift;                             // workgroups of kv4_prefix, columns that one takes at a time (a power of two)
-  int own_tiles;                                    // not 0: the grid is key heads, so many tiles of columns (where max_q does not hold, more of them one after the other), requests
+  int direct;                                       // the grid is key heads, tiles of columns (more of them, one after the other, where max_q or max_rows do not hold), requests ...
+  int split_shift;                                  // ... and, narrow, groups times a power of two of runs of their prefix's tokens
   float *whole, *whole_ml, *wide_part, *wide_ml;
   WideBook *book;                                   // [groups], written by kv4_prefix
   int32_t *group_at;                                // [batch], so is this: a request's group (-1: none with a prefix)
@@ -358,8 +359,6 @@ __device__ __forceinline__ constexpr int kv4_unit(const Kv4Attend &) { return kK
 __device__ __forceinline__ int kv4_unit(const Kv4SharedAttend &a) { return 1 << a.unit_shift; }
 __device__ __forceinline__ int kv4_row(const Kv4Attend &a, int column) { return column / a.group; }
 __device__ __forceinline__ int kv4_row(const Kv4SharedAttend &a, int column) { return a.group_shift >= 0 ? column >> a.group_shift : column / a.group; }
-__device__ __forceinline__ constexpr int kv4_own_tiles(const Kv4Attend &) { return 0; }
-__device__ __forceinline__ int kv4_own_tiles(const Kv4SharedAttend &a) { return a.own_tiles; }
 __device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4Attend &) { return b.batch; }
 __device__ __forceinline__ int kv4_requests(const PagedBatch &b, const Kv4SharedAttend &a) { return a.wide ? b.batch : b.batch + a.prefix.groups; }
 __device__ __forceinline__ Kv4Request kv4_request(const Kv4Cache &c, const PagedBatch &b, const Kv4SharedAttend &a, int i) {
@@ -381,6 +380,9 @@ __device__ __forceinline__ Kv4Request wide_request(const Kv4Cache &c, const Page
   r.work = (long long)r.units * (((r.rows.count * a.group + (1 << a.wide_shift) - 1) >> a.wide_shift) * c.kv_heads);
   return r;
 }
+
+// Tokens of a run of a prefix that is cut into a power of two of them: whole units.
+__device__ __forceinline__ int kv4_split(int tokens, int shift) { return (((tokens - 1) >> shift) + kKv4Unit) & ~(kKv4Unit - 1); }
 
 // Which group request i belongs to (-1: none).  Groups that are described follow each other, so at most one does.
 __device__ __forceinline__ int group_of(const PrefixGroups &p, int i) {
@@ -495,7 +497,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     s_req[wave][lane] = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
   };
   bool direct = false;
-  if constexpr (SHARED) direct = a.own_tiles != 0;
+  if constexpr (SHARED) direct = a.direct != 0;
   if (!direct) requests(0);
   else end = 1ll << 62;
   long long all = end;
@@ -508,12 +510,15 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       requests(end);
     }
     if (at >= end) break;                                       // not reached while the lengths stay as they are
-    int local = 0, req;
+    int local = 0, req, split = 0;
     int4 rq;
     if (SHARED && direct) {
       req = blockIdx.z;
+      if constexpr (SHARED)
+        if (req >= b.batch) split = (req - b.batch) & ((1 << a.split_shift) - 1), req = b.batch + ((req - b.batch) >> a.split_shift);
+      req = __builtin_amdgcn_readfirstlane(req);
       const Kv4Request r = kv4_request(c, b, a, req);
-      rq = make_int4(r.rows.begin, r.rows.count, r.seq, r.units);
+      rq = make_int4(r.rows.begin, r.rows.count, r.seq, 1);
     } else {
       local = 63 - __clzll(__ballot(s_start[wave][lane] <= at));             // the last of those that begin here has the work
       req = first + local;
@@ -525,16 +530,26 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     const int segment = direct ? 0 : __builtin_amdgcn_readfirstlane((int)wave_div(in_req, units));
     const int u0 = direct ? 0 : __builtin_amdgcn_readfirstlane((int)(in_req - (long long)segment * units));
     const int u1 = direct ? 1 : __builtin_amdgcn_readfirstlane((int)min((long long)units, u0 + (run1 - at)));
-    const int tile = __builtin_amdgcn_readfirstlane(direct ? (int)blockIdx.y + (int)at * kv4_own_tiles(a) : segment / c.kv_heads);
+    const int tile = __builtin_amdgcn_readfirstlane(direct ? (int)(blockIdx.y + at * gridDim.y) : segment / c.kv_heads);
     const int head = __builtin_amdgcn_readfirstlane(direct ? (int)blockIdx.x : segment - tile * c.kv_heads), col0 = tile * (16 * CT);
     const bool whole = u0 == 0 && u1 == units;
     const long long slot = 2 * (long long)blockIdx.x + (at != run0);
     const int n_cols = rows.count * a.group;
     if (SHARED && direct && col0 >= n_cols) break;
-    const int unit = kv4_unit(a), t1 = (int)min((long long)seq, (long long)u1 * unit);
+    const int unit = kv4_unit(a);
+    int t_first = u0 * unit, t1 = (int)min((long long)seq, (long long)u1 * unit);
     int owner = req, few = seq - rows.count + 1;                  // whose blocks; tokens that every row sees
     if constexpr (SHARED)
-      if (req >= b.batch) owner = __builtin_amdgcn_readfirstlane(a.prefix.prefix[req - b.batch]), few = seq;
+      if (req >= b.batch) {
+        owner = __builtin_amdgcn_readfirstlane(a.prefix.prefix[req - b.batch]), few = seq;
+        if (direct) {
+          const int run = kv4_split(seq, a.split_shift);
+          t_first = split * run;
+          t1 = min(seq, t_first + run);
+          if (t_first >= t1) break;
+        }
+      }
+    if constexpr (SHARED) t_first = __builtin_amdgcn_readfirstlane(t_first), t1 = __builtin_amdgcn_readfirstlane(t1);
     const int32_t *table = b.table + (long long)owner * b.max_blocks;
 
     [[maybe_unused]] Kv4Parts prefix{};                         // wide: of this request's prefix
@@ -742,7 +757,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
       }
       __builtin_amdgcn_sched_barrier(0);
     };
-    for (t0 = u0 * unit; t0 < t1; t0 += 32 * kKv4Unit) {
+    for (t0 = t_first; t0 < t1; t0 += 32 * kKv4Unit) {
       // the blocks of the wave's tiles: lane 2 i + n holds that of tile n of its i-th pair of these 32
       const int t = t0 + 32 * (wave + 4 * (lane >> 1)) + 16 * (lane & 1);
       my_id = t < t1 ? table[t >> c.block_shift] : -1;
@@ -764,7 +779,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     // what is not finite makes NaN of the columns that do see it (rare: the exponents of all of the wave's tokens are read again)
     uint32_t nan_out = 0;                                       // bit ct: the lane's column of tile ct, in the lane's channels
     if (__ballot(odd)) {
-      for (int t = u0 * unit; t < t1; ++t) {
+      for (int t = t_first; t < t1; ++t) {
         if ((t / 32 - wave) % 4) continue;
         const int id = table[t >> c.block_shift], o = t & (bs - 1);
         if (id < 0 || id >= c.n_blocks) continue;
@@ -810,7 +825,7 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
         const long long r = rows.begin + i;
         float *lse = a.lse && d == 0 ? a.lse + r * a.q_heads + h : nullptr;
         if constexpr (SHARED) {
-          const long long at_row = ((long long)(a.wide || req >= b.batch) * b.rows + r) * a.q_heads + h;      // own tokens first, then prefixes
+          const long long at_row = ((long long)(req >= b.batch ? 1 + split : a.wide != 0) * b.rows + r) * a.q_heads + h;      // own tokens first, then prefixes
           if (whole && a.wide) {
             prefix.add<HD, V>(s, s_place[ct * 16 + n], d, a.whole + at_row * HD, a.whole_ml + at_row * 2);
             s.store(out.at(r, h) + d, lse);

@@ -440,6 +440,41 @@ __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b,
   }
 }
 
+// The same where every segment is whole: own tokens, and the runs of the prefix, all kept by row.
+constexpr int kSplitsMost = 32;
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void kv4_direct_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4SharedAttend a) {
+  constexpr int PER = 256 / (HD / 4), K = 8;
+  const int req = blockIdx.y;
+  const Span rows = wave_span(b.cu_rows, req, b.rows);
+  const int n_cols = rows.count * a.q_heads;
+  if ((long long)blockIdx.x * PER >= n_cols) return;
+  const int g = group_of(a.prefix, req);
+  PrefixSpan span{{0, 0}, -1, 0};
+  if (g >= 0 && kv4_live(c, b, a, req)) span = prefix_span(c, b, a.prefix, g);
+  const int run = span.tokens ? kv4_split(span.tokens, a.split_shift) : 1, runs = (span.tokens + run - 1) / run;
+  for (int u = blockIdx.x * PER + threadIdx.x / (HD / 4); u < n_cols; u += gridDim.x * PER) {
+    const int d = threadIdx.x % (HD / 4) * 4;
+    const long long first = (long long)rows.begin * a.q_heads, at = first + u, apart = (long long)b.rows * a.q_heads;
+    const int i = u / a.q_heads, h = u - i * a.q_heads, in_group = rows.begin + i - span.rows.begin;
+    const int parts = 1 + (in_group >= 0 && in_group < span.rows.count ? runs : 0);      // own tokens first
+    Kv4Sums<1> s;
+    for (int p = 0; p < parts; p += K) {
+      float2 ml[K];
+      f32x4 x[K][1];
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const long long from = at + min(p + k, parts - 1) * apart;
+        ml[k] = *reinterpret_cast<const float2 *>(a.whole_ml + from * 2);
+        x[k][0] = *reinterpret_cast<const f32x4 *>(a.whole + from * HD + d);
+        if (p + k >= parts) ml[k] = make_float2(-INFINITY, 0.f);
+      }
+      s.add(ml, x);
+    }
+    s.store(out.at(rows.begin + i, h) + d, a.lse && d == 0 ? a.lse + at : nullptr);
+  }
+}
+
 // ---- positions -----------------------------------------------------------------------------------------------------------
 
 // Rows of a request whose cached tokens begin later than at 0 (behind a shared prefix, after an eviction): a wave finds the requests of its first row, a
