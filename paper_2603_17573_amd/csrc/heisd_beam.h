@@ -329,7 +329,7 @@ __device__ __forceinline__ void reorder_row(const ReorderArgs &a, int b, int lan
 // The books, on one workgroup: who takes its parent's blocks over, what goes back to the free ones, who takes how many of them.  Between the
 // passes owned_out holds who goes on in a request's blocks (-1: itself, else the lowest), and the first entry of a row of table_out where its blocks
 // are: -1 - parent for those that take them over, else the place of its first one among the free ones.  Everything is a function of the inputs (the
-// minimum does not depend on the order of the atomics).  TABLES: the rows of the table too; otherwise reorder_tables writes them.
+// minimum does not depend on the order of the atomics).  TABLES: the rows of the table too, of no more requests than threads; otherwise reorder_tables writes them.
 template <int W, bool TABLES>
 __global__ __launch_bounds__(W * 64) void reorder_books(ReorderArgs a) {
   constexpr int N = W * 64, kNobody = 0x7FFFFFFF;
@@ -405,11 +405,15 @@ __global__ __launch_bounds__(W * 64) void reorder_books(ReorderArgs a) {
     const int owned = at < 0 ? reorder_kept(a, min(max(a.owned_in[-1 - at], 0), a.max_blocks), a.len_in[-1 - at])
                              : a.copy_from[b] < 0 ? 0 : reorder_blocks(a, a.len_out[b]);
     a.owned_out[b] = owned;
+    if (TABLES) lengths[b] = at, skip[b] = owned;
   }
   if (!TABLES) return;
   __threadfence();
   __syncthreads();
-  for (int b = tid >> 6; b < a.batch; b += W) reorder_row(a, b, tid & 63);
+  for (int n = tid; n < a.batch * a.max_blocks; n += N) {
+    const int b = n / a.max_blocks, j = n - b * a.max_blocks, at = lengths[b];
+    a.table_out[n] = j >= skip[b] ? -1 : at < 0 ? a.table_in[(long long)(-1 - at) * a.max_blocks + j] : a.free_ids[at - j];
+  }
 }
 
 __global__ __launch_bounds__(256) void reorder_tables(ReorderArgs a) {

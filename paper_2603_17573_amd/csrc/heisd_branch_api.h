@@ -95,7 +95,9 @@ extern "C" int heisd_paged_reorder(const heisd_reorder_desc *d, void *stream) {
                       d->owned_out, d->table_out, d->copy_from, d->free_ids, d->free_count_in, d->free_count_out};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (d->batch <= 64 && (int64_t)d->batch * d->max_blocks <= 4096) reorder_books<4, true><<<dim3(1), dim3(256), 0, st>>>(a);
+  const int64_t entries = (int64_t)d->batch * d->max_blocks;
+  if (d->batch <= 64 && entries <= 1024) reorder_books<1, true><<<dim3(1), dim3(64), 0, st>>>(a);
+  else if (d->batch <= 256 && entries <= 8192) reorder_books<4, true><<<dim3(1), dim3(256), 0, st>>>(a);
   else {
     if (d->batch <= 256) reorder_books<4, false><<<dim3(1), dim3(256), 0, st>>>(a);
     else reorder_books<16, false><<<dim3(1), dim3(1024), 0, st>>>(a);
@@ -161,8 +163,8 @@ struct SharedPlan {
     const int64_t wide_cols = 32 * wide_waves;
     wide = p.groups && cols >= kWideLeast
                ? std::min<int64_t>(p.groups * kv_heads * ((cols + wide_cols - 1) / wide_cols) * ((p.max_prefix + 255) / 256), 8 / wide_waves * kKv4Units) : 0;
-    col_tiles = !wide && std::max(own_cols, cols) > 16 ? 2 : 1;
-    const int64_t tile = 16 * col_tiles, most = kv4_per_unit((int)head_dim, col_tiles) * kKv4Units;
+    col_tiles = (wide ? own_cols : std::max(own_cols, cols)) > 16 ? 2 : 1;
+    const int64_t tile = 16 * col_tiles, most = kv4_shared_per_unit(col_tiles) * kKv4Units;
     const int64_t own_tiles = (own_cols + tile - 1) / tile, group_tiles = wide ? 0 : (cols + tile - 1) / tile;
     tiles = std::max<int64_t>(own_tiles, group_tiles);
     for (split_shift = 0; !wide && p.groups && (1 << split_shift) < kSplitsMost && ((int64_t)p.groups * kv_heads * group_tiles << split_shift) < kSplitGroups &&
@@ -223,8 +225,8 @@ static hipError_t kv4_shared_launch(const Kv4Cache &c, const PagedBatch &b, cons
     const hipError_t e = plan.wide_waves == 8 ? kv4_prefix_launch<T, HD, 8>(c, b, qc, a, st) : kv4_prefix_launch<T, HD, 4>(c, b, qc, a, st);
     if (e != hipSuccess) return e;
   }
-  if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
-  else kv4_attend<T, HD, 1, TERMS, Kv4SharedAttend><<<grid, block, 0, st>>>(c, b, qc, o, a);
+  if (plan.col_tiles == 2) kv4_shared<T, HD, 2, TERMS><<<grid, block, 0, st>>>(c, b, qc, o, a);
+  else kv4_shared<T, HD, 1, TERMS><<<grid, block, 0, st>>>(c, b, qc, o, a);
   if (plan.direct && plan.wide) return hipSuccess;
   const int64_t per = 256 / (HD / 4), cols = std::min<int64_t>((int64_t)max_q * a.q_heads, (int64_t)b.rows * a.q_heads);
   const dim3 joins((unsigned)std::min<int64_t>((cols + per - 1) / per, 65535), b.batch);

@@ -252,6 +252,7 @@ constexpr int kKv4Unit = 128;
 // Workgroups of 256 threads that the registers of a compute unit hold: two column tiles need more of them, heads of 64 fewer.  Queries of two terms
 // fit as those of one do.
 __host__ __device__ constexpr int kv4_per_unit(int head_dim, int col_tiles) { return col_tiles == 2 ? 2 : head_dim == 64 ? 4 : 3; }
+__host__ __device__ constexpr int kv4_shared_per_unit(int col_tiles) { return col_tiles == 2 ? 2 : 3; }
 
 // What a request asks for: its rows, its tokens, units per segment, units in all.
 struct Kv4Request {
@@ -462,8 +463,9 @@ __device__ __forceinline__ bool kv4_live(const Kv4Cache &c, const PagedBatch &b,
 // shares with others goes to kv4_join.  A probability enters as a bf16 and a bf16 remainder: one bf16 alone (off by up to 2^-8, and with few
 // large probabilities nothing averages that out) made the results of single tokens 1.4 times as inexact as their own rounding does, for 3 % of the
 // time (59.9 against 62.1 us with 64 contexts of 256 to 8191 tokens).  TERMS 2: so do the queries (fp16 rows, whose 11 bits a bf16 does not hold).
+// A: Kv4Attend (kv4_attend) or Kv4SharedAttend (kv4_attend's work with shared prefixes: kv4_shared).
 template <typename T, int HD, int CT, int TERMS, typename A>
-__global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, A a) {
+__device__ __forceinline__ void attend_cached(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, A a) {
   constexpr bool SHARED = std::is_same_v<A, Kv4SharedAttend>;
   constexpr int W = HD / 32, ND = HD / 16, KJ = HD / 32;        // code dwords, tiles of channels, products per score tile
   constexpr int LD = HD + 4;
@@ -848,6 +850,15 @@ __global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache
     }
     at += u1 - u0;
   }
+}
+
+template <typename T, int HD, int CT, int TERMS>
+__global__ __launch_bounds__(256, kv4_per_unit(HD, CT)) void kv4_attend(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4Attend a) {
+  attend_cached<T, HD, CT, TERMS>(c, b, q, out, a);
+}
+template <typename T, int HD, int CT, int TERMS>
+__global__ __launch_bounds__(256, kv4_shared_per_unit(CT)) void kv4_shared(Kv4Cache c, PagedBatch b, HeadRows<const T> q, HeadRows<T> out, Kv4SharedAttend a) {
+  attend_cached<T, HD, CT, TERMS>(c, b, q, out, a);
 }
 
 // Joins the parts of segments that several workgroups worked on, in the order of their tokens.  A workgroup per segment; 16 bytes of

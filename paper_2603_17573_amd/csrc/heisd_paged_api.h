@@ -353,8 +353,8 @@ static void kv4_attention_launch(const Kv4Cache &c, const PagedBatch &b, const h
   const HeadRows<const T> qc{qi.p, qi.rs, qi.hs};
   const dim3 block(256);
   const int groups = plan.groups(HD);
-  if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS, Kv4Attend><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
-  else kv4_attend<T, HD, 1, TERMS, Kv4Attend><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
+  if (plan.col_tiles == 2) kv4_attend<T, HD, 2, TERMS><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
+  else kv4_attend<T, HD, 1, TERMS><<<dim3(groups), block, 0, st>>>(c, b, qc, o, a);
   if (groups > 1) kv4_join<T, HD><<<dim3(plan.segments, b.batch), block, 0, st>>>(c, b, o, a, groups);
 }
 

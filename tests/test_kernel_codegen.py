@@ -181,3 +181,10 @@ def test_paged_kernels_use_no_scratch(device_asm):
             seen += 1
             assert int(re.search(r"\.amdhsa_private_segment_fixed_size\s+(\d+)", block).group(1)) == 0, name
     assert seen == 8 + 4 + 12 + 12 + 16 + 12 + 5 + 1, seen
+
+
+def test_shared_attention_uses_no_scratch(device_asm):
+    """kv4_shared counts its transfers as kv4_attend does."""
+    sizes = [int(re.search(r"\.amdhsa_private_segment_fixed_size\s+(\d+)", m.group(2)).group(1))
+             for m in re.finditer(r"\.amdhsa_kernel (\S+)(.*?)\.end_amdhsa_kernel", device_asm, flags=re.S) if re.search(r"heisd\d+kv4_sharedI", m.group(1))]
+    assert sizes == [0] * 8, sizes
