@@ -158,7 +158,7 @@ struct SharedPlan {
   int64_t groups, wide, tiles, depth;
   size_t part_ml, whole, whole_ml, wide_part, wide_ml, book, group_of, total;
   SharedPlan(int64_t batch, int64_t rows, int64_t kv_heads, int64_t group, int64_t max_q, int64_t max_seq, const PrefixGroups &p, int64_t head_dim) {
-    const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::min<int64_t>(std::min<int64_t>(p.max_rows, rows) * group, 1 << 22);
+    const int64_t own_cols = std::min<int64_t>(max_q * group, 1 << 22), cols = std::min<int64_t>(p.max_rows * group, 1 << 22);
     wide_waves = cols >= kWideMany ? 8 : 4;
     const int64_t wide_cols = 32 * wide_waves;
     wide = p.groups && cols >= kWideLeast

@@ -266,3 +266,34 @@ def test_steps_without_rows(P):
     assert c.fork(i32([-1, 7, -9]), i32([0, 0, 0])).tolist() == [-1, -1, -1]
     c.begin(i32([-1, -1, -1]), i32([0, 0, 0]), 0)
     assert c.attend_shared(0, q).shape == q.shape and int(c.free_count) == 30
+
+
+def test_steps_of_any_number_of_rows(P):
+    """The workspace is made for the largest step; smaller ones are cut otherwise and fit it, whatever the bounds are."""
+    rng = np.random.default_rng(4)
+    for max_own in (60, 1500):
+        for max_rows in (1, 9, 40, 4000):
+            c = P.PagedCache(1, 8, 2, 64, 9, 1500, 400, n_blocks=400, block_size=16, max_new=40)
+            c.share(i32([0, 8]), i32([8]), max_rows, max_own=max_own)
+            size = P.heisd_kv4_shared_attention_workspace_bytes
+            most = c._shared[2].numel()
+            for n in (0, 1, 2, 7, 8, 15, 16, 17, 64, 399, 400):
+                assert size(c.descs[0], 9, n, 8, 40, max_own, c._shared[0]) <= most
+    cached, new = [0] * 8 + [0], [0] * 8 + [300]
+    c.begin(i32(cached), i32(new), 300)
+    k, v = (randn(rng, (300, 2, 64), "bf16") for _ in range(2))
+    c.append(0, k, v)
+    rows = [[] for _ in range(8)]
+    for n in (1, 40, 3, 1):
+        c.begin(i32([len(r) for r in rows] + [300]), i32([n] * 8 + [0]), 8 * n)
+        q, k2, v2 = (randn(rng, (8 * n, h, 64), "bf16") for h in (8, 2, 2))
+        c.append(0, k2, v2)
+        out = host(c.attend_shared(0, q))
+        hk, hv = ref.held(host(k2)), ref.held(host(v2))
+        for i in range(8):
+            rows[i] += list(zip(hk[i * n:(i + 1) * n], hv[i * n:(i + 1) * n]))
+            kk, vv = (np.concatenate([ref.held(host(x)), np.stack([r[j] for r in rows[i]])]) for j, x in ((0, k), (1, v)))
+            seen = [len(kk) - n + j + 1 for j in range(n)]
+            want, _, mean, flat, size = ref.attention(host(q)[i * n:(i + 1) * n], kk, vv, seen, 0.125)
+            assert np.all(np.abs(out[i * n:(i + 1) * n] - want) <= tolerance("bf16", 2.0 ** -11, 2.0 ** -36, 64, len(kk), want, mean, flat, size))
+
