@@ -4,7 +4,8 @@
 // ---- the next beams --------------------------------------------------------------------------------------------------
 
 constexpr int kBeamMostVocab = (1 << 19) - 8;       // as many segments as beam_pick's lanes hold; a row's address may cut its first and last
-constexpr int kBeamDirectVocab = 4096;              // up to here one launch does
+constexpr int kBeamDirectVocab = 4096;              // up to here one launch does.  us, one / two: four beams over 256 logits 8.8 / 12.7, 4000 10.4 / 12.6,
+                                                    // 8000 15.0 / 13.3; 64 beams over 1000 11.2 / 14.6, 4000 12.3 / 13.9, 8000 15.6 / 13.8
 
 static int beam_sizes_ok(const char *who, int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
   if (groups < 1 || groups > 65535 || beams < 1 || beams > kBeamMost || width < 1 || width > kBeamMost || vocab < 1 || vocab > kBeamMostVocab)
@@ -151,7 +152,11 @@ static int groups_desc_ok(const char *who, const heisd_prefix_groups *g, PrefixG
 }
 
 // As Kv4Plan, with the groups' work beside the requests'.  Groups of many columns are kv4_prefix's.  Where the requests' own tokens are few, nothing of them is cut, and a
-// workgroup knows by its number what it has to do (`direct`): prefixes are cut into a power of two of runs then, so that there are kSplitGroups workgroups for them.
+// workgroup knows by its number what it has to do (`direct`): prefixes are cut into a power of two of runs then, so that there are kSplitGroups workgroups for them
+// (four requests behind 95 tokens: 12.8 us in two kernels, 18.8 as runs).
+// us a call, narrow / wide, 4 query heads per key head, 8 key heads of 128, prefixes of up to 8191 tokens: eight groups of 64 columns 70.8 / 62.2, of 96 84.8 / 65.9, of 128
+// 183.9 / 84.0, of 192 236 / 109; two of 64 32.9 / 37.4; one of 128 35.4 / 35.9, of 256 63.4 / 42.5.  Waves of a wide workgroup, four / eight: 64 columns 62.2 / 59.7, 128 84.0 /
+// 80.8, heads of 64 45.1 / 49.9 and 63.4 / 67.8; 1792 columns, the prefixes' kernel alone, 108 / 87.
 constexpr int64_t kWideLeast = 64, kWideMany = 192, kWholeTokens = 1024, kSplitGroups = 512, kSplitTokens = 4096;
 struct SharedPlan {
   int col_tiles, unit, wide_waves, direct, split_shift;
@@ -323,7 +328,8 @@ extern "C" int heisd_kv4_weigh(const heisd_kv4_desc *cache, const heisd_paged_ba
   if ((!lse && b.rows > 0) || !weight_in || !weight_out || !std::isfinite(scale) || !std::isfinite(decay))
     return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer, scale %g or decay %g", who, scale, decay);
   const WeighArgs a{scale * 1.4426950408889634f, decay, q->heads / c.kv_heads, q->heads, max_seq, lse, weight_in, weight_out};
-  // As many pairs per wave as leave some workgroups per compute unit, counted with the largest lengths.
+  // As many pairs per wave as leave some workgroups per compute unit, counted with the largest lengths (kWeighFill 8192 / 4096 / 2048 / 1024: 38.9 / 35.8 / 53.6 / 74.1 us
+  // with 64 contexts of up to 7847 tokens).
   const int64_t units = ((int64_t)std::max(max_seq, p.max_prefix) + kWeighUnit - 1) / kWeighUnit;
   const int pairs = (int)std::max<int64_t>(1, std::min<int64_t>(kWeighPairs, units * c.kv_heads * b.batch / kWeighFill));
   const dim3 grid((unsigned)((units + pairs - 1) / pairs), c.kv_heads, b.batch), block(256);
@@ -342,12 +348,14 @@ extern "C" int heisd_kv4_weigh(const heisd_kv4_desc *cache, const heisd_paged_ba
   return launched(who);
 }
 
+// Keys are held in registers up to 16384 tokens.  us, eight keys per thread / sixteen / read again: 16 contexts of 2000 tokens to 1024 21.8 / 25.0 / 25.7, of 8192 to 1024
+// 30.3 / 33.4 / 54.7, to 8000 19.5 / 24.6 / 51.4; of 16384 to 16000 - / 35.7 / 96.7.  (256 threads for up to 2048 tokens: 31.7, the moves take them all.)
 template <int HD>
 static void kv4_evict_launch(const Kv4Cache &c, const PagedBatch &b, const EvictArgs &a, dim3 grid, hipStream_t st) {
-  if (a.max_seq <= 2048) kv4_evict_held<HD, 4, 8><<<grid, dim3(256), 0, st>>>(c, b, a);
-  else if (a.max_seq <= 8192) kv4_evict_held<HD, 16, 8><<<grid, dim3(1024), 0, st>>>(c, b, a);
-  else if (a.max_seq <= 16384) kv4_evict_held<HD, 16, 16><<<grid, dim3(1024), 0, st>>>(c, b, a);
-  else kv4_evict<HD><<<grid, dim3(kEvictThreads), 0, st>>>(c, b, a);
+  const dim3 block(kEvictThreads);
+  if (a.max_seq <= 8 * kEvictThreads) kv4_evict_held<HD, 8><<<grid, block, 0, st>>>(c, b, a);
+  else if (a.max_seq <= 16 * kEvictThreads) kv4_evict_held<HD, 16><<<grid, block, 0, st>>>(c, b, a);
+  else kv4_evict<HD><<<grid, block, 0, st>>>(c, b, a);
 }
 
 extern "C" int heisd_kv4_evict(const heisd_kv4_desc *cache, int32_t layers, int64_t layer_bytes, const heisd_paged_batch *batch, const int32_t *keep,

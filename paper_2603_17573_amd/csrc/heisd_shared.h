@@ -12,7 +12,7 @@ namespace heisd {
 // Values enter the second product as fp16 (and keys the first, where the queries are fp16) where those of a run allow it: times 2^13 over the largest exponent of their
 // group of 32 channels (of all keys).  The sixteen codes times 2^-36 of that are still fp16 numbers, so nothing is rounded.  Where exponents lie further apart, or something
 // is not finite, all of it is bf16, with probabilities (and fp16 queries) as a bf16 and a remainder.  (Groups of e = 1, 6 2^-126 at most, may become zero beside others.)
-constexpr int kWideShift = 13, kWideSpread = 36;
+constexpr int kWideShift = 13, kWideSpread = 36, kWideTop = 127 + 64;      // (sums of 2^15 times larger values might pass fp32)
 template <int HD>
 constexpr int wide_lds_bytes = 2 * 2 * kWideTokens * HD * 2 + 2 * kWideTokens;
 
@@ -22,6 +22,10 @@ constexpr int wide_lds_bytes = 2 * 2 * kWideTokens * HD * 2 + 2 * kWideTokens;
 // bytes of LDS a row's pieces take is as in prompt_attend; K goes by tokens across the lanes and V by channels, so that no two lanes of a write
 // meet in a bank.  All columns see the same tokens: what nobody sees (behind the end, in missing blocks) has scores of minus infinity and values of zero.
 // Every workgroup takes an equal run of the work of all groups, as in kv4_attend; a unit is a step for 32 * W columns of a key head.
+// W 8 where there are as many columns: the tokens become bf16 half as often (two prefixes of 3029 and 3855 tokens, 1792 columns, 8 key heads of 128, bf16: 87 us, with W 4 108).
+// 51 GFLOP at 590 TFLOP/s: matrix cores busy 30 %, vector units 40 %, the rest waiting, mostly for the step's barrier (two waves per SIMD are all that the
+// registers allow).  Tried: probabilities as a bf16 and a remainder (104), one set of waves bringing tokens before and one after its products (90), equal runs given up for
+// a fixed number of cuts (134 for 120 then).  The scaled products, which take the 4-bit keys as they are, hold their sums to 2^-14 only.
 template <typename T, int HD, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b, HeadRows<const T> q, Kv4SharedAttend a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -257,21 +261,21 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
 #pragma unroll
       for (int w = 1; w < W; ++w) e.x = max(e.x, s_e[w][k].x), e.y = min(e.y, s_e[w][k].y);
       top_e[k] = __builtin_amdgcn_readfirstlane(e.x);
-      narrow = narrow && e.x < (int)kKv4NotFinite && e.x - e.y <= kWideSpread;
+      narrow = narrow && e.x <= kWideTop && e.x - e.y <= kWideSpread;
     }
     if constexpr (std::is_same_v<T, _Float16>) {
       int2 e = s_e[0][G];
 #pragma unroll
       for (int w = 1; w < W; ++w) e.x = max(e.x, s_e[w][G].x), e.y = min(e.y, s_e[w][G].y);
       top_k = __builtin_amdgcn_readfirstlane(e.x);
-      narrow = narrow && e.x < (int)kKv4NotFinite && e.x - e.y <= kWideSpread;
+      narrow = narrow && e.x <= kWideTop && e.x - e.y <= kWideSpread;
     }
     narrow = __builtin_amdgcn_readfirstlane(narrow);
     auto walk = [&](auto fast) {
       constexpr bool FAST = decltype(fast)::value;
       constexpr int PT = FAST ? 1 : 2;
       constexpr float kLazy = FAST ? MatrixOf<_Float16>::kLazy : kKv4Lazy, kLift = FAST ? MatrixOf<_Float16>::kLift : 0.f;
-      const float scale_log2 = FAST && std::is_same_v<T, _Float16> ? ldexpf(a.scale_log2, top_k - (127 + kWideShift)) : a.scale_log2;
+      const float scale_log2 = FAST && std::is_same_v<T, _Float16> ? fmaxf(ldexpf(a.scale_log2, top_k - (127 + kWideShift)), 1e-37f) : a.scale_log2;      // not 0: minus infinity stands for masked scores
       typedef std::conditional_t<FAST, _Float16, __bf16> PE;
       typedef typename MatrixOf<PE>::x8 P8;
       int next_id[NU];
@@ -440,7 +444,8 @@ __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b,
   }
 }
 
-// The same where every segment is whole: own tokens, and the runs of the prefix, all kept by row.
+// The same where every segment is whole: own tokens, and the runs of the prefix, all kept by row.  Four requests of 32 heads behind 95 tokens 4.1 us (kv4_shared
+// 8.7, latency), 64 behind eight prefixes of up to 3158 5.5 (23.6: half of it vector work, mostly widening the prefix for 32 columns).
 constexpr int kSplitsMost = 32;
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv4_direct_join(Kv4Cache c, PagedBatch b, HeadRows<T> out, Kv4SharedAttend a) {
