@@ -628,7 +628,7 @@ int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const heisd_paged_ba
  * cell is.
  * heisd_kv4_weigh: weight_out = decay * weight_in + the sum, over the rows that see the token (its request's, or those of the groups whose prefix its
  * request is) and the query heads of the key head, of exp(scale * q . k - lse), for every token of every request.  The last n tokens of a request
- * with n rows are new: their weight_in is not read and counts as zero, so nothing has to be cleared.
+ * with n rows are new: their weight_in is not read and counts as zero, so nothing has to be cleared where every step that appends tokens is followed by this call.
  *   lse        DEVICE f32 [rows][q heads], as heisd_kv4_attention or heisd_kv4_shared_attention of the same rows gave it; -inf: the row adds nothing
  *   weight_in, weight_out   the same buffer or different ones
  *   max_seq    as in the attention: requests of more tokens have no weights written (up to max_prefix if that is larger, for their groups' rows)
@@ -638,7 +638,7 @@ int heisd_kv4_shared_attention(const heisd_kv4_desc *cache, const heisd_paged_ba
  * them the keep[b] - recent heaviest, in each layer and head for itself (equal ones: the lowest token first; NaN is the lightest).  Tokens that stay and
  * lie behind the first keep[b] - recent places fill, in order, the places that get free, and the last ones follow in order.  Attention over
  * the whole cache does not depend on the order.  Blocks stay with their requests (heisd_paged_reorder with trim gives them back).
- *   cache, layers, layer_bytes   as in heisd_kv4_copy     keep  DEVICE i32 [batch]      seq_out  DEVICE i32 [batch] out, not seq_len
+ *   cache, layers, layer_bytes   as in heisd_kv4_copy     keep  DEVICE i32 [batch]      seq_out  DEVICE i32 [batch] out, not seq_len or keep
  *   weight_in, weight_out        DEVICE f32 [layers][n_blocks][kv_heads][block_size], the same buffer or different ones: weights move with their tokens
  *   max_seq    at most 2^24; requests of more tokens, or with blocks outside the pool, stay as they are
  * No two requests may have a block in common.  cu_rows of the batch may be NULL.

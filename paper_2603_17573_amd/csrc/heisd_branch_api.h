@@ -90,8 +90,9 @@ extern "C" int heisd_paged_reorder(const heisd_reorder_desc *d, void *stream) {
   if (!d->parent || !d->len_in || !d->owned_in || !d->table_in || !d->len_out || !d->owned_out || !d->table_out || !d->copy_from || !d->free_ids ||
       !d->free_count_in || !d->free_count_out)
     return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer", who);
-  if (d->len_out == d->len_in || d->owned_out == d->owned_in || d->table_out == d->table_in)
-    return fail(nullptr, HEISD_EINVAL, "%s: lengths, owned blocks or tables in place", who);
+  if (d->len_out == d->len_in || d->owned_out == d->owned_in || d->table_out == d->table_in || d->len_out == d->parent || d->copy_from == d->parent ||
+      d->copy_from == d->len_in)
+    return fail(nullptr, HEISD_EINVAL, "%s: lengths, owned blocks, tables or parents in place", who);
   const ReorderArgs a{d->batch, d->block_size, d->max_blocks, d->n_blocks, d->trim != 0, d->parent, d->len_in, d->owned_in, d->table_in, d->len_out,
                       d->owned_out, d->table_out, d->copy_from, d->free_ids, d->free_count_in, d->free_count_out};
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -369,7 +370,7 @@ extern "C" int heisd_kv4_evict(const heisd_kv4_desc *cache, int32_t layers, int6
   if (rc != HEISD_OK) return rc;
   if (!keep || !weight_in || !weight_out || !seq_out || recent < 0 || max_seq < 1 || max_seq > (1 << 24))
     return fail(nullptr, HEISD_EINVAL, "%s: NULL pointer, recent=%d or max_seq=%d (1..2^24)", who, recent, max_seq);
-  if (seq_out == b.seq_len) return fail(nullptr, HEISD_EINVAL, "%s: lengths in place", who);
+  if (seq_out == b.seq_len || seq_out == keep) return fail(nullptr, HEISD_EINVAL, "%s: lengths in place", who);
   const EvictArgs a{keep, recent, max_seq, layer_bytes, kv4_weights(c), weight_in, weight_out, seq_out};
   const dim3 grid(c.kv_heads, b.batch, layers);
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -388,7 +388,20 @@ class PagedCache:
         if n == 0:
             raise ValueError("invalid groups: max_rows %d, max_prefix %d, max_own %d" % (max_rows, groups.max_prefix, own))
         with torch.cuda.device(self.device):
-            self._shared = (groups, own, torch.empty(n, dtype=torch.uint8, device=self.device), first, prefix)
+            self._shared = (groups, own, torch.empty(n, dtype=torch.uint8, device=self.device), first, prefix, set())
+
+    def _sharing(self):
+        """What share() was given last, kept for whatever this stream has queued, or a graph being captured, when share() is called again."""
+        with torch.cuda.device(self.device):
+            if not torch.cuda.is_current_stream_capturing():
+                stream, seen = torch.cuda.current_stream(), self._shared[5]
+                if stream.cuda_stream not in seen:                     # once per stream: it counts until the tensor is freed
+                    for t in self._shared[2:5]:
+                        t.record_stream(stream)
+                    seen.add(stream.cuda_stream)
+            elif all(self._shared is not s for s in self._captured):
+                self._captured.append(self._shared)
+        return self._shared[:3]
 
     def attend_shared(self, layer, q, scale=None, out=None, lse=None):
         """Attention of this step's rows over their group's prefix and everything their requests have cached."""
@@ -396,17 +409,18 @@ class PagedCache:
             raise ValueError("attend_shared without share")
         out = torch.empty_like(q) if out is None else out
         hq, ho = self._of_step(q, self.q_heads, "q"), self._of_step(out, self.q_heads, "out")
-        groups, own, workspace = self._shared[:3]
+        groups, own, workspace = self._sharing()
         self._call(B.heisd_kv4_shared_attention, self.descs[layer], self.batch, groups, hq, ho, self._lse(lse),
                    self.head_dim ** -0.5 if scale is None else scale, self.max_new, own, workspace.data_ptr(), workspace.numel())
         return out
 
     def weigh(self, layer, q, lse, scale=None, decay=1.0):
-        """Adds to the weight of every cached token (times decay) the attention that it receives from this step's rows; lse: what attend() or attend_shared() of
-        the same rows gave."""
+        """Adds to the weight of every cached token (times decay) the attention that it receives from this step's rows, and begins the weights of
+        this step's tokens (so no step that appends is left out); lse: what attend(), attend_shared() or chunk() of the same
+        rows gave (prompt()'s is of keys as they are, not as they are held: weights are as far off as they)."""
         if self.weights is None:
             raise ValueError("weigh: made without weights")
-        groups, own = self._shared[:2] if self._shared is not None else (None, self.max_len)
+        groups, own = self._sharing()[:2] if self._shared is not None else (None, self.max_len)
         w = self.weights[layer].data_ptr()
         self._call(B.heisd_kv4_weigh, self.descs[layer], self.batch, groups, self._of_step(q, self.q_heads, "q"), self._lse(lse),
                    self.head_dim ** -0.5 if scale is None else scale, decay, w, w, own)
@@ -418,6 +432,8 @@ class PagedCache:
         if self.weights is None:
             raise ValueError("evict: made without weights")
         w = self.weights.data_ptr()
+        if keep.data_ptr() == self.lengths.data_ptr():
+            keep = keep.clone()
         self._call(B.heisd_kv4_evict, self.descs[0], len(self.descs), self.pools.shape[1], self.batch,
                    _ints(keep, self.seq_len.shape, "keep", self.device), recent, w, w, self.lengths.data_ptr(), self.max_len)
         self.seq_len.copy_(self.lengths)

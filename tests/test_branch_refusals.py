@@ -67,7 +67,8 @@ def test_paged_reorder(P):
     names = [n for n, _ in P.heisd_reorder_desc._fields_[5:]]
     for more in [{n: None} for n in names] + [dict(batch=0), dict(batch=65536), dict(block_size=0), dict(n_blocks=0), dict(max_blocks=0), dict(max_blocks=(1 << 20) + 1),
                                               dict(n_blocks=1 << 28), dict(max_blocks=1 << 20, block_size=4096), dict(len_out=reorder(P).len_in),
-                                              dict(owned_out=reorder(P).owned_in), dict(table_out=reorder(P).table_in)]:
+                                              dict(owned_out=reorder(P).owned_in), dict(table_out=reorder(P).table_in),
+                                              dict(len_out=reorder(P).parent), dict(copy_from=reorder(P).parent), dict(copy_from=reorder(P).len_in)]:
         refused(P, P.heisd_paged_reorder(reorder(P, **more), None), P.HEISD_EINVAL, "paged_reorder")
     refused(P, P.heisd_paged_reorder(None, None), P.HEISD_EINVAL, "NULL")
 
@@ -98,7 +99,7 @@ def test_layers(P):
     def copy(c=None, layers=2, apart=size, b=None, source=FAKE, most=64):
         return P.heisd_kv4_copy(c or cache(P), layers, apart, b or batch(P), source, None, most, None)
 
-    def evict(c=None, layers=2, apart=size, b=None, keep=FAKE, recent=3, w=FAKE, out=FAKE, seq=FAKE, most=64):
+    def evict(c=None, layers=2, apart=size, b=None, keep=FAKE, recent=3, w=FAKE, out=FAKE, seq=0x30000, most=64):
         return P.heisd_kv4_evict(c or cache(P), layers, apart, b or batch(P), keep, recent, w, out, seq, most, None)
     for call, who in ((copy, "kv4_copy"), (evict, "kv4_evict")):
         for kw in [dict(c=cache(P, **m)) for m in BAD_CACHE] + [dict(b=batch(P, **m)) for m in BAD_BATCH] + \
@@ -106,7 +107,7 @@ def test_layers(P):
             refused(P, call(**kw), P.HEISD_EINVAL, who)
         refused(P, call(c=cache(P, head_dim=96)), P.HEISD_EUNSUPPORTED, "head_dim")
     refused(P, copy(source=None), P.HEISD_EINVAL, "NULL")
-    for kw in (dict(keep=None), dict(w=None), dict(out=None), dict(seq=None), dict(recent=-1), dict(most=(1 << 24) + 1), dict(seq=0x20000)):
+    for kw in (dict(keep=None), dict(w=None), dict(out=None), dict(seq=None), dict(recent=-1), dict(most=(1 << 24) + 1), dict(seq=0x20000), dict(seq=FAKE)):
         refused(P, evict(**kw), P.HEISD_EINVAL, "kv4_evict")
 
 

@@ -297,3 +297,66 @@ def test_steps_of_any_number_of_rows(P):
             want, _, mean, flat, size = ref.attention(host(q)[i * n:(i + 1) * n], kk, vv, seen, 0.125)
             assert np.all(np.abs(out[i * n:(i + 1) * n] - want) <= tolerance("bf16", 2.0 ** -11, 2.0 ** -36, 64, len(kk), want, mean, flat, size))
 
+
+
+def test_a_graph_outlives_its_sharing(P):
+    """What share() was given and allocated stays with a captured graph, and with what other streams have queued, when it is called again."""
+    c = P.PagedCache(1, 8, 2, 64, 9, 1500, 400, n_blocks=400, block_size=16, weights=True)
+    rng = np.random.default_rng(5)
+    c.begin(i32([0] * 9), i32([0] * 8 + [300]), 300)
+    k, v = (randn(rng, (300, 2, 64), "bf16") for _ in range(2))
+    c.append(0, k, v)
+    c.begin(i32([0] * 8 + [300]), i32([1] * 8 + [0]), 8)
+    q, k, v = (randn(rng, (8, h, 64), "bf16") for h in (8, 2, 2))
+    c.append(0, k, v)
+    c.weights.zero_()
+
+    def share(*edges):
+        c.share(i32(edges), i32([8]), 8, max_prefix=300, max_own=1500)
+
+    def run():
+        lse = torch.empty(8, 8, device=DEV)
+        out = c.attend_shared(0, q, lse=lse)
+        c.weigh(0, q, lse, decay=0.0)
+        return out, lse
+
+    share(0, 8)
+    want = [*run(), c.weights.clone()]
+    share(0, 3)
+    other = [*run(), c.weights.clone()]
+    share(0, 8)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            got = run()
+    size = c._shared[2].numel()
+    for n in range(3):
+        share(0, 3)                                                    # the first one is the graph's alone now
+        filled = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(4)] + [i32([7, 7]) for _ in range(40)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*got, c.weights), want))
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            eager = run()
+        share(0, 1)                                                    # while that may still run
+        filled += [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*eager, c.weights), other))
+    assert not torch.equal(want[0], other[0])
+
+
+def test_lengths_that_a_call_gave_bound_the_next(P):
+    """keep, lengths: the buffer of the last evict() or fork() itself."""
+    c = P.PagedCache(1, 4, 2, 64, 3, 64, 100, n_blocks=12, block_size=16, weights=True)
+    c.begin(i32([0] * 3), i32([20, 40, 30]), 90)
+    k, v = (torch.randn(90, 2, 64, device=DEV).bfloat16() for _ in range(2))
+    c.append(0, k, v)
+    c.weights.fill_(1.0)
+    kept = c.evict(i32([10, -1, 64]), 4)
+    assert kept.tolist() == [10, 40, 30]
+    c.seq_len.copy_(i32([20, 40, 30]))
+    assert c.evict(kept, 4).tolist() == [10, 40, 30]
+    kept = c.fork(i32([0, 1, 2]), kept)
+    assert c.fork(i32([2, 1, 0]), kept, trim=True).tolist() == [30, 40, 10] and int(c.free_count) == 6
