@@ -320,11 +320,14 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
               s[t] = MatrixOf<T>::mul(*reinterpret_cast<const typename MatrixOf<T>::x8 *>(kt + k_at[n] + t * 32 * RB), qf[n], s[t]);
             else {                                  // fp16 queries as a bf16 and a remainder
               const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + k_at[n] + t * 32 * RB);
+              u32x4 held = __builtin_bit_cast(u32x4, qf[n]);
+              asm volatile("" : "+v"(held));        // converted in every step: kept, they are 64 registers that have to be spilled
+              const typename MatrixOf<T>::x8 qh = __builtin_bit_cast(typename MatrixOf<T>::x8, held);
               bf16x8 hi, lo;
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
-                hi[e] = (__bf16)(float)qf[n][e];
-                lo[e] = (__bf16)((float)qf[n][e] - (float)hi[e]);
+                hi[e] = (__bf16)(float)qh[e];
+                lo[e] = (__bf16)((float)qh[e] - (float)hi[e]);
               }
               s[t] = MatrixOf<__bf16>::mul(kf, hi, s[t]);
               s[t] = MatrixOf<__bf16>::mul(kf, lo, s[t]);
