@@ -798,16 +798,14 @@ __device__ __forceinline__ void attend_cached(Kv4Cache c, PagedBatch b, HeadRows
         s_m[wave][col] = m[ct];
         s_l[wave][col] = l[ct];
       }
-      if (SHARED && !busy) {                                    // a wave that had no tokens has nothing to add
-        __syncthreads();
-      } else {
-      float *to = reinterpret_cast<float *>(s_mine[wave]) + col * LD;
+      if (!SHARED || busy) {                                    // a wave that had no tokens has nothing to add
+        float *to = reinterpret_cast<float *>(s_mine[wave]) + col * LD;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) to[(4 * quad + e) * ND + d] = nan_out >> ct & 1 ? __uint_as_float(0x7FC00000u) : acc[ct][d][e];
-      __syncthreads();
+          for (int d = 0; d < ND; ++d) to[(4 * quad + e) * ND + d] = nan_out >> ct & 1 ? __uint_as_float(0x7FC00000u) : acc[ct][d][e];
       }
+      __syncthreads();
       constexpr int V = SHARED && HD == 128 ? 2 : 1, PER = HD / (4 * V);      // 16 bytes that a thread has of a column, threads per column
       for (int u = threadIdx.x; u < 16 * PER; u += 256) {
         const int n = u / PER, d = u % PER * (4 * V), cn = col0 + ct * 16 + n;
