@@ -609,9 +609,9 @@ int heisd_paged_offset(const heisd_paged_batch *batch, const int32_t *offset, in
  *   groups          may be 0 or the description NULL: nobody shares anything
  * Requests with a negative seq_len (or one above max_seq) see nothing, their prefix neither: zeros and lse -inf.
  * How a call is cut goes by the bounds (batch, max_q, max_seq, groups, max_rows, max_prefix) and not by what is live: bounds that hold closely are faster.  A workspace for
- * the most rows holds calls of fewer with the same bounds.  Scores, sums and log-sums are fp32.  Where 64 query rows and heads of a group may meet at a key head
- * (max_rows times the heads that share it), a probability over the prefix may enter the product as one fp16 number (off by half a step of 2^-11, or by 2^-36 of the largest
- * probability); elsewhere, and over own tokens, as a bf16 and a remainder.
+ * the most rows holds calls of fewer with the same bounds.  Scores, sums and log-sums are fp32.  A probability enters the product as a 16-bit number and what its rounding left,
+ * bf16s (off by at most 2^-16 of it) or, over a prefix where 64 query rows and heads of a group may meet at a key head (max_rows times the heads that share it), fp16s (2^-21 of it, or
+ * 2^-36 of the largest probability).
  */
 typedef struct {
   const int32_t *first, *prefix;

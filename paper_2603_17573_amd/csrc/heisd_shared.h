@@ -22,10 +22,13 @@ constexpr int wide_lds_bytes = 2 * 2 * kWideTokens * HD * 2 + 2 * kWideTokens;
 // bytes of LDS a row's pieces take is as in prompt_attend; K goes by tokens across the lanes and V by channels, so that no two lanes of a write
 // meet in a bank.  All columns see the same tokens: what nobody sees (behind the end, in missing blocks) has scores of minus infinity and values of zero.
 // Every workgroup takes an equal run of the work of all groups, as in kv4_attend; a unit is a step for 32 * W columns of a key head.
-// W 8 where there are as many columns: the tokens become bf16 half as often (two prefixes of 3029 and 3855 tokens, 1792 columns, 8 key heads of 128, bf16: 87 us, with W 4 108).
-// 51 GFLOP at 590 TFLOP/s: matrix cores busy 30 %, vector units 40 %, the rest waiting, mostly for the step's barrier (two waves per SIMD are all that the
-// registers allow).  Tried: probabilities as a bf16 and a remainder (104), one set of waves bringing tokens before and one after its products (90), equal runs given up for
-// a fixed number of cuts (134 for 120 then).  The scaled products, which take the 4-bit keys as they are, hold their sums to 2^-14 only.
+// A probability enters the second product as two 16-bit numbers, itself and what its rounding left: bf16s (off by 2^-16 of it together) or fp16s (2^-21, or 2^-36 of the
+// largest), so that a prefix is as exact for many columns as for few.  One fp16 alone takes 87 us for 108, but it is off by up to 2^-11, which nothing averages out: fp16 rows
+// are then off by 0.00029 where their own rounding gives 0.00021, and more bf16 rows get another last bit.
+// W 8 where there are as many columns: the tokens become bf16 half as often (two prefixes of 3029 and 3855 tokens, 1792 columns, 8 key heads of 128, bf16: 108 us; with the own
+// tokens a call takes 122, with W 4 137).  51 GFLOP (77 with the second terms) at 470 TFLOP/s: matrix cores busy 31 %, vector units 35 %, the rest waiting, mostly for the
+// step's barrier (two waves per SIMD are all that the registers allow).  Tried, with one term: one set of waves bringing tokens before and one after its products (90 for 87), equal
+// runs given up for a fixed number of cuts (134 for 120 then).  The scaled products, which take the 4-bit keys as they are, hold their sums to 2^-14 only.
 template <typename T, int HD, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b, HeadRows<const T> q, Kv4SharedAttend a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -273,7 +276,6 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
     narrow = __builtin_amdgcn_readfirstlane(narrow);
     auto walk = [&](auto fast) {
       constexpr bool FAST = decltype(fast)::value;
-      constexpr int PT = FAST ? 1 : 2;
       constexpr float kLazy = FAST ? MatrixOf<_Float16>::kLazy : kKv4Lazy, kLift = FAST ? MatrixOf<_Float16>::kLift : 0.f;
       const float scale_log2 = FAST && std::is_same_v<T, _Float16> ? fmaxf(ldexpf(a.scale_log2, top_k - (127 + kWideShift)), 1e-37f) : a.scale_log2;      // not 0: minus infinity stands for masked scores
       typedef std::conditional_t<FAST, _Float16, __bf16> PE;
@@ -358,15 +360,22 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
           for (int d = 0; d < ND; ++d) acc[d] *= by;
         }
         const float use = m == -INFINITY ? 0.f : m - kLift;
-        P8 pf[NK][PT];
+        P8 pf[NK][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = exp2_fast(__builtin_fmaf(s[t][e], scale_log2, -use));
-            l[e & 3] += p;
-            pf[2 * t + (e >> 3)][0][e & 7] = (PE)p;
-            if constexpr (PT == 2) pf[2 * t + (e >> 3)][1][e & 7] = (PE)(p - (float)(PE)p);
+          for (int e = 0; e < 16; e += 2) {
+            const float p0 = exp2_fast(__builtin_fmaf(s[t][e], scale_log2, -use)), p1 = exp2_fast(__builtin_fmaf(s[t][e + 1], scale_log2, -use));
+            l[e & 3] += p0;
+            l[(e & 3) + 1] += p1;
+            typedef __attribute__((ext_vector_type(2))) float f32x2;
+            typedef __attribute__((ext_vector_type(2))) PE two;
+            uint32_t held = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p0, p1}, two));
+            asm("" : "+v"(held));                   // converted once, and two at a time
+            const two hi = __builtin_bit_cast(two, held), lo = __builtin_convertvector(f32x2{p0 - (float)hi[0], p1 - (float)hi[1]}, two);
+            P8 *const to = pf[2 * t + (e >> 3)];
+            to[0][e & 7] = hi[0], to[0][(e & 7) + 1] = hi[1];
+            to[1][e & 7] = lo[0], to[1][(e & 7) + 1] = lo[1];
           }
 #pragma unroll
         for (int n = 0; n < NK; ++n)
@@ -378,7 +387,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_prefix(Kv4Cache c, PagedBatch b
             struct Both { s16x4 a, b; } both = {lo, hi};
             const P8 vf = __builtin_bit_cast(P8, both);
 #pragma unroll
-            for (int e = 0; e < PT; ++e) acc[d] = MatrixOf<PE>::mul(vf, pf[n][e], acc[d]);
+            for (int e = 0; e < 2; ++e) acc[d] = MatrixOf<PE>::mul(vf, pf[n][e], acc[d]);
           }
       }
       m -= kLift;
