@@ -315,6 +315,7 @@ class PagedCache:
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
             self.weights = torch.empty((n_layers, n_blocks, kv_heads, block_size), device=self.device) if weights else None
             self.lengths, self.copy_from = torch.empty(max_batch, **i32), torch.empty(max_batch, **i32)
+            self._cached = torch.full((max_batch,), -1, **i32) if weights else None      # tokens of requests that seq_len has none of, for evict()
             self._table, self._owned = torch.empty_like(self.table), torch.empty_like(self.owned)
             desc = rope if rope is not None else make_rope_desc(head_dim)
             self.rotary_dim, self.layout = desc.rotary_dim, B.ROPE_LAYOUT[layout]
@@ -347,9 +348,13 @@ class PagedCache:
         rows: packed rows of this step, at least the sum of new_len.  A request that does not fit has seq_len -1 afterwards."""
         if not 0 <= rows <= self.slot.shape[0]:
             raise ValueError("rows=%d, made for at most %d" % (rows, self.slot.shape[0]))
+        if cached_len.data_ptr() == self.seq_len.data_ptr():
+            cached_len = cached_len.clone()
         self._call(B.heisd_paged_plan, make_plan_desc(self.block_size, self.n_blocks, cached_len, new_len, self.owned, self.owned, self.table,
                                                       self.free_ids, self.free_count, self.free_count, self.seq_len, self.cu_rows,
                                                       self.slot[:rows], self.position[:rows], self.cu_seq))
+        if self._cached is not None:
+            self._cached.copy_(cached_len)
         self.rows, self.batch = rows, make_paged_batch(self.table, self.seq_len, self.cu_rows, rows)
 
     def rotate(self, q, k):
@@ -427,16 +432,19 @@ class PagedCache:
 
     def evict(self, keep, recent):
         """Cuts every request of more than keep[b] tokens (i32[max_batch], negative: it stays as it is) to keep[b], in every layer and head for itself: the last `recent`
-        stay, and of the others those with the largest weights.  Returns the lengths, i32[max_batch], which the next begin() takes as cached_len (the buffer is
+        stay, and of the others those with the largest weights.  A request's tokens are those of the step begun last; of a request that this step left out, the
+        cached_len that begin() was given; after fork(), what that returned.  Returns the lengths, i32[max_batch], which the next begin() takes as cached_len (the buffer is
         written again by the next evict() or fork())."""
         if self.weights is None:
             raise ValueError("evict: made without weights")
         w = self.weights.data_ptr()
         if keep.data_ptr() == self.lengths.data_ptr():
             keep = keep.clone()
-        self._call(B.heisd_kv4_evict, self.descs[0], len(self.descs), self.pools.shape[1], self.batch,
+        torch.where(self.seq_len >= 0, self.seq_len, self._cached, out=self._cached)
+        self._call(B.heisd_kv4_evict, self.descs[0], len(self.descs), self.pools.shape[1], make_paged_batch(self.table, self._cached, None, 0),
                    _ints(keep, self.seq_len.shape, "keep", self.device), recent, w, w, self.lengths.data_ptr(), self.max_len)
-        self.seq_len.copy_(self.lengths)
+        self._cached.copy_(self.lengths)
+        torch.where(self.seq_len >= 0, self.lengths, self.seq_len, out=self.seq_len)
         return self.lengths
 
     def fork(self, parent, length, trim=False):
@@ -453,6 +461,8 @@ class PagedCache:
         self.table.copy_(self._table)
         self.owned.copy_(self._owned)
         self.seq_len.fill_(-1)
+        if self._cached is not None:
+            self._cached.copy_(self.lengths)
         return self.lengths
 
     def prompt(self, q, k, v, scale=None, out=None, lse=None):

@@ -3,11 +3,12 @@ differ, the exactness of attention over prefixes of many rows.  Tolerances: thos
 import numpy as np
 import pytest
 
+import branch_reference as branch
 import paged_reference as ref
 
 torch = pytest.importorskip("torch")
 from test_gpu_branch import WIDE, prefix_of, shared  # noqa: E402
-from test_gpu_paged import Cache, host, randn, tolerance  # noqa: E402
+from test_gpu_paged import DEV, Cache, host, i32, randn, tolerance  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +58,97 @@ def test_probabilities_are_two_terms_whatever_the_form(P, dtype, head_dim, rows,
         want, _, mean, flat, size = ref.attention(hq[cu[i]:cu[i + 1]], kk, vv, seen, scale)
         over = np.abs(out[cu[i]:cu[i + 1]] - want) - tolerance(dtype, 2.0 ** -16, 2.0 ** -36, head_dim, len(kk), want, mean, flat, size)
         assert over.max() <= 0, (i, float(over.max()), np.argwhere(over > 0)[:4].tolist())
+
+
+# ---- evictions between other calls of a cache -----------------------------------------------------------------------------
+
+class Rows:
+    """A cache of one layer and what its requests' cells hold, as lists of (k, v) with what each head kept."""
+
+    def __init__(self, P, rng, lengths, **more):
+        self.c = P.PagedCache(1, 4, 2, 64, len(lengths), 200, 300, block_size=16, weights=True, **more)
+        self.rng, self.rows, self.batch = rng, [[] for _ in lengths], len(lengths)
+        self.step([0] * self.batch, lengths)
+
+    def step(self, cached, new, takes=None):
+        """Appends rows, weighs and attends; checks the attention against what is held.  takes: the requests that the step takes (all)."""
+        n = sum(new)
+        self.c.begin(cached if torch.is_tensor(cached) else i32(cached), i32(new), n)
+        q, k, v = (randn(self.rng, (n, h, 64), "bf16") for h in (4, 2, 2))
+        self.c.append(0, k, v)
+        lse = torch.empty((n, 4), device=DEV)
+        out = self.c.attend(0, q, lse=lse)
+        self.c.weigh(0, q, lse)
+        hk, hv, hq, out, at = ref.held(host(k)), ref.held(host(v)), host(q), host(out), 0
+        for i, m in enumerate(new):
+            if takes is None or i in takes:
+                self.rows[i] += list(zip(hk[at:at + m], hv[at:at + m]))
+                if m:
+                    kk, vv = (np.stack([r[j] for r in self.rows[i]]) for j in (0, 1))
+                    want, _, mean, flat, size = ref.attention(hq[at:at + m], kk, vv, [len(kk) - m + j + 1 for j in range(m)], 0.125)
+                    assert np.all(np.abs(out[at:at + m] - want) <= tolerance("bf16", 2.0 ** -16, 0.0, 64, len(kk), want, mean, flat, size)), i
+            else:
+                assert not out[at:at + m].any()
+            at += m
+
+    def evict(self, keep, recent):
+        table, weights = host(self.c.table).astype(int), host(self.c.weights[0])
+        lengths = self.c.evict(i32(keep), recent)
+        for i, rows in enumerate(self.rows):
+            t = np.arange(len(rows))
+            w = weights[table[i, t // 16], :, t % 16]
+            order = [branch.cut(w[:, h], keep[i], recent) for h in range(2)]
+            self.rows[i] = [tuple(np.stack([rows[order[h][t]][j][h] for h in range(2)]) for j in (0, 1)) for t in range(len(order[0]))]
+        assert lengths.tolist() == [len(r) for r in self.rows]
+        return lengths
+
+
+def test_eviction_between_a_fork_and_a_step(P):
+    """What is cut is what fork() left, and nothing is lost."""
+    r = Rows(P, np.random.default_rng(1), [20, 70, 33], n_blocks=30)
+    length = r.c.fork(i32([0, 1, 1]), i32([20, 70, 33]))
+    assert length.tolist() == [20, 70, 70]
+    r.rows[2] = list(r.rows[1])
+    length = r.evict([10, 30, -1], 8)
+    length = r.evict([10, 30, 40], 8)                                  # and again
+    length = r.c.fork(i32([0, 1, 2]), length, trim=True)
+    assert length.tolist() == [10, 30, 40] and int(r.c.free_count) == 30 - 1 - 2 - 3
+    r.step(length, [1, 2, 1])
+    assert r.c.fork(i32([-1, 1, 2]), r.c.seq_len).tolist() == [-1, 32, 41]
+    assert r.c.evict(i32([5, 5, 5]), 1).tolist() == [-1, 5, 5]
+
+
+def test_eviction_makes_room_for_a_request_that_a_step_left_out(P):
+    """A request that the plan has no blocks for keeps its tokens; evict() cuts it as it is cached."""
+    r = Rows(P, np.random.default_rng(2), [64, 64, 48], n_blocks=12)
+    r.step([64, 64, 48], [1, 1, 1], takes=[0])                          # one block is left
+    assert r.c.seq_len.tolist() == [65, -1, -1]
+    length = r.evict([32, 40, -1], 8)
+    assert length.tolist() == [32, 40, 48]
+    length = r.c.fork(i32([0, 1, 2]), length, trim=True)
+    assert int(r.c.free_count) == 12 - 2 - 3 - 3
+    r.step(length, [3, 1, 1])
+    assert r.c.seq_len.tolist() == [35, 41, 49]
+
+
+def test_eviction_after_a_step_that_ended_a_request(P):
+    """A finished request stays finished; the others' rows go on being attended to in the same step."""
+    r = Rows(P, np.random.default_rng(3), [40, 50, 30], n_blocks=30)
+    r.rows[1] = []
+    r.step([40, -1, 30], [1, 0, 1])
+    assert r.c.evict(i32([41, 9, 20]), 4).tolist() == [41, -1, 20] and r.c.seq_len.tolist() == [41, -1, 20]
+    assert r.c.evict(i32([40, 9, 20]), 4).tolist() == [40, -1, 20]
+
+
+def test_a_step_s_lengths_may_change_after_it(P):
+    """begin() does not go on reading the lengths that it was given."""
+    r = Rows(P, np.random.default_rng(4), [64, 64, 48], n_blocks=12)
+    cached = i32([64, 64, 48])
+    r.step(cached, [1, 1, 1], takes=[0])
+    cached.fill_(3)
+    length = r.evict([32, 40, -1], 8)
+    assert length.tolist() == [32, 40, 48]
+    r.c.begin(r.c.fork(i32([0, 1, 2]), length), i32([0, 0, 0]), 0)
+    r.step(r.c.seq_len, [50, 1, 1], takes=[1])                          # and may be what the step before gave; all blocks are owned
+    assert r.c.seq_len.tolist() == [-1, 41, -1]
+    assert r.evict([-1, -1, -1], 0).tolist() == [32, 41, 48]
