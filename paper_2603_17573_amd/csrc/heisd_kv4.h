@@ -385,13 +385,20 @@ __device__ __forceinline__ Kv4Request wide_request(const Kv4Cache &c, const Page
 // Tokens of a run of a prefix that is cut into a power of two of them: whole units.
 __device__ __forceinline__ int kv4_split(int tokens, int shift) { return (((tokens - 1) >> shift) + kKv4Unit) & ~(kKv4Unit - 1); }
 
-// Which group request i belongs to (-1: none).  Groups that are described follow each other, so at most one does.
-__device__ __forceinline__ int group_of(const PrefixGroups &p, int i) {
+// The group of request i that describes something (-1: none), and what it asks for.  Groups that do follow each other, so at most one has the request; others may lie over it.
+__device__ __forceinline__ int group_of(const Kv4Cache &c, const PagedBatch &b, const PrefixGroups &p, int i, PrefixSpan *span) {
   const int lane = threadIdx.x & 63;
   for (int g0 = 0; g0 < p.groups; g0 += 64) {
     const int g = min(g0 + lane, p.groups - 1);
-    const unsigned long long m = __ballot(p.first[g] <= i && i < p.first[g + 1]);
-    if (m) return g0 + __builtin_ctzll(m);
+    PrefixSpan s{{0, 0}, -1, 0};
+    if (p.first[g] <= i && i < p.first[g + 1]) s = prefix_span(c, b, p, g);
+    const unsigned long long m = __ballot(s.tokens > 0);
+    if (m) {
+      const int at = __builtin_ctzll(m);
+      *span = PrefixSpan{{__builtin_amdgcn_readlane(s.rows.begin, at), __builtin_amdgcn_readlane(s.rows.count, at)}, __builtin_amdgcn_readlane(s.request, at),
+                         __builtin_amdgcn_readlane(s.tokens, at)};
+      return min(g0 + at, p.groups - 1);
+    }
   }
   return -1;
 }

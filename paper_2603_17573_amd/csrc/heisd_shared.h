@@ -424,7 +424,8 @@ __global__ __launch_bounds__(256) void kv4_shared_join(Kv4Cache c, PagedBatch b,
   const int n_cols = own.r.rows.count * a.q_heads;
   constexpr int PER = 256 / (HD / 4);
   if ((long long)blockIdx.x * PER >= n_cols) return;
-  const int g = a.wide ? -1 : group_of(a.prefix, req);
+  PrefixSpan span;
+  const int g = a.wide ? -1 : group_of(c, b, a.prefix, req, &span);
   long long all = 0;
   shared.r.work = 0;
   for (int i = lane; i < kv4_requests(b, a); i += 64) {
@@ -466,9 +467,9 @@ __global__ __launch_bounds__(256) void kv4_direct_join(Kv4Cache c, PagedBatch b,
   const Span rows = wave_span(b.cu_rows, req, b.rows);
   const int n_cols = rows.count * a.q_heads;
   if ((long long)blockIdx.x * PER >= n_cols) return;
-  const int g = group_of(a.prefix, req);
   PrefixSpan span{{0, 0}, -1, 0};
-  if (g >= 0 && kv4_live(c, b, a, req)) span = prefix_span(c, b, a.prefix, g);
+  group_of(c, b, a.prefix, req, &span);
+  if (!kv4_live(c, b, a, req)) span = PrefixSpan{{0, 0}, -1, 0};
   const int run = span.tokens ? kv4_split(span.tokens, a.split_shift) : 1, runs = (span.tokens + run - 1) / run;
   for (int u = blockIdx.x * PER + threadIdx.x / (HD / 4); u < n_cols; u += gridDim.x * PER) {
     const int d = threadIdx.x % (HD / 4) * 4;

@@ -7,7 +7,7 @@ import branch_reference as branch
 import paged_reference as ref
 
 torch = pytest.importorskip("torch")
-from test_gpu_branch import WIDE, prefix_of, shared  # noqa: E402
+from test_gpu_branch import WIDE, check_shared, check_weigh, prefix_of, shared  # noqa: E402
 from test_gpu_paged import DEV, Cache, host, i32, randn, tolerance  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -58,6 +58,33 @@ def test_probabilities_are_two_terms_whatever_the_form(P, dtype, head_dim, rows,
         want, _, mean, flat, size = ref.attention(hq[cu[i]:cu[i + 1]], kk, vv, seen, scale)
         over = np.abs(out[cu[i]:cu[i + 1]] - want) - tolerance(dtype, 2.0 ** -16, 2.0 ** -36, head_dim, len(kk), want, mean, flat, size)
         assert over.max() <= 0, (i, float(over.max()), np.argwhere(over > 0)[:4].tolist())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("max_own,max_rows", [(40, 9), (3000, 9), (40, WIDE), (3000, WIDE)])
+def test_groups_that_describe_nothing_hide_no_others(P, dtype, max_own, max_rows):
+    """Spans that leave the batch, of prefixes that are not there, are empty, too long or one of the group, in front of spans that describe something, in every form; and the
+    weights count the same rows."""
+    rng = np.random.default_rng(12)
+    total = [20, 3, 40, 16, 5, 33, 30, 9, 8, 31, 60, 0]
+    c = Cache(P, rng, total, 2, 64, 16)
+    k, v = (randn(rng, (sum(total), 2, 64), "f32") for _ in range(2))
+    c.write(P, k, v)
+    new = [1, 2, 3, 1, 5, 1, 1, 2, 1, 2, 0, 0]
+    cu = np.concatenate([[0], np.cumsum(new)]).tolist()
+    q = randn(rng, (cu[-1], 4, 64), dtype)
+    for groups in (([0, 20, 2, 4], [10, 10, 10]), ([0, 8, 2, 4], [-1, 10, 10]), ([-1, 10, 2, 4], [10, 10, 10]), ([0, 8, 2, 4, 9], [11, 10, 10, 9]),
+                   ([0, 9, 2, 4], [8, 10, 9]), ([0, 9, 1, 9], [12, 0, 10]), ([0, 9] * 40 + [3, 5], [-1] * 80 + [10])):
+        out, lse = shared(P, c, groups, q, cu, 5, max_own, max_rows, 60, 0.125)
+        check_shared(c, groups, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.125, dtype, 60)
+        if max(groups[0]) <= 12:
+            check_weigh(P, c, groups, q, lse, cu, 0.125, 0.5, ref.held(host(k)), max_own, 60)
+    groups = ([0, 9, 2, 4], [9, 10, 9])                                # prefix 9 has 31 tokens: too long here
+    out, lse = shared(P, c, groups, q, cu, 5, max_own, max_rows, 30, 0.125)
+    check_shared(c, groups, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.125, dtype, 30)
+    groups = ([0, 9, 2, 4], [10, 10, 9])                               # 10 has 60, 9 has 31
+    out, lse = shared(P, c, groups, q, cu, 5, max_own, max_rows, 31, 0.125)
+    check_shared(c, groups, q, out, lse, cu, ref.held(host(k)), ref.held(host(v)), 0.125, dtype, 31)
 
 
 # ---- evictions between other calls of a cache -----------------------------------------------------------------------------
