@@ -422,13 +422,14 @@ class PagedCache:
     def weigh(self, layer, q, lse, scale=None, decay=1.0):
         """Adds to the weight of every cached token (times decay) the attention that it receives from this step's rows, and begins the weights of
         this step's tokens (so no step that appends is left out); lse: what attend(), attend_shared() or chunk() of the same
-        rows gave (prompt()'s is of keys as they are, not as they are held: weights are as far off as they)."""
+        rows gave (prompt()'s is of keys as they are, not as they are held: weights are as far off as they).  Rows of requests that share a prefix count on its tokens, too:
+        theirs is attend_shared()'s."""
         if self.weights is None:
             raise ValueError("weigh: made without weights")
-        groups, own = self._sharing()[:2] if self._shared is not None else (None, self.max_len)
+        groups = self._sharing()[0] if self._shared is not None else None
         w = self.weights[layer].data_ptr()
         self._call(B.heisd_kv4_weigh, self.descs[layer], self.batch, groups, self._of_step(q, self.q_heads, "q"), self._lse(lse),
-                   self.head_dim ** -0.5 if scale is None else scale, decay, w, w, own)
+                   self.head_dim ** -0.5 if scale is None else scale, decay, w, w, self.max_len)      # not share()'s max_own: attend() goes as far
 
     def evict(self, keep, recent):
         """Cuts every request of more than keep[b] tokens (i32[max_batch], negative: it stays as it is) to keep[b], in every layer and head for itself: the last `recent`

@@ -1,5 +1,7 @@
 """Requests that continue others where the calls meet each other: groups that describe nothing beside those that do, evictions between other calls, bounds that
 differ, the exactness of attention over prefixes of many rows.  Tolerances: those of test_gpu_branch.py, except where a test derives its own."""
+import math
+
 import numpy as np
 import pytest
 
@@ -179,3 +181,37 @@ def test_a_step_s_lengths_may_change_after_it(P):
     r.step(r.c.seq_len, [50, 1, 1], takes=[1])                          # and may be what the step before gave; all blocks are owned
     assert r.c.seq_len.tolist() == [-1, 41, -1]
     assert r.evict([-1, -1, -1], 0).tolist() == [32, 41, 48]
+
+
+# ---- weights -----------------------------------------------------------------------------------------------------------------
+
+def test_weights_of_requests_longer_than_the_bounds_of_sharing(P):
+    """attend() goes as far as the cache, and so do the weights of its rows, whatever share() was told of those that share."""
+    rng = np.random.default_rng(5)
+    c = P.PagedCache(1, 4, 2, 64, 4, 200, 300, n_blocks=40, block_size=16, weights=True)
+    first, prefix = i32([1, 2]), i32([3])
+    c.share(first, prefix, 4, max_prefix=64, max_own=16)
+    rows = [[] for _ in range(4)]
+    for step, (cached, new) in enumerate((([0, -1, 0, 0], [100, 0, 30, 40]), ([100, -1, 30, 40], [2, 0, 1, 0]))):
+        c.begin(i32(cached), i32(new), sum(new))
+        q, k, v = (randn(rng, (sum(new), h, 64), "bf16") for h in (4, 2, 2))
+        c.append(0, k, v)
+        if step == 0:
+            c.weights.fill_(math.nan)                                  # new tokens have no weight before
+        lse = torch.empty((sum(new), 4), device=DEV)
+        c.attend(0, q, lse=lse)
+        before = host(c.weights[0])
+        c.weigh(0, q, lse, decay=0.5)
+        got, table, at, hk = host(c.weights[0]), host(c.table).astype(int), 0, ref.held(host(k))
+        for i, m in enumerate(new):
+            rows[i] += list(hk[at:at + m])
+            n = len(rows[i])
+            if n:
+                t = np.arange(n)
+                slot = (table[i, t // 16], slice(None), t % 16)
+                want, size = branch.weights(host(q)[at:at + m], np.stack(rows[i]), 0.125, host(lse)[at:at + m], [n - m + j + 1 for j in range(m)])
+                old = np.where((t < n - m)[:, None], before[slot], 0.0)
+                large = np.abs(host(lse)).max()
+                off = np.expm1(2 * (72 * 2.0 ** -24 * size + 2.0 ** -22 * (size + large + 1))) + (4 * m + 32) * 2.0 ** -24
+                assert np.all(np.abs(got[slot] - (want + 0.5 * old)) <= off * want + 2.0 ** -23 * (want + 0.5 * old) + 2.0 ** -100), (step, i)
+            at += m
