@@ -27,7 +27,8 @@ struct BeamLayout {
 
 extern "C" size_t heisd_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
   if (beam_sizes_ok("beam_select_workspace_bytes", groups, beams, width, vocab) != HEISD_OK) return 0;
-  return BeamLayout((int64_t)groups * beams, vocab, 4).total;        // fp32 has most
+  const int64_t rows = (int64_t)groups * beams;      // fp32 has more segments, but 16-bit rows may be cut into one more part
+  return std::max(BeamLayout(rows, vocab, 4).total, BeamLayout(rows, vocab, 2).total);
 }
 
 template <typename T>

@@ -9,7 +9,7 @@ import branch_reference as branch
 import paged_reference as ref
 
 torch = pytest.importorskip("torch")
-from test_gpu_branch import WIDE, check_shared, check_weigh, prefix_of, shared  # noqa: E402
+from test_gpu_branch import WIDE, check_select, check_shared, check_weigh, prefix_of, run_select, shared  # noqa: E402
 from test_gpu_paged import DEV, Cache, host, i32, randn, tolerance  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -215,3 +215,15 @@ def test_weights_of_requests_longer_than_the_bounds_of_sharing(P):
                 off = np.expm1(2 * (72 * 2.0 ** -24 * size + 2.0 ** -22 * (size + large + 1))) + (4 * m + 32) * 2.0 ** -24
                 assert np.all(np.abs(got[slot] - (want + 0.5 * old)) <= off * want + 2.0 ** -23 * (want + 0.5 * old) + 2.0 ** -100), (step, i)
             at += m
+
+
+# ---- the next beams ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_workspaces_hold_every_dtype(P, dtype):
+    """A workspace is as large as its function says for any dtype and any number of rows and tokens."""
+    rng = np.random.default_rng(8)
+    for beams, vocab in ((64, 2044), (64, 2042), (11, 4092), (64, 4097), (64, 8188), (3, 6139), (50, 6138)):
+        logits = randn(rng, (beams, vocab), dtype, spread=False)
+        score = torch.tensor(-5 * rng.random(beams), dtype=torch.float32, device=DEV)
+        check_select(run_select(P, logits, beams, 5, score), logits, beams, 5, score)
