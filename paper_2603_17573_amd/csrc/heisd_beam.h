@@ -1,5 +1,6 @@
 // Continuations of requests: beam search's choice over beams and vocabulary, and block tables when requests go on as continuations of others.
 #pragma once
+#include <float.h>
 #include "heisd_common.h"
 #include "heisd_paged.h"
 
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(kBeamWaves * 64) void beam_pick(BeamArgs a) {
     }
     if (lane == 0) {
       s_add[b] = add;
-      s_norm[b] = a.power == 0 ? 1.0 : exp(-a.power * log((double)max(length, 1)));
+      s_norm[b] = a.power == 0 ? 1.0 : fmin(fmax(exp(-a.power * log((double)max(length, 1))), DBL_MIN), DBL_MAX);      // not 0 or infinite: a score of 0 would rank as NaN
       s_len[b] = length;
       s_done[b] = done;
       s_count[b] = count;

@@ -227,3 +227,13 @@ def test_workspaces_hold_every_dtype(P, dtype):
         logits = randn(rng, (beams, vocab), dtype, spread=False)
         score = torch.tensor(-5 * rng.random(beams), dtype=torch.float32, device=DEV)
         check_select(run_select(P, logits, beams, 5, score), logits, beams, 5, score)
+
+
+def test_lengths_whose_power_ends(P):
+    """A power of a length that passes 64 bits leaves every continuation its place."""
+    logits = torch.tensor([[1.0], [2.0], [3.0]], device=DEV)
+    score, length, done = torch.tensor([0.0, -1.0, 0.0], device=DEV), i32([2000, 3, 3000]), i32([0, 0, 1])
+    for power in (-200.0, 200.0, -1e9, 1e9):
+        o = run_select(P, logits, 3, 3, score, length, done, 0, power)
+        assert sorted(o["beam"][0].tolist()) == [0, 1, 2] and o["token"][0].tolist() == [0, 0, 0], power
+        assert sorted(o["score"][0].tolist()) == [-1.0, 0.0, 0.0] and sorted(o["length"][0].tolist()) == [4, 2001, 3000]
