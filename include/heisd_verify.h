@@ -588,7 +588,7 @@ int heisd_paged_reorder(const heisd_reorder_desc *reorder, void *stream);
  * copy_from[b] in 0 .. batch - 1 and not b.  No block may be copied to twice, nor from and to.  Blocks outside the pool are left out.
  *   cache      the first layer; layer n's pool is layer_bytes * n bytes behind (a multiple of 16; not used for one layer)
  *   weight     DEVICE f32 [layers][n_blocks][kv_heads][block_size], optional: weights of tokens (below) that are copied with them
- *   max_seq    at least the longest of those requests; what lies behind is not copied.  cu_rows of the batch may be NULL.
+ *   max_seq    at least the longest of those requests; what lies behind is not copied (cells are up to a whole tile of 16 tokens).  cu_rows of the batch may be NULL.
  * heisd_paged_offset adds offset[b] to the positions of request b's rows (behind a shared prefix: its length; after evictions: the number of tokens
  * that are gone), so that heisd_rope turns them as if nothing was missing.  Negative positions stay; sums outside 0 .. 2^31 - 1 become -1.
  *   offset     DEVICE i32 [batch]       position  DEVICE i32 [rows] in, out

@@ -13,7 +13,7 @@ struct CopyArgs {
   const int32_t *from;
   float *weight;                                    // or null
   long long layer_bytes, layer_weights;
-  int blocks, head_dim;                             // blocks: of the longest request
+  int max_seq, head_dim;
 };
 
 // One workgroup per block of 16-byte pieces of a request, block and layer.  A block's cells of all heads lie together in the source and in the
@@ -24,8 +24,8 @@ constexpr int kCopyPieces = 4;
 __global__ __launch_bounds__(256) void kv4_copy_blocks(Kv4Cache c, PagedBatch b, CopyArgs a, int per_block) {
   const int req = blockIdx.y, from = a.from[req];
   if (from < 0 || from >= b.batch || from == req) return;
-  const int n = b.seq_len[req], j = blockIdx.x / per_block, bs = c.block_size;
-  if (n <= 0 || (long long)n > (long long)b.max_blocks * bs || (long long)j * bs >= n) return;
+  const int all = b.seq_len[req], n = min(all, a.max_seq), j = blockIdx.x / per_block, bs = c.block_size;
+  if (n <= 0 || (long long)all > (long long)b.max_blocks * bs || (long long)j * bs >= n) return;
   const int to_id = b.table[(long long)req * b.max_blocks + j], from_id = b.table[(long long)from * b.max_blocks + j];
   if (to_id < 0 || to_id >= c.n_blocks || from_id < 0 || from_id >= c.n_blocks || to_id == from_id) return;
   const int used = min((n - j * bs + 15) & ~15, bs);
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void kv4_copy_blocks(Kv4Cache c, PagedBatch b,
   const int piece0 = (blockIdx.x % per_block) * (256 * kCopyPieces) + threadIdx.x;
   const uint8_t *src = c.at(from_id, 0);
   uint8_t *dst = c.at(to_id, 0);
-  const int codes = bs * (a.head_dim / 2), all = c.kv_heads * (int)(c.cell / 16);
+  const int codes = bs * (a.head_dim / 2), pieces = c.kv_heads * (int)(c.cell / 16);
   u32x4 x[kCopyPieces];
   bool ok[kCopyPieces];
 #pragma unroll
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void kv4_copy_blocks(Kv4Cache c, PagedBatch b,
       o -= 2 * codes;
       if (o >= bs * per_token) o -= bs * per_token;
     }
-    ok[i] = p < all && o < used * per_token;
+    ok[i] = p < pieces && o < used * per_token;
     if (ok[i]) x[i] = *reinterpret_cast<const u32x4 *>(src + (long long)p * 16);
   }
 #pragma unroll

@@ -10,7 +10,7 @@ import paged_reference as ref
 
 torch = pytest.importorskip("torch")
 from test_gpu_branch import WIDE, check_select, check_shared, check_weigh, prefix_of, run_select, shared  # noqa: E402
-from test_gpu_paged import DEV, Cache, host, i32, randn, tolerance  # noqa: E402
+from test_gpu_paged import DEV, Cache, host, i32, ok, randn, stream, tolerance  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -215,6 +215,27 @@ def test_weights_of_requests_longer_than_the_bounds_of_sharing(P):
                 off = np.expm1(2 * (72 * 2.0 ** -24 * size + 2.0 ** -22 * (size + large + 1))) + (4 * m + 32) * 2.0 ** -24
                 assert np.all(np.abs(got[slot] - (want + 0.5 * old)) <= off * want + 2.0 ** -23 * (want + 0.5 * old) + 2.0 ** -100), (step, i)
             at += m
+
+
+# ---- copies ------------------------------------------------------------------------------------------------------------------
+
+def test_copies_end_where_they_are_told_to(P):
+    """Of requests longer than max_seq the tokens before it are copied; the weights of those behind stay."""
+    rng = np.random.default_rng(7)
+    c = Cache(P, rng, [60, 60], 2, 64, 64)
+    k, v = (randn(rng, (120, 2, 64), "bf16") for _ in range(2))
+    c.write(P, k, v)
+    weight = torch.rand((c.n_blocks, 2, 64), device=DEV)
+    want, source = host(weight), i32([-1, 0])
+    for most in (1, 37, 59):
+        ok(P, P.heisd_kv4_copy(c.desc, 1, 0, P.make_paged_batch(c.t_table, c.t_seq, None, 0), source.data_ptr(), weight.data_ptr(), most, stream()))
+        got = [host(x) for x in c.read(P)]
+        want[c.table[1, 0], :, :most] = want[c.table[0, 0], :, :most]
+        assert np.array_equal(host(weight), want)
+        for x, y in zip(got, (k, v)):
+            last = -(-most // 16) * 16                                 # whole tiles of 16 tokens
+            held = ref.held(host(y))
+            assert np.array_equal(x[60:60 + min(last, 60)], held[:min(last, 60)]) and np.array_equal(x[60 + last:], held[60 + last:])
 
 
 # ---- the next beams ----------------------------------------------------------------------------------------------------------
