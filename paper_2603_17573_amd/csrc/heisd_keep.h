@@ -522,8 +522,12 @@ __global__ __launch_bounds__(kEvictThreads) void kv4_evict_held(Kv4Cache cache, 
   float w[E];
   if (t0 < k.n) {                                   // E is a part of 16, so these are in one block
     const float *from = k.w_in + k.weight_at(t0);
+    typedef f32x4 __attribute__((aligned(4))) four;              // weights may begin at any float
 #pragma unroll
-    for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4 *>(w + i) = *reinterpret_cast<const f32x4 *>(from + i);
+    for (int i = 0; i < E; i += 4) {
+      const four x = *reinterpret_cast<const four *>(from + i);
+      w[i] = x[0], w[i + 1] = x[1], w[i + 2] = x[2], w[i + 3] = x[3];
+    }
   }
 #pragma unroll
   for (int i = 0; i < E; ++i) key[i] = t0 + i < k.cand ? evict_key(w[i]) : 0;

@@ -217,6 +217,30 @@ def test_weights_of_requests_longer_than_the_bounds_of_sharing(P):
             at += m
 
 
+def test_weights_at_any_address(P):
+    """Weights that begin at any float: eviction moves them as it moves aligned ones."""
+    rng = np.random.default_rng(6)
+    total, keep = [300, 90, 40], [100, 90, 7]
+    c = Cache(P, rng, total, 2, 64, 16)
+    k, v = (randn(rng, (sum(total), 2, 64), "bf16") for _ in range(2))
+    shape = (c.n_blocks, 2, 16)
+    w = torch.rand(shape, device=DEV)
+    got = []
+    for off in (0, 1, 2, 3):
+        c.write(P, k, v)
+        held = torch.full((2, w.numel() + 4), -7.0, device=DEV)
+        w_in, w_out = (x[off:off + w.numel()].view(shape) for x in held)
+        w_in.copy_(w)
+        c.t_seq = i32(total)
+        out, t_keep = i32([-7] * 3), i32(keep)
+        ok(P, P.heisd_kv4_evict(c.desc, 1, 0, P.make_paged_batch(c.t_table, c.t_seq, None, 0), t_keep.data_ptr(), 20, w_in.data_ptr(), w_out.data_ptr(),
+                                out.data_ptr(), 300, stream()))
+        torch.cuda.synchronize()
+        assert out.tolist() == [100, 90, 7] and held[:, :off].eq(-7).all() and held[:, off + w.numel():].eq(-7).all()
+        got.append((c.pool.clone(), w_out.clone()))
+    assert all(torch.equal(a, b) for x in got[1:] for a, b in zip(x, got[0]))
+
+
 # ---- copies ------------------------------------------------------------------------------------------------------------------
 
 def test_copies_end_where_they_are_told_to(P):
