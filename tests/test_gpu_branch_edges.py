@@ -274,6 +274,19 @@ def test_workspaces_hold_every_dtype(P, dtype):
         check_select(run_select(P, logits, beams, 5, score), logits, beams, 5, score)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("beams,vocab", [(5, 4095), (5, 4096), (5, 4097), (1, 524280)])
+def test_select_where_the_forms_meet_and_end(P, dtype, beams, vocab):
+    """The largest vocabulary of one launch, the smallest of two, the largest of all, at addresses that cut the first and last segments."""
+    rng = np.random.default_rng(vocab)
+    whole = randn(rng, (beams * vocab + 16,), dtype, spread=False)
+    score = torch.tensor(-5 * rng.random(beams), dtype=torch.float32, device=DEV)
+    for off in (0, 1, 3, 7):
+        logits = whole[off:off + beams * vocab].view(beams, vocab)
+        logits[0, 0] = logits[-1, -1] = 9.0                            # the first and the last token of the rows are among the best
+        check_select(run_select(P, logits, beams, 8, score), logits, beams, 8, score)
+
+
 def test_lengths_whose_power_ends(P):
     """A power of a length that passes 64 bits leaves every continuation its place."""
     logits = torch.tensor([[1.0], [2.0], [3.0]], device=DEV)
@@ -282,3 +295,33 @@ def test_lengths_whose_power_ends(P):
         o = run_select(P, logits, 3, 3, score, length, done, 0, power)
         assert sorted(o["beam"][0].tolist()) == [0, 1, 2] and o["token"][0].tolist() == [0, 0, 0], power
         assert sorted(o["score"][0].tolist()) == [-1.0, 0.0, 0.0] and sorted(o["length"][0].tolist()) == [4, 2001, 3000]
+
+
+# ---- two caches at once --------------------------------------------------------------------------------------------------------
+
+def test_weights_of_two_runs_on_two_streams(P):
+    """Weights that two caches in flight at once add up and copy are those that each has alone."""
+    from test_gpu_branch_steps import Run
+    found = []
+    for together in (False, True):
+        runs = [Run(P, np.random.default_rng(s), 1, 16, (8, 2), 128, "bf16", layers=2) for s in (1, 2)]
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()] if together else [torch.cuda.current_stream()] * 2
+        ins = []
+        for r in runs:
+            r.c.weights.zero_()
+            r.prompts([100])
+            r.new = i32([1] * r.n + [0])
+            ins.append([(r.inputs(r.n), randn(r.rng, (r.n, r.vocab), "bf16", spread=False)) for _ in range(6)])
+        cached = [i32([0] * r.n + [100]) for r in runs]
+        torch.cuda.synchronize()
+        for n in range(6):
+            for j, r in enumerate(runs):
+                with torch.cuda.stream(streams[j]):
+                    x, logits = ins[j][n]
+                    s, _ = r.step(cached[j], *([y[m] for y in x] for m in range(3)), logits)
+                    r.score = s["score"].view(-1)
+                    cached[j] = r.c.seq_len.clone()
+        torch.cuda.synchronize()
+        found.append([(r.c.weights.clone(), r.c.table.clone()) for r in runs])
+    for alone, both in zip(*found):
+        assert float(alone[0].sum()) > 0 and all(torch.equal(a, b) for a, b in zip(alone, both))
