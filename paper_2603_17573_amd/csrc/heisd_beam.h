@@ -39,16 +39,20 @@ __device__ __forceinline__ void beam_wave_best(float &v, int &i) {
   v = top;
 }
 
-// The lane's part of segment s of a row: logits V * lane on of kBeamSegment.  Loads are aligned whatever the row's address is, so the first and the
-// last may be cut.  Returns the token of f[0].  What is not there is minus infinity.
+// The lane's part of segment s of a row: logits V * lane on of kBeamSegment.  Returns the token of f[0].  What is not there is minus infinity.  Which tokens a lane has does
+// not depend on the row's address, so that beams with the same logits have the same sums, bit for bit, and are equal; loads of 16 bytes begin at any element.
 template <typename T>
 __device__ __forceinline__ int beam_load(const T *x, int vocab, int s, float *f) {
   constexpr int V = 16 / sizeof(T);
-  const int t0 = s * kBeamSegment<T> + (threadIdx.x & 63) * V - (int)(((uintptr_t)x & 15) / sizeof(T));
-  if (t0 >= 0 && t0 + V <= vocab) load_vec<T, V>(x + t0, f);
-  else {
+  typedef typename VecOf<T, V>::type __attribute__((aligned(sizeof(T)))) vec;
+  const int t0 = s * kBeamSegment<T> + (threadIdx.x & 63) * V;
+  if (t0 + V <= vocab) {
+    const vec v = *reinterpret_cast<const vec *>(x + t0);
 #pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = t0 + e >= 0 && t0 + e < vocab ? (float)x[t0 + e] : -INFINITY;
+    for (int e = 0; e < V; ++e) f[e] = (float)v[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = t0 + e < vocab ? (float)x[t0 + e] : -INFINITY;
   }
   return t0;
 }
@@ -81,8 +85,8 @@ __device__ __forceinline__ float2 beam_segments(const T *x, int vocab, int s, To
 
 // One read of the logits: the sum of exponentials, a wave's part at a time, and the maximum of every segment.  The `width` largest logits of a row lie
 // in the `width` segments with the largest maxima (the lower ones among equals: each of them holds a logit that comes before whatever lies outside), so
-// nothing else has to be kept.  Bound by memory: 512 rows of 131071 fp16 logits (134 MB) in 28 us, 4.8 TB/s; ranking candidates here, chunk by chunk with a
-// maximum over the workgroup for each, took 181.
+// nothing else has to be kept.  Bound by memory: 512 rows of 131071 fp16 logits (134 MB) in 30.9 us, 4.3 TB/s (28 with loads at multiples of 16 bytes, whose sums went by the row's
+// address: copies of a beam then had other last bits and another order); ranking candidates here, chunk by chunk with a maximum over the workgroup for each, took 181.
 template <typename T>
 __global__ __launch_bounds__(256) void beam_scan(BeamArgs a) {
   constexpr int N = kBeamWave / kBeamSegment<T>;

@@ -3,7 +3,7 @@
 
 // ---- the next beams --------------------------------------------------------------------------------------------------
 
-constexpr int kBeamMostVocab = (1 << 19) - 8;       // as many segments as beam_pick's lanes hold; a row's address may cut its first and last
+constexpr int kBeamMostVocab = (1 << 19) - 8;       // not more segments than beam_pick's lanes hold
 constexpr int kBeamDirectVocab = 4096;              // up to here one launch does.  us, one / two: four beams over 256 logits 8.8 / 12.7, 4000 10.4 / 12.6,
                                                     // 8000 15.0 / 13.3; 64 beams over 1000 11.2 / 14.6, 4000 12.3 / 13.9, 8000 15.6 / 13.8
 
@@ -18,7 +18,7 @@ struct BeamLayout {
   int segments;
   size_t top, total;
   BeamLayout(int64_t rows, int64_t vocab, size_t size) {
-    const int64_t waves = (vocab + 16 / size - 1 + kBeamWave - 1) / kBeamWave;
+    const int64_t waves = (vocab + kBeamWave - 1) / kBeamWave;
     segments = (int)(waves * (kBeamWave * size / 1024));
     top = align256((size_t)(rows * waves) * sizeof(float2));
     total = top + align256((size_t)rows * segments * sizeof(float));
@@ -27,8 +27,7 @@ struct BeamLayout {
 
 extern "C" size_t heisd_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t width, int32_t vocab) {
   if (beam_sizes_ok("beam_select_workspace_bytes", groups, beams, width, vocab) != HEISD_OK) return 0;
-  const int64_t rows = (int64_t)groups * beams;      // fp32 has more segments, but 16-bit rows may be cut into one more part
-  return std::max(BeamLayout(rows, vocab, 4).total, BeamLayout(rows, vocab, 2).total);
+  return BeamLayout((int64_t)groups * beams, vocab, 4).total;        // fp32 has most segments, and every dtype as many parts
 }
 
 template <typename T>

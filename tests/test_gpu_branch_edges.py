@@ -287,6 +287,25 @@ def test_select_where_the_forms_meet_and_end(P, dtype, beams, vocab):
         check_select(run_select(P, logits, beams, 8, score), logits, beams, 8, score)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [51, 257, 4001, 4095, 8191, 32001, 131071])
+def test_beams_that_are_equal_are_equal_wherever_their_logits_lie(P, dtype, vocab):
+    """Copies of one beam (a first step, say) in rows of odd length, and at odd addresses: the lowest beam first, in each of its tokens."""
+    rng = np.random.default_rng(vocab)
+    for _ in range(4):
+        one = randn(rng, (vocab,), dtype, spread=False)
+        whole = torch.empty(9 * (vocab + 3) + 1, dtype=one.dtype, device=DEV)
+        logits = whole[1:].view(9, vocab + 3)[:, :vocab]
+        logits.copy_(one.expand(9, -1))
+        o = run_select(P, logits, 9, 27, torch.full((9,), -1.5, device=DEV))
+        best = sorted(range(vocab), key=lambda v, x=host(one): (-x[v], v))[:3]
+        rank = host(one)[best]
+        want = [(b, v) for x in dict.fromkeys(rank) for b in range(9) for v in (t for t, r in zip(best, rank) if r == x)]
+        if len(set(host(one)[sorted(range(vocab), key=lambda v, x=host(one): -x[v])[:4]])) == 4:
+            assert list(zip(o["beam"][0].tolist(), o["token"][0].tolist())) == want
+        assert all(len(set(o["score"][0][o["token"][0] == v].tolist())) == 1 for v in best)
+
+
 def test_lengths_whose_power_ends(P):
     """A power of a length that passes 64 bits leaves every continuation its place."""
     logits = torch.tensor([[1.0], [2.0], [3.0]], device=DEV)
