@@ -530,9 +530,12 @@ int heisd_paged_prompt_attention(const heisd_paged_batch *batch, const heisd_hea
  * What is said above of the calls on paged requests holds for these, too.
  *
  * Beam search's choice: of every group of `beams` beams the `width` best continuations, by score / length^length_power.
- *   score of token v behind beam i: score_in[i] + logits[i][v] - log(sum over v of exp(logits[i][v])), in 64 bits, rounded once in score_out;
- *   its length is length_in[i] + 1 (a power that 64 bits do not hold counts as the smallest or largest number that they do).  A beam with done_in != 0 goes on once, as it is (score, length), in the place of end_token.
- *   Equal ones: the lowest beam, then the lowest token.  NaN and minus infinity are no continuations (and add nothing to the sum); a
+ *   score of token v behind beam i: score_in[i] + logits[i][v] - log(sum over v of exp(logits[i][v])), added in 64 bits and rounded once in score_out.  The
+ *   exponentials and the sums of up to 2048 of them are fp32, joined in 64 bits: the logarithm is off by at most 2^-18, and by the same
+ *   for beams with the same logits.  Its length is length_in[i] + 1 (a power that 64 bits do not hold counts as the smallest or largest number that they do).
+ *   A beam with done_in != 0 goes on once, as it is (score, length), in the place of end_token.
+ *   Equal ones: the lowest beam.  Of one beam: the larger logit, then the lowest token.  Continuations of different beams that are nearer than the logarithms are off may be in
+ *   either order.  NaN and minus infinity are no continuations (and add nothing to the sum); a
  *   beam whose score is minus infinity or NaN has none, nor has one with a logit of plus infinity.  Where there are fewer than `width`: beam and token -1, score
  *   minus infinity, length 0, done 1.
  *   logits     DEVICE [groups * beams][vocab], any dtype, row_stride elements apart (at any address that suits the dtype)
