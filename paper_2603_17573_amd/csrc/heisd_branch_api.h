@@ -158,7 +158,7 @@ static int groups_desc_ok(const char *who, const heisd_prefix_groups *g, PrefixG
 // us a call, narrow / wide on four waves / on eight, 4 query heads per key head, 8 key heads of 128, bf16, prefixes of up to 8191 tokens: eight groups of 64 columns 71.0 / 64.3 /
 // 63.8, of 96 90.8 / 68.4 / 67.0, of 128 166 / 77.7 / 74.1, of 192 200 / 101 / 90.1; two of 64 31.3 / 40.9 / 31.1, of 1792 394 / 137 / 122; one of 128 40.4 / 36.2 / 33.5, of 256 59.8 /
 // 39.6 / 42.2.  fp16: eight of 64 76.1 / 71.4 / 68.2, of 128 178 / 86.1 / 78.5; two of 64 32.9 / 44.6 / 32.8.  Heads of 64: eight of 64 59.7 / 45.7 / 50.1, of 128 144 / 57.8 / 60.1.  So the
-// two numbers below fit heads of 64; heads of 128 would have eight waves from the first column on.
+// two numbers below fit heads of 64; heads of 128 would nearly always have eight waves.
 // Own tokens whole (up to kWholeTokens) / cut, two groups of four requests of up to 250, 500 and 1000 own tokens 20.8 / 21.6, 17.4 / 20.1 and 21.6 / 23.6, eight of eight of up to 1000
 // 42.7 / 46.3, two of 64 of up to 900 with seven rows each 148 / 199; of up to 2000, for which the limit would have to be 4096, 23.8 / 26.7 and 50.6 / 56.9.
 constexpr int64_t kWideLeast = 64, kWideMany = 192, kWholeTokens = 1024, kSplitGroups = 512, kSplitTokens = 4096;

@@ -24,9 +24,9 @@ constexpr int wide_lds_bytes = 2 * 2 * kWideTokens * HD * 2 + 2 * kWideTokens;
 // Every workgroup takes an equal run of the work of all groups, as in kv4_attend; a unit is a step for 32 * W columns of a key head.
 // A probability enters the second product as two 16-bit numbers, itself and what its rounding left: bf16s (off by 2^-16 of it together) or fp16s (2^-21, or 2^-36 of the
 // largest), so that a prefix is as exact for many columns as for few.  One fp16 alone takes 87 us for 108, but it is off by up to 2^-11, which nothing averages out: fp16 rows
-// are then off by 0.00029 where their own rounding gives 0.00021, and more bf16 rows get another last bit.
+// are then off by 0.00027 to 0.00029 where their own rounding gives 0.00021, and more bf16 rows get another last bit.
 // W 8 where there are as many columns: the tokens become bf16 half as often (two prefixes of 3029 and 3855 tokens, 1792 columns, 8 key heads of 128, bf16: 108 us; with the own
-// tokens a call takes 122, with W 4 137).  51 GFLOP (77 with the second terms) at 470 TFLOP/s: matrix cores busy 31 %, vector units 35 %, the rest waiting, mostly for the
+// tokens a call takes 118 to 122, with W 4 137).  51 GFLOP (77 with the second terms) at 470 TFLOP/s: matrix cores busy 31 %, vector units 35 %, the rest waiting, mostly for the
 // step's barrier (two waves per SIMD are all that the registers allow).  Tried, with one term: one set of waves bringing tokens before and one after its products (90 for 87), equal
 // runs given up for a fixed number of cuts (134 for 120 then).  The scaled products, which take the 4-bit keys as they are, hold their sums to 2^-14 only.
 template <typename T, int HD, int W>

@@ -378,7 +378,7 @@ class PagedCache:
 
     def offset(self, offset):
         """Adds offset i32[max_batch] to the positions of this step's rows, request by request: the length of the prefix that a request's tokens lie behind, the
-        number of its tokens that were evicted.  Once per step, before rotate()."""
+        number of its tokens that were evicted.  Once per step, before rotate().  They are the caller's: after fork() a request has those of its parent (offset[parent])."""
         self._call(B.heisd_paged_offset, self.batch, _ints(offset, self.seq_len.shape, "offset", self.device), self.position.data_ptr())
 
     def share(self, first, prefix, max_rows, max_prefix=None, max_own=None):
